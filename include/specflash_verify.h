@@ -71,6 +71,7 @@ typedef enum {
 #define SF_DEVICE_TIMEOUT 0x4u   /* a bounded wait on a copy gave up (~1 s)   */
 #define SF_DEVICE_BAD_SEQLEN 0x8u /* seq_lens[b] outside [n_q, max_pages*16]   */
 #define SF_DEVICE_OUT_OF_PAGES 0x10u /* sf_kv_commit: free-page stack too small */
+#define SF_DEVICE_BAD_INDEX 0x20u /* group_starts / freq_axis: an entry out of range */
 
 /* Compile-time limits of the library (calls beyond them return an error). */
 #define SF_PAGE_SIZE 16      /* tokens per KV page                            */
@@ -80,6 +81,13 @@ typedef enum {
 #define SF_MAX_DRAFT 16      /* k: draft length                               */
 #define SF_MAX_DRAFT_ROWS 256 /* R: rows of one LM-head projection            */
 #define SF_MAX_VOCAB 8388608  /* V for sf_lm_head / sf_sample / sf_draft_sample */
+#define SF_MAX_NORM_DIM 32768 /* d of sf_add_rms_norm                         */
+#define SF_MAX_AXES 4         /* position axes of sf_kv_append                */
+
+/* Element types of the operators that take more than one. */
+#define SF_BF16 0
+#define SF_F32 1
+#define SF_E4M3 2
 
 /* Static string naming a status code. */
 const char *sf_status_string(int status);
@@ -388,6 +396,162 @@ size_t sf_visual_compress_workspace_size(int F, int N, int C, int d);
 
 int sf_visual_compress(const void *queries, const void *features, int F, int N, int C, int d,
                        void *out, void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* The decoder layer around the verification attention.  One layer of the    */
+/* target model is: sf_add_rms_norm, the q/k/v projection, sf_kv_append,     */
+/* sf_verify_attention or sf_shared_prefix_attention, the output projection, */
+/* sf_add_rms_norm, ...; the projections are plain matrix products.          */
+/*                                                                           */
+/* Each of these kernels waits for the previous kernel on the stream before  */
+/* it reads or writes any tensor, so all their arguments may come from it.   */
+/*                                                                           */
+/* Residual addition and root-mean-square norm: for each of T rows           */
+/*     h = x + residual            (h = x without a residual)                */
+/*     residual_out = h                                                      */
+/*     y = h * weight / sqrt(mean(h^2) + eps)                                */
+/* with h, the mean and y in fp32 (y comes from h before residual_out's      */
+/* rounding), and                                                            */
+/*     out_dtype SF_BF16: out = bf16(y), or                                  */
+/*     out_dtype SF_E4M3: per row (group 0) or per `group` = 128 columns     */
+/*       (the last group may be shorter) scale = max(max|y| / 448, 2^-126)   */
+/*       and out = e4m3(y / scale), so that out * scale stands for y.        */
+/* Infinities and NaN go through the formulas (a NaN in a group makes its    */
+/* scale NaN); nothing else is touched by them.                              */
+/*                                                                           */
+/* x             [T][d], `dtype` SF_BF16 or SF_F32, row stride x_stride.     */
+/* residual      as x, row stride residual_stride; NULL for none.            */
+/* weight        [d], weight_dtype SF_BF16 or SF_F32.                        */
+/* residual_out  as x, row stride residual_out_stride; may be `residual`     */
+/*               itself (same stride) or x; NULL where residual is NULL.     */
+/* out           [T][d], row stride out_stride; may be x itself where types  */
+/*               and strides agree.                                          */
+/* scales        fp32 [T][ceil(d / group)], or [T] for group 0; NULL with    */
+/*               SF_BF16.                                                    */
+/* Strides count elements.  0 <= T < 2^31 (0: nothing is done), 1 <= d <=    */
+/* SF_MAX_NORM_DIM; every pointer aligned to its element.  16-byte accesses  */
+/* are used where addresses, strides and d allow them, else one element at a */
+/* time.  One launch; asynchronous on `stream`; deterministic.               */
+/* ------------------------------------------------------------------------ */
+int sf_add_rms_norm(const void *x, const void *residual, const void *weight, int dtype,
+                    int weight_dtype, int T, int d, long long x_stride,
+                    long long residual_stride, float eps, void *residual_out,
+                    long long residual_out_stride, void *out, int out_dtype,
+                    long long out_stride, int group, float *scales, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary position encoding of new rows, and their keys' and values' way     */
+/* into the paged cache (Sec. 3.1: the draft block joins the cached prefix;  */
+/* the caches' layout is that of sf_verify_attention).                       */
+/*                                                                           */
+/* Row t of the T new rows belongs to sequence b: with row_starts NULL there */
+/* are T / B rows per sequence, else row_starts [B + 1] holds each           */
+/* sequence's first row (prompts of different lengths; rows from             */
+/* row_starts[B] on are padding: their q is rotated, nothing is appended).   */
+/* Row i of the n_b new rows of sequence b goes to cache position            */
+/* seq_lens[b] - n_b + i, so seq_lens counts the new rows, as               */
+/* sf_verify_attention expects and sf_kv_commit leaves it.  seq_lens[b] = 0  */
+/* marks an idle slot of the batch: its rows are not appended.               */
+/*                                                                           */
+/* Rotation: with n = rotary_dim / 2 pairs per head, pair j of row t turns by*/
+/*     angle = positions[freq_axis[j]][t] * inv_freq[j]                      */
+/*     (a, b) -> amplitude * (a cos - b sin, a sin + b cos),                 */
+/* pair j being elements (j, j + n), or (2j, 2j + 1) with `interleaved`;     */
+/* elements from rotary_dim on stay as they are.  Several axes (time, height */
+/* and width of visual tokens) are rows of `positions`.  The angle is taken  */
+/* modulo one turn in 64-bit fixed point, so its error does not grow with    */
+/* the position (cos and sin within 2^-21 for |positions| <= 2^24).          */
+/*                                                                           */
+/* q, k, v       [T][heads][head_dim], dtype SF_BF16 or SF_F32, innermost    */
+/*               stride 1, row and head strides in elements (views of one    */
+/*               fused projection).  q NULL with H_q 0: keys and values only.*/
+/* positions     int32 [axes][T], 1 <= axes <= SF_MAX_AXES; may be negative. */
+/* inv_freq      fp64 [n]: radians per position.                             */
+/* freq_axis     int32 [n], values in [0, axes); NULL: axis 0.  A value      */
+/*               outside sets SF_DEVICE_BAD_INDEX and reads axis 0.          */
+/* rotary_dim    even, in [0, head_dim]; 0: no rotation, and positions,      */
+/*               inv_freq and freq_axis may be NULL.                         */
+/* q_out         bf16 [T][H_q][head_dim], contiguous; may be q where q is    */
+/*               bf16 and contiguous.                                        */
+/* k_cache, v_cache  bf16 [num_pages][H_kv][16][head_dim], written at the    */
+/*               new rows' positions only.                                   */
+/* block_table   int32 [B][max_pages_per_seq]; seq_lens int32 [B].           */
+/* A position outside [0, 16 * max_pages_per_seq) sets SF_DEVICE_BAD_SEQLEN, */
+/* a page outside [0, num_pages) SF_DEVICE_BAD_PAGE, a row that row_starts   */
+/* puts in no sequence though it lies before row_starts[B]                   */
+/* SF_DEVICE_BAD_INDEX; such rows are not appended.                          */
+/* 0 <= T < 2^31 (0: nothing is done); 1 <= B <= 1024; head_dim a multiple   */
+/* of 8 in [8, 256]; page_size 16; H_q, H_kv <= 1024.                        */
+/* workspace     >= sf_kv_append_workspace_size() bytes, 256-byte aligned,   */
+/*               zero-filled before first use (status word).                 */
+/* sf_verify_attention reads the prefix before it waits for the kernel in    */
+/* front of it: it may follow the append of its own n_q draft rows directly, */
+/* but not the append of a prompt (another kernel must come between).        */
+/* sf_shared_prefix_attention may follow either.                             */
+/* ------------------------------------------------------------------------ */
+size_t sf_kv_append_workspace_size(void);
+
+int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long long q_row_stride,
+                 long long q_head_stride, long long k_row_stride, long long k_head_stride,
+                 long long v_row_stride, long long v_head_stride, const int32_t *positions,
+                 int axes, const double *inv_freq, const int32_t *freq_axis, int rotary_dim,
+                 int interleaved, float amplitude, const int32_t *block_table,
+                 const int32_t *seq_lens, const int32_t *row_starts, int T, int B, int H_q,
+                 int H_kv, int head_dim, int page_size, int num_pages, int max_pages_per_seq,
+                 void *q_out, void *k_cache, void *v_cache, void *workspace,
+                 size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Verification attention of a batch whose sequences share long prefixes     */
+/* (several questions about one video, several samples of one prompt): the   */
+/* prefix's keys and values are read once for all rows of its group instead  */
+/* of once per sequence.                                                     */
+/*                                                                           */
+/* Group g is the sequences group_starts[g] <= b < group_starts[g + 1]; its  */
+/* prefix is the first prefix_lens[g] tokens of the pages in                 */
+/* prefix_table[g].  Each sequence's own tokens follow: seq_lens[b] tokens   */
+/* in the pages of block_table[b], the last n_q of them the draft rows, so   */
+/* L_b = seq_lens[b] - n_q >= 0.  Row i of sequence b sees the whole prefix  */
+/* of its group and its own tokens 0 .. L_b + i; with that,                  */
+/*     s_t = softmax_scale * <q, k_t>, lse = ln sum_t exp(s_t),              */
+/*     out = sum_t exp(s_t - lse) * v_t.                                     */
+/* (The own tokens start on a page of their own; positions enter by the      */
+/* rotation of q and k alone.)  seq_lens[b] = 0 marks an idle slot of the    */
+/* batch: out = 0 and lse = -inf for its rows.  Groups may be empty, and     */
+/* prefixes may have length 0.                                               */
+/*                                                                           */
+/* q            bf16 [B][n_q][H_q][head_dim]                                 */
+/* k_cache, v_cache  bf16 [num_pages][H_kv][16][head_dim]                    */
+/* prefix_table int32 [num_groups][max_prefix_pages]                         */
+/* prefix_lens  int32 [num_groups], in [0, 16 * max_prefix_pages]            */
+/* group_starts int32 [num_groups + 1], ascending, first 0, last B; anything */
+/*              else sets SF_DEVICE_BAD_INDEX, and no sequence has a prefix. */
+/* block_table  int32 [B][max_pages_per_seq]                                 */
+/* seq_lens     int32 [B]: 0, or in [n_q, 16 * max_pages_per_seq]            */
+/* Lengths outside are clamped and flagged with SF_DEVICE_BAD_SEQLEN; a page */
+/* outside the pool reads as zeros, flagged with SF_DEVICE_BAD_PAGE.  What   */
+/* pages hold past a length (NaN too) has no effect.                         */
+/* out          bf16 [B][n_q][H_q][head_dim]; lse fp32 [B][n_q][H_q] or NULL.*/
+/* Limits: those of sf_verify_attention; 1 <= num_groups <= B.               */
+/* softmax_scale  0 selects 1/sqrt(head_dim).                                */
+/* workspace    >= sf_shared_prefix_attention_workspace_size(...) bytes,     */
+/*              256-byte aligned, zero-filled before first use.              */
+/* Accuracy: scores and softmax statistics in fp32, the softmax weights in   */
+/* bf16 for the product with V (relative rounding 2^-9 per weight, below     */
+/* that of the bf16 output).  Deterministic.                                 */
+/* ------------------------------------------------------------------------ */
+size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_kv, int head_dim,
+                                                 int num_groups, int max_prefix_pages,
+                                                 int max_pages_per_seq, int page_size);
+
+int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v_cache,
+                               const int32_t *prefix_table, const int32_t *prefix_lens,
+                               const int32_t *group_starts, const int32_t *block_table,
+                               const int32_t *seq_lens, int B, int n_q, int H_q, int H_kv,
+                               int head_dim, int page_size, int num_pages, int num_groups,
+                               int max_prefix_pages, int max_pages_per_seq, float softmax_scale,
+                               void *out, float *lse, void *workspace, size_t workspace_bytes,
+                               cudaStream_t stream);
 
 #ifdef __cplusplus
 }

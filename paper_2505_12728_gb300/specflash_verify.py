@@ -23,6 +23,7 @@ SF_DEVICE_BAD_TOKEN = 0x2
 SF_DEVICE_TIMEOUT = 0x4
 SF_DEVICE_BAD_SEQLEN = 0x8
 SF_DEVICE_OUT_OF_PAGES = 0x10
+SF_DEVICE_BAD_INDEX = 0x20
 PAGE_SIZE = 16
 
 EXPORTED_SYMBOLS = (
@@ -35,6 +36,8 @@ EXPORTED_SYMBOLS = (
     "sf_draft_tail_workspace_size", "sf_lm_head", "sf_sample", "sf_draft_sample",
     "sf_visual_compress_workspace_size", "sf_visual_compress",
     "sf_verify_lm_head_accept_workspace_size", "sf_verify_lm_head_accept",
+    "sf_add_rms_norm", "sf_kv_append_workspace_size", "sf_kv_append",
+    "sf_shared_prefix_attention_workspace_size", "sf_shared_prefix_attention",
 )
 
 _lock = threading.Lock()
@@ -115,6 +118,19 @@ def load_library(path: str | None = None):
         lib.sf_verify_lm_head_accept_workspace_size.restype = S
         lib.sf_verify_lm_head_accept.argtypes = [P, P, P, P, P, P, I, I, I, I, P, P, P, P, P, S, P]
         lib.sf_verify_lm_head_accept.restype = I
+        L = ctypes.c_longlong
+        lib.sf_add_rms_norm.argtypes = [P, P, P, I, I, I, I, L, L, F, P, L, P, I, L, I, P, P]
+        lib.sf_add_rms_norm.restype = I
+        lib.sf_kv_append_workspace_size.argtypes = []
+        lib.sf_kv_append_workspace_size.restype = S
+        lib.sf_kv_append.argtypes = [P, P, P, I, L, L, L, L, L, L, P, I, P, P, I, I, F, P, P, P, I,
+                                     I, I, I, I, I, I, I, P, P, P, P, S, P]
+        lib.sf_kv_append.restype = I
+        lib.sf_shared_prefix_attention_workspace_size.argtypes = [I] * 9
+        lib.sf_shared_prefix_attention_workspace_size.restype = S
+        lib.sf_shared_prefix_attention.argtypes = [P, P, P, P, P, P, P, P, I, I, I, I, I, I, I, I,
+                                                   I, I, F, P, P, P, S, P]
+        lib.sf_shared_prefix_attention.restype = I
         _lib = lib
         return lib
 
@@ -529,3 +545,223 @@ def visual_compress(queries, features, *, out=None, workspace=None, stream=None)
                                              _ptr(workspace), workspace.numel(),
                                              _stream_handle(stream)))
     return out
+
+
+# --------------------------------------------------------------------------- #
+# the decoder layer around the attention                                      #
+# --------------------------------------------------------------------------- #
+_DTYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float8_e4m3fn: 2}
+
+
+def _need_rows(t, name, dtype, shape):
+    """A CUDA tensor of this type and shape whose innermost dimension is
+    contiguous (its other strides are passed on)."""
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape
+            and (t.stride(-1) == 1 or t.shape[-1] == 1)):
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.shape[-1] != 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _new(shape, dtype, device, stream, zero=False):
+    """A tensor for a call on `stream`: allocated (and zeroed) in its order."""
+    make = torch.zeros if zero else torch.empty
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
+def add_rms_norm(x, weight, residual=None, *, eps=1e-6, out_dtype=torch.bfloat16, group=0, out=None,
+                 residual_out=None, scales=None, stream=None):
+    """sf_add_rms_norm: x bf16 or fp32 [T][d] (rows may be strided), residual like
+    x or None, weight bf16 or fp32 [d].  y = rms_norm(x + residual) * weight as
+    bf16, or with out_dtype (or out) float8_e4m3fn as 8-bit values with fp32
+    scales, one per row (group 0) or per 128 columns (group 128).
+    Returns (out [T][d], residual_out like x or None, scales [T][groups] or
+    None).  residual_out may be the residual itself."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    if x.dim() != 2:
+        raise ValueError(f"x has shape {tuple(x.shape)}, expected (T, d)")
+    shape, kind = x.shape, x.dtype
+    T, d = shape
+    if kind is not torch.bfloat16 and kind is not torch.float32:
+        raise TypeError(f"x must be bfloat16 or float32, got {kind}")
+    _need_rows(x, "x", kind, shape)
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("weight must be a bfloat16 or float32 torch.Tensor")
+    _need(weight, "weight", weight.dtype, (d,))
+    if residual is not None:
+        _need_rows(residual, "residual", kind, shape)
+        if residual_out is None:
+            residual_out = _new(shape, kind, x.device, stream)
+        _need_rows(residual_out, "residual_out", kind, shape)
+    elif residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    if out is None:
+        if out_dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise TypeError(f"out_dtype must be bfloat16 or float8_e4m3fn, got {out_dtype}")
+        out = _new(shape, out_dtype, x.device, stream)
+    elif not isinstance(out, torch.Tensor) or out.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise TypeError("out must be a bfloat16 or float8_e4m3fn torch.Tensor")
+    _need_rows(out, "out", out.dtype, shape)
+    if out.dtype is torch.float8_e4m3fn:
+        if group not in (0, 128):
+            raise ValueError(f"group={group}: 0 (a scale per row) or 128 columns")
+        groups = -(-d // group) if group else 1
+        if scales is None:
+            scales = _new((T, groups), torch.float32, x.device, stream)
+        _need(scales, "scales", torch.float32, (T, groups))
+    elif scales is not None or group:
+        raise ValueError("scales and group belong to float8_e4m3fn output")
+    _check(load_library().sf_add_rms_norm(
+        x.data_ptr(), _ptr(residual), weight.data_ptr(), _DTYPES[kind], _DTYPES[weight.dtype], T, d,
+        x.stride(0), 0 if residual is None else residual.stride(0), eps, _ptr(residual_out),
+        0 if residual_out is None else residual_out.stride(0), out.data_ptr(), _DTYPES[out.dtype],
+        out.stride(0), group, _ptr(scales), _stream_handle(stream)))
+    return out, residual_out, scales
+
+
+def kv_append_workspace_size() -> int:
+    return int(load_library().sf_kv_append_workspace_size())
+
+
+def kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_lens, *, axis=None,
+              row_starts=None, interleaved=False, amplitude=1.0, q_out=None, workspace=None,
+              stream=None):
+    """sf_kv_append: rotates the new rows' q and k and writes k and v into the
+    paged cache.  q [T][H_q][d] (None: keys and values only), k and v
+    [T][H_kv][d], bf16 or fp32, views of a fused projection allowed; positions
+    int32 [axes][T]; inv_freq fp64 [rotary_dim / 2] (None: no rotation, and no
+    positions); axis int32 [rotary_dim / 2] (None: axis 0); caches, block_table
+    and seq_lens (counting the new rows) as for verify_attention; row_starts
+    int32 [B + 1] for sequences of different numbers of new rows (None: T / B
+    each).  Returns q_out bf16 [T][H_q][d] or None."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a tensor [T][H_kv][d]")
+    T, H_kv, d = k.shape
+    kind = k.dtype
+    if kind is not torch.bfloat16 and kind is not torch.float32:
+        raise TypeError(f"k must be bfloat16 or float32, got {kind}")
+    _need_rows(k, "k", kind, k.shape)
+    _need_rows(v, "v", kind, k.shape)
+    dev = k.device
+    H_q = q_row = q_head = 0
+    if q is not None:
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("q must be a tensor [T][H_q][d] or None")
+        H_q = q.shape[1]
+        _need_rows(q, "q", kind, (T, H_q, d))
+        q_row, q_head, _ = q.stride()
+        if q_out is None:
+            q_out = _new((T, H_q, d), torch.bfloat16, dev, stream)
+        _need(q_out, "q_out", torch.bfloat16, (T, H_q, d))
+    elif q_out is not None:
+        raise ValueError("q_out needs a q")
+    _need(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B][max_pages]")
+    B, max_pages = block_table.shape
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a tensor [pages][H_kv][16][d]")
+    num_pages, page = k_cache.shape[0], k_cache.shape[2]
+    _need(k_cache, "k_cache", torch.bfloat16, (num_pages, H_kv, page, d))
+    _need(v_cache, "v_cache", torch.bfloat16, k_cache.shape)
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    axes = pairs = 0
+    if inv_freq is not None:
+        _need(inv_freq, "inv_freq", torch.float64)
+        if inv_freq.dim() != 1 or positions is None or positions.dim() != 2:
+            raise ValueError("inv_freq must be [rotary_dim / 2] and positions [axes][T]")
+        pairs, axes = inv_freq.shape[0], positions.shape[0]
+        _need(positions, "positions", torch.int32, (axes, T))
+        if axis is not None:
+            _need(axis, "axis", torch.int32, (pairs,))
+    elif positions is not None or axis is not None:
+        raise ValueError("positions and axis need inv_freq")
+    if row_starts is not None:
+        _need(row_starts, "row_starts", torch.int32, (B + 1,))
+    if workspace is None:
+        workspace = _new(kv_append_workspace_size(), torch.uint8, dev, stream, zero=True)
+    _need_workspace(workspace)
+    k_row, k_head, _ = k.stride()
+    v_row, v_head, _ = v.stride()
+    _check(load_library().sf_kv_append(
+        _ptr(q), k.data_ptr(), v.data_ptr(), _DTYPES[kind], q_row, q_head, k_row, k_head, v_row, v_head,
+        _ptr(positions), axes, _ptr(inv_freq), _ptr(axis), 2 * pairs, bool(interleaved), amplitude,
+        block_table.data_ptr(), seq_lens.data_ptr(), _ptr(row_starts), T, B, H_q, H_kv, d, page,
+        num_pages, max_pages, _ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return q_out
+
+
+def shared_prefix_attention_workspace_size(B, n_q, H_q, H_kv, head_dim, num_groups,
+                                           max_prefix_pages, max_pages_per_seq,
+                                           page_size=PAGE_SIZE) -> int:
+    n = load_library().sf_shared_prefix_attention_workspace_size(
+        B, n_q, H_q, H_kv, head_dim, num_groups, max_prefix_pages, max_pages_per_seq, page_size)
+    if n == 0:
+        raise SFError(1, "invalid shared-prefix shape: " + load_library().sf_last_error().decode())
+    return int(n)
+
+
+def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_starts,
+                            block_table, seq_lens, *, out=None, lse=None, workspace=None,
+                            softmax_scale=0.0, stream=None, with_lse=True):
+    """sf_shared_prefix_attention: verification attention of a batch whose
+    sequences share prefixes.  q bf16 [B][n_q][H_q][d]; k/v_cache bf16
+    [pages][H_kv][16][d]; group g = sequences group_starts[g] ..
+    group_starts[g + 1] - 1 (int32 [groups + 1]) with the prefix_lens[g] (int32
+    [groups]) tokens of the pages prefix_table[g] (int32 [groups][pages]);
+    block_table int32 [B][pages] and seq_lens int32 [B] (0: idle slot) describe
+    each sequence's own tokens, draft rows included.  Returns (out bf16
+    [B][n_q][H_q][d], lse fp32 [B][n_q][H_q] or None)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor [B][n_q][H_q][d]")
+    B, n_q, H_q, d = shape = q.shape
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a tensor [pages][H_kv][16][d]")
+    num_pages, H_kv, page, d2 = k_cache.shape
+    if d2 != d:
+        # the library sizes the caches' tensor maps from q's head_dim
+        raise ValueError("head_dim of q and caches differ")
+    _need(q, "q", torch.bfloat16)
+    _need(k_cache, "k_cache", torch.bfloat16)
+    _need(v_cache, "v_cache", torch.bfloat16, k_cache.shape)
+    _need(prefix_table, "prefix_table", torch.int32)
+    _need(block_table, "block_table", torch.int32)
+    if prefix_table.dim() != 2 or block_table.dim() != 2:
+        raise ValueError("prefix_table and block_table must be two-dimensional")
+    G, max_prefix = prefix_table.shape
+    max_pages = block_table.shape[1]
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected ({B}, max_pages)")
+    _need(prefix_lens, "prefix_lens", torch.int32, (G,))
+    _need(group_starts, "group_starts", torch.int32, (G + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    if out is None:
+        out = _new(shape, torch.bfloat16, q.device, stream)
+    _need(out, "out", torch.bfloat16, shape)
+    if lse is None and with_lse:
+        lse = _new((B, n_q, H_q), torch.float32, q.device, stream)
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (B, n_q, H_q))
+    if workspace is None:
+        workspace = _new(shared_prefix_attention_workspace_size(
+            B, n_q, H_q, H_kv, d, G, max_prefix, max_pages, page), torch.uint8, q.device, stream, zero=True)
+    _need_workspace(workspace)
+    _check(load_library().sf_shared_prefix_attention(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),
+        prefix_lens.data_ptr(), group_starts.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        B, n_q, H_q, H_kv, d, page, num_pages, G, max_prefix, max_pages, softmax_scale,
+        out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return out, lse
