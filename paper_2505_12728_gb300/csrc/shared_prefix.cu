@@ -1,100 +1,846 @@
 // shared_prefix.cu -- verification attention of a batch whose sequences share
-// long prefixes.  Row i of sequence b sees the prefix of its group and its own
-// tokens 0 .. L_b + i.
+// long prefixes, on the 5th-generation tensor cores.
 //
-// One warp per query row and head: each lane holds head_dim / 32 elements of q
-// and of the output, keys come one at a time, with the running maximum and sum
-// of the softmax.
+// Row i of sequence b sees the prefix of its group and its own tokens
+// 0 .. L_b + i.  The softmax over both parts is the merge of the softmaxes over
+// the parts (running maximum, sum and unnormalised output), so the work is a
+// list of segments, each a product of up to 256 query rows with a run of keys:
+//  * prefix segments (group, KV head, pair of row tiles): the rows of all of a
+//    group's sequences for one KV head, packed into tiles of 128 rows (whole
+//    tokens: floor(128 / g) tokens of g query heads), two tiles a segment.  The
+//    prefix's keys and values are copied to shared memory once for 256 rows.
+//  * own segments (sequence, KV head): the sequence's n_q * g rows against its
+//    own tokens, with the causal mask of the draft block.
+// The segments' key tiles (128 keys) lie on one axis, which is cut into one
+// equal range per SM by a cost rule (below); a CTA works through the pieces of
+// its range and leaves one partial result (maximum, sum, O in fp32) per piece
+// and row tile; shared_prefix_merge_kernel joins the partials of every row.
+//
+// The CTA has two streams, each with 128 softmax threads (one TMEM lane, one
+// query row a thread), a score buffer and an accumulator:
+//     TMEM columns  S_0 [0, 128)  S_1 [128, 256)  O_0 [256, 384)  O_1 [384, 512).
+// A piece with two row tiles gives one to each stream; a piece with one row tile
+// gives its even key tiles to stream 0 and its odd ones to stream 1 (two
+// partials), or, with one key tile, goes to the streams in turn.  So while one
+// stream's softmax runs, the tensor cores work for the other.
+// P = exp2(S') goes back over the scores as bf16 (the A operand of O += P V), so
+// a stream's next Q K^T is issued behind its P V; tcgen05 MMAs of one thread
+// execute in issue order.  One warp issues every MMA, one every copy.
+// K and V tiles go through one ring of 32 KB slots (16 KB with 64-wide heads).
+//
+// The running maximum is a reference that moves when a row's new maximum
+// exceeds it by more than kSpRescaleLog2, so rescaling O is rare.  The row sums
+// are sums of the fp32 weights.  P V takes the weights rounded to bf16 (up to 2^-8
+// of a weight, which averages out over many keys), and on every segment's first
+// key tile also what that rounding left, as a second bf16 term: rows with a
+// handful of visible keys have them there.
+// Every wait is bounded; a timeout sets SF_DEVICE_TIMEOUT and stops every role.
 #include <cmath>
+#include <mutex>
 
-#include "sf_device.cuh"
+#include "attn_common.cuh"
 #include "sf_host.h"
 
 namespace sf {
 
-constexpr int kSpThreads = 128;
+constexpr int kSpTile = 128;     // keys per tile, query rows per row tile
+constexpr int kSpTilePages = kSpTile / SF_PAGE_SIZE;
+constexpr int kSpThreads = 320;  // two softmax warpgroups, MMA warp, copy warp
+constexpr int kSpMmaWarp = 8, kSpCopyWarp = 9;
+constexpr int kSpMaxRegs = 168;  // three warps share a sub-partition's 16K registers
+constexpr uint32_t kSpTmemCols = 512;
+constexpr float kSpRescaleLog2 = 8.f;
+constexpr int kSpMergeThreads = 256;
+constexpr int kSpSmemMax = 227 * 1024;
+// Cost of a piece on the partition's axis: kSpCostSeg for a segment (its Q copy,
+// pipeline start and epilogue), kSpCostTile for a key tile of one row tile.
+constexpr uint32_t kSpCostSeg = 1, kSpCostTile = 1;
 
 struct SpParams {
-  const __nv_bfloat16 *q, *k_cache, *v_cache;
   const int32_t *prefix_table, *prefix_lens, *group_starts, *block_table, *seq_lens;
   __nv_bfloat16 *out;
   float *lse;
   uint32_t *status;
+  float *part_o;   // unnormalised outputs, [D / 4][rows] float4 per piece and row tile
+  float2 *part_ml; // maximum (base-2 units) and sum of every row of a partial
   int B, n_q, H_q, H_kv, group, num_pages, num_groups, max_prefix_pages, max_pages;
+  int tokens_per_tile;  // floor(128 / group)
+  int oob_row;          // a tensor-map row beyond the pool: loads as zeros
+  int G;                // CTAs of the split kernel
   float scale_log2;
 };
 
-template <int D>
-__global__ void __launch_bounds__(kSpThreads) shared_prefix_kernel(const __grid_constant__ SpParams p) {
-  constexpr int E = D / 32;
-  constexpr float kLn2 = 0.6931471805599453f;
-  __shared__ int s_bad;
-  grid_dependency_wait();
-  if (threadIdx.x == 0) s_bad = p.group_starts[0] != 0 || p.group_starts[p.num_groups] != p.B;
-  __syncthreads();
-  for (int g = threadIdx.x; g < p.num_groups; g += kSpThreads)
-    if (p.group_starts[g + 1] < p.group_starts[g]) s_bad = 1;
-  __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row = static_cast<long long>(blockIdx.x) * (kSpThreads / 32) + warp;
-  if (row >= static_cast<long long>(p.B) * p.n_q * p.H_q) return;
-  const int hq = static_cast<int>(row % p.H_q), h = hq / p.group;
-  const int bi = static_cast<int>(row / p.H_q), b = bi / p.n_q, i = bi - b * p.n_q;
-  int L = p.seq_lens[b];
-  const int most = p.max_pages * SF_PAGE_SIZE;
-  if (L != 0 && (L < p.n_q || L > most)) {
-    set_status(p.status, SF_DEVICE_BAD_SEQLEN);
-    L = L < p.n_q ? p.n_q : most;
+// The segments, in shared memory of every CTA of both kernels.  Entities are the
+// groups' prefixes, then the sequences' own tokens.
+struct SpPlan {
+  uint32_t *cost;  // [E + 1] cost of the entities before
+  uint32_t *slot;  // [E + 1] partial rows of the entities before
+  int *len;        // [E] keys
+  int *start;      // [num_groups + 1] first sequence of each group
+  uint32_t Tot, q, r;
+  int G;
+  // CTA c's range of the axis begins at start(c); c * r < G^2
+  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * q + c * r / static_cast<uint32_t>(G); }
+  __device__ __forceinline__ int owner(uint32_t x) const {
+    int c = static_cast<int>((static_cast<float>(x) + 0.5f) * (static_cast<float>(G) / static_cast<float>(Tot)));
+    c = c < 0 ? 0 : (c >= G ? G - 1 : c);
+    while (c > 0 && begin(c) > x) --c;
+    while (c + 1 < G && begin(c + 1) <= x) ++c;
+    return c;
   }
-  int P = 0, g = 0;
-  if (s_bad) {
-    set_status(p.status, SF_DEVICE_BAD_INDEX);
-  } else {
-    int lo = 0, hi = p.num_groups;  // the group: last g with starts[g] <= b
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (p.group_starts[mid] <= b) lo = mid + 1; else hi = mid;
-    }
-    g = lo - 1;
-    P = p.prefix_lens[g];
-    const int most_prefix = p.max_prefix_pages * SF_PAGE_SIZE;
-    if (P < 0 || P > most_prefix) {
-      set_status(p.status, SF_DEVICE_BAD_SEQLEN);
-      P = P < 0 ? 0 : most_prefix;
-    }
-  }
-  float q[E], o[E];
-  for (int e = 0; e < E; ++e) {
-    q[e] = __bfloat162float(p.q[row * D + lane * E + e]);
-    o[e] = 0.f;
-  }
-  float m = -INFINITY, l = 0.f;
-  for (int part = 0; part < 2 && L > 0; ++part) {
-    const int32_t *table = part ? p.block_table + static_cast<size_t>(b) * p.max_pages
-                                : p.prefix_table + static_cast<size_t>(g) * p.max_prefix_pages;
-    const int keys = part ? L - p.n_q + i + 1 : P;
-    for (int t = 0; t < keys; ++t) {
-      const int page = table[t / SF_PAGE_SIZE];
-      const bool in = page >= 0 && page < p.num_pages;
-      if (!in && t % SF_PAGE_SIZE == 0) set_status(p.status, SF_DEVICE_BAD_PAGE);
-      const size_t at = ((static_cast<size_t>(in ? page : 0) * p.H_kv + h) * SF_PAGE_SIZE + t % SF_PAGE_SIZE) * D + lane * E;
-      float s = 0.f, v[E];
-      for (int e = 0; e < E; ++e) {
-        s += in ? q[e] * __bfloat162float(p.k_cache[at + e]) : 0.f;
-        v[e] = in ? __bfloat162float(p.v_cache[at + e]) : 0.f;
-      }
-      for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-      s *= p.scale_log2;
-      const float top = fmaxf(m, s), w = exp2f(s - top), a = exp2f(m - top);
-      l = l * a + w;
-      for (int e = 0; e < E; ++e) o[e] = o[e] * a + w * v[e];
-      m = top;
-    }
-  }
-  for (int e = 0; e < E; ++e) p.out[row * D + lane * E + e] = __float2bfloat16_rn(L > 0 ? o[e] / l : 0.f);
-  if (p.lse && lane == 0) p.lse[row] = L > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+};
+
+__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) {
+  return 4 * (3 * (B + num_groups) + 2 + num_groups + 1);
 }
 
+// One entity: `tokens` query tokens from token0 on (rows of all its sequences)
+// against `keys` keys.
+struct SpEntity {
+  int keys, tokens, token0, tiles, pairs, key_tiles;
+  uint32_t head_cost;  // per KV head
+  uint32_t slot_rows;  // partial rows of one piece
+};
+
+__device__ __forceinline__ SpEntity sp_entity(const SpParams &p, const SpPlan &pl, int e) {
+  SpEntity x;
+  x.keys = pl.len[e];
+  if (e < p.num_groups) {
+    x.token0 = pl.start[e] * p.n_q;
+    x.tokens = (pl.start[e + 1] - pl.start[e]) * p.n_q;
+  } else {
+    x.token0 = (e - p.num_groups) * p.n_q;
+    x.tokens = p.n_q;
+  }
+  x.tiles = (x.tokens + p.tokens_per_tile - 1) / p.tokens_per_tile;
+  x.pairs = (x.tiles + 1) >> 1;
+  x.key_tiles = (x.keys + kSpTile - 1) / kSpTile;
+  x.head_cost = x.keys > 0 ? static_cast<uint32_t>(x.pairs) * kSpCostSeg +
+                                 static_cast<uint32_t>(x.key_tiles) * static_cast<uint32_t>(x.tiles) * kSpCostTile
+                           : 0u;
+  x.slot_rows = x.tiles > 1 ? 2u * kSpTile : 2u * static_cast<uint32_t>(x.tokens * p.group);
+  return x;
+}
+
+// Lengths and prefix sums over the entities; every thread of the block calls it.
+template <int NT>
+__device__ SpPlan sp_plan(const SpParams &p, int *mem, uint32_t (*s_warp)[2]) {
+  const int E = p.num_groups + p.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  SpPlan pl;
+  pl.cost = reinterpret_cast<uint32_t *>(mem);
+  pl.slot = pl.cost + E + 1;
+  pl.len = reinterpret_cast<int *>(pl.slot + E + 1);
+  pl.start = pl.len + E;
+  int bad = 0;
+  for (int g = tid; g <= p.num_groups; g += NT) {
+    const int s = p.group_starts[g];
+    pl.start[g] = s;
+    bad |= g == 0 ? s != 0 : s < p.group_starts[g - 1];
+    bad |= g == p.num_groups && s != p.B;
+  }
+  for (int e = tid; e < E; e += NT) {
+    const bool own = e >= p.num_groups;
+    int n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
+    const int least = own ? p.n_q : 0, most = (own ? p.max_pages : p.max_prefix_pages) * SF_PAGE_SIZE;
+    if ((n < least || n > most) && n != 0) {
+      set_status(p.status, SF_DEVICE_BAD_SEQLEN);
+      n = n < least ? least : most;
+    }
+    pl.len[e] = n;
+  }
+  bad = __syncthreads_or(bad);
+  if (bad) {  // malformed groups: no sequence has a prefix
+    for (int g = tid; g <= p.num_groups; g += NT) pl.start[g] = 0;
+    if (tid == 0) set_status(p.status, SF_DEVICE_BAD_INDEX);
+    __syncthreads();
+  }
+  const int per = (E + NT - 1) / NT, e0 = tid * per;
+  uint32_t c = 0, s = 0;
+  for (int e = e0; e < e0 + per && e < E; ++e) {
+    const SpEntity x = sp_entity(p, pl, e);
+    c += x.head_cost * p.H_kv;
+    if (x.head_cost) s += x.slot_rows * x.pairs * p.H_kv;
+  }
+  uint32_t ci = c, si = s;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, ci, o), b = __shfl_up_sync(0xffffffffu, si, o);
+    if (lane >= o) {
+      ci += a;
+      si += b;
+    }
+  }
+  if (lane == 31) {
+    s_warp[warp][0] = ci;
+    s_warp[warp][1] = si;
+  }
+  __syncthreads();
+  uint32_t co = ci - c, so = si - s;
+  pl.Tot = 0;
+  for (int w = 0; w < NT / 32; ++w) {
+    if (w < warp) {
+      co += s_warp[w][0];
+      so += s_warp[w][1];
+    }
+    pl.Tot += s_warp[w][0];
+  }
+  for (int e = e0; e < e0 + per && e < E; ++e) {
+    const SpEntity x = sp_entity(p, pl, e);
+    pl.cost[e] = co;
+    pl.slot[e] = so;
+    co += x.head_cost * p.H_kv;
+    if (x.head_cost) so += x.slot_rows * x.pairs * p.H_kv;
+  }
+  if (tid == 0) pl.cost[E] = pl.Tot;
+  pl.G = pl.Tot < static_cast<uint32_t>(p.G) ? static_cast<int>(pl.Tot) : p.G;
+  pl.q = pl.G ? pl.Tot / pl.G : 0;
+  pl.r = pl.G ? pl.Tot % pl.G : 0;
+  __syncthreads();
+  return pl;
+}
+
+// First key tile of a segment (cost base `base`, `unit` per key tile) at or
+// behind position x of the axis.
+__device__ __forceinline__ int sp_tile_at(uint32_t x, uint32_t base, uint32_t unit, int key_tiles) {
+  const uint32_t b = base + kSpCostSeg;
+  if (x <= b) return 0;
+  const uint32_t t = (x - b + unit - 1) / unit;
+  return t < static_cast<uint32_t>(key_tiles) ? static_cast<int>(t) : key_tiles;
+}
+
+// The pieces of one CTA, in order.
+struct SpPiece {
+  int e, h, pair, dual;   // dual: two row tiles, one per stream
+  int t0, n;              // key tiles
+  uint32_t slot;          // its first partial row
+};
+
+struct SpWalk {
+  uint32_t at, end;       // the CTA's range
+  uint32_t base;          // cost base of the current segment
+  uint32_t slot;          // partial rows before the current segment
+  int e, h, pair;
+  SpEntity x;
+
+  __device__ __forceinline__ void init(const SpParams &p, const SpPlan &pl, int c) {
+    const int E = p.num_groups + p.B;
+    e = E;
+    at = end = 0;
+    if (c >= pl.G) return;
+    at = pl.begin(c);
+    end = pl.begin(c + 1);
+    int lo = 0, hi = E - 1;  // last entity whose cost base is <= at
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (pl.cost[mid] <= at) lo = mid; else hi = mid - 1;
+    }
+    e = lo;
+    x = sp_entity(p, pl, e);
+    const uint32_t in = at - pl.cost[e], pair_cost = kSpCostSeg + 2u * x.key_tiles * kSpCostTile;
+    h = static_cast<int>(in / x.head_cost);
+    pair = static_cast<int>((in - h * x.head_cost) / pair_cost);
+    base = pl.cost[e] + h * x.head_cost + pair * pair_cost;
+    slot = pl.slot[e] + (h * x.pairs + pair) * x.slot_rows;
+  }
+
+  // The next piece with keys; false behind the last.
+  __device__ __forceinline__ bool next(const SpParams &p, const SpPlan &pl, int c, SpPiece &pc) {
+    const int E = p.num_groups + p.B;
+    while (e < E && base < end) {
+      const int dual = 2 * pair + 1 < x.tiles;
+      const uint32_t unit = (1u + dual) * kSpCostTile;
+      const int t0 = sp_tile_at(at, base, unit, x.key_tiles), t1 = sp_tile_at(end, base, unit, x.key_tiles);
+      pc.e = e;
+      pc.h = h;
+      pc.pair = pair;
+      pc.dual = dual;
+      pc.t0 = t0;
+      pc.n = t1 - t0;
+      pc.slot = slot + 2u * kSpTile * c;
+      // the next segment
+      base += kSpCostSeg + unit * x.key_tiles;
+      slot += x.slot_rows;
+      if (++pair == x.pairs) {
+        pair = 0;
+        if (++h == p.H_kv) {
+          h = 0;
+          do ++e;
+          while (e < E && pl.cost[e + 1] == pl.cost[e]);  // entities without keys or rows
+          if (e < E) {
+            x = sp_entity(p, pl, e);
+            slot = pl.slot[e];
+          }
+        }
+      }
+      if (pc.n > 0) return true;
+    }
+    return false;
+  }
+};
+
+// What stream s does of a piece: its row tile and key tiles t0 + first, + step, ..
+struct SpJob {
+  int tile;         // row tile of the entity
+  int first, step;  // key tiles within the piece
+  int n;            // number of them (0: nothing for this stream)
+  uint32_t slot;    // first partial row
+};
+
+__device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int tile) {
+  const int left = x.tokens - tile * p.tokens_per_tile;
+  return (left < p.tokens_per_tile ? left : p.tokens_per_tile) * p.group;
+}
+
+// `turn`: the stream of the next piece of one row tile and one key tile.
+__device__ __forceinline__ SpJob sp_job(const SpPiece &pc, int s, int rows0, int &turn) {
+  SpJob j;
+  j.tile = 2 * pc.pair + (pc.dual ? s : 0);
+  if (pc.dual) {
+    j.first = 0;
+    j.step = 1;
+    j.n = pc.n;
+    j.slot = pc.slot + s * kSpTile;
+  } else if (pc.n > 1) {
+    j.first = s;
+    j.step = 2;
+    j.n = (pc.n + 1 - s) >> 1;
+    j.slot = pc.slot + s * rows0;
+  } else {
+    j.first = 0;
+    j.step = 1;
+    j.n = turn == s;
+    j.slot = pc.slot;
+    turn ^= 1;
+  }
+  return j;
+}
+
+template <int D, int STAGES>
+struct SpSmem {
+  static constexpr int kTileBytes = kSpTile * D * 2;  // a K, V or Q tile
+  static constexpr int kQOffset = STAGES * kTileBytes;
+  static constexpr int kBarOffset = kQOffset + 2 * kTileBytes;
+  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full, o_done; fin
+  static constexpr int kNumBars = 2 * STAGES + 11;
+  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars + 8;  // TMEM base, abort word, scan scratch
+  static constexpr int kPlanOffset = kMiscOffset + 16 + 8 * (kSpThreads / 32);
+};
+
+template <int N>
+__device__ __forceinline__ void sp_tmem_st(uint32_t taddr, const uint32_t (&v)[N]) {
+  if constexpr (N == 32) tmem_st_32x32b_x32(taddr, v);
+  else tmem_st_32x32b_x16(taddr, v);
+}
+
+template <int D, int STAGES>
+__global__ void __maxnreg__(kSpMaxRegs)
+shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                           const __grid_constant__ CUtensorMap tmap_q_tile,
+                           const __grid_constant__ CUtensorMap tmap_q_own,
+                           const __grid_constant__ SpParams p) {
+  using L = SpSmem<D, STAGES>;
+  constexpr int HALVES = D / 64;
+  constexpr int kPageBytes = SF_PAGE_SIZE * D * 2;
+  constexpr int kPageHalfBytes = SF_PAGE_SIZE * kRowBytes;
+  constexpr int kHalfTileBytes = kSpTile * kRowBytes;       // 64 columns of a Q tile
+  constexpr uint32_t kKSbo = HALVES == 2 ? 2048u : 1024u;   // 8-key atoms of a K tile
+  constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kSpTile, 0, 0);
+  constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, 0, 1);
+  constexpr int FULL = 0, EMPTY = STAGES, QFULL = 2 * STAGES, QEMPTY = QFULL + 2, SFULL = QEMPTY + 2,
+                PFULL = SFULL + 2, ODONE = PFULL + 2, FIN = ODONE + 2;
+
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t ring = smem_addr(smem);
+  auto bar = [&](int i) -> uint32_t { return ring + L::kBarOffset + 8u * static_cast<uint32_t>(i); };
+  int *s_misc = reinterpret_cast<int *>(smem + L::kMiscOffset);
+  volatile int *s_abort = s_misc + 1;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
+
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(bar(FULL + s), 1);
+      mbar_init(bar(EMPTY + s), 2);  // one arrival per stream that reads the tile, or two
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(QFULL + s), 1);
+      mbar_init(bar(QEMPTY + s), 1);
+      mbar_init(bar(SFULL + s), 1);
+      mbar_init(bar(PFULL + s), 4);
+      mbar_init(bar(ODONE + s), 1);
+    }
+    mbar_init(bar(FIN), 1);
+    fence_mbar_init();
+    prefetch_tensormap(&tmap_k);
+    prefetch_tensormap(&tmap_v);
+    prefetch_tensormap(&tmap_q_tile);
+    prefetch_tensormap(&tmap_q_own);
+    s_misc[1] = 0;
+  }
+  grid_dependency_wait();
+  // (behind the wait: the merge kernel reads the lengths as soon as it starts)
+  grid_launch_dependents();
+  const SpPlan pl = sp_plan<kSpThreads>(p, reinterpret_cast<int *>(smem + L::kPlanOffset),
+                                        reinterpret_cast<uint32_t(*)[2]>(s_misc + 4));
+  if (warp == kSpMmaWarp) {
+    tmem_alloc(smem_addr(s_misc), kSpTmemCols);
+    tmem_relinquish_alloc_permit();
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = static_cast<uint32_t>(s_misc[0]);
+  const int c = static_cast<int>(blockIdx.x);
+
+  SpWalk walk;
+  walk.init(p, pl, c);
+  SpPiece pc;
+
+  if (warp == kSpCopyWarp) {
+    // ------------------------------------------------------------------
+    // copies: a piece's Q tiles, then its key tiles' K and V, one box a page
+    // ------------------------------------------------------------------
+    const uint64_t once = l2_policy_evict_first(), again = l2_policy_evict_last();
+    uint32_t pos = 0;           // ring slots filled
+    uint32_t jobs[2] = {0, 0};  // Q tiles copied per stream
+    int turn = 0;
+    bool ok = true;
+    // every lane gets the answer of lane 0's bounded wait
+    auto wait = [&](uint32_t b, uint32_t parity) -> bool {
+      int w = 1;
+      if (lane == 0) w = mbar_wait_or_abort(b, parity, s_abort);
+      return __shfl_sync(0xffffffffu, w, 0) != 0;
+    };
+    while (ok && walk.next(p, pl, c, pc)) {
+      const bool own = pc.e >= p.num_groups;
+      const SpEntity x = sp_entity(p, pl, pc.e);
+      const int rows0 = sp_rows(p, x, 2 * pc.pair);
+      const int turn0 = turn;
+      for (int s = 0; s < 2 && ok; ++s) {
+        int tn = turn0;
+        const SpJob j = sp_job(pc, s, rows0, tn);
+        turn = tn;
+        if (j.n == 0) continue;
+        if (jobs[s] > 0) ok = wait(bar(QEMPTY + s), (jobs[s] - 1) & 1u);
+        if (!ok) break;
+        if (lane == 0) {
+          const int tokens = own ? p.n_q : p.tokens_per_tile;
+          mbar_arrive_expect_tx(bar(QFULL + s), static_cast<uint32_t>(tokens * p.group * D * 2));
+          const int token = x.token0 + j.tile * p.tokens_per_tile;
+          for (int hf = 0; hf < HALVES; ++hf)
+            tma_load_4d(ring + L::kQOffset + s * L::kTileBytes + hf * kHalfTileBytes, own ? &tmap_q_own : &tmap_q_tile,
+                        64 * hf, 0, pc.h, token, bar(QFULL + s), again);
+        }
+        __syncwarp();
+        ++jobs[s];
+      }
+      const int32_t *table = own ? p.block_table + static_cast<size_t>(pc.e - p.num_groups) * p.max_pages
+                                 : p.prefix_table + static_cast<size_t>(pc.e) * p.max_prefix_pages;
+      // (a prefix with more than one pair of row tiles is read again)
+      const uint64_t policy = !own && x.pairs > 1 ? again : once;
+      int ids = kBeyondEnd;
+      for (int it = 0; it < pc.n && ok; ++it) {
+        if ((it & 3) == 0) {  // page ids of the next four tiles, one a lane
+          const int lt = it + (lane >> 3), page = (pc.t0 + lt) * kSpTilePages + (lane & 7);
+          ids = lt < pc.n && page * SF_PAGE_SIZE < x.keys ? table[page] : kBeyondEnd;
+        }
+        const int phys = __shfl_sync(0xffffffffu, ids, ((it & 3) << 3) + (lane & 7));
+        int row = p.oob_row;  // pages past the end or outside the pool load as zeros
+        if (phys != kBeyondEnd) {
+          if (phys < 0 || phys >= p.num_pages) {
+            if (lane < kSpTilePages) set_status(p.status, SF_DEVICE_BAD_PAGE);
+          } else {
+            row = (phys * p.H_kv + pc.h) * SF_PAGE_SIZE;
+          }
+        }
+        for (int kv = 0; kv < 2 && ok; ++kv, ++pos) {
+          const uint32_t slot = pos % STAGES;
+          if (pos >= STAGES) ok = wait(bar(EMPTY + slot), (pos / STAGES - 1) & 1u);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(bar(FULL + slot), L::kTileBytes);
+          __syncwarp();
+          if (lane < kSpTilePages) {
+            const uint32_t dst = ring + slot * L::kTileBytes + lane * kPageBytes;
+            if (kv == 0) {
+              if constexpr (HALVES == 2) tma_load_4d(dst, &tmap_k, 0, 0, 0, row / 8, bar(FULL + slot), policy);
+              else tma_load_2d(dst, &tmap_k, 0, row, bar(FULL + slot), policy);
+            } else {
+              if constexpr (HALVES == 2) tma_load_3d(dst, &tmap_v, 0, row, 0, bar(FULL + slot), policy);
+              else tma_load_2d(dst, &tmap_v, 0, row, bar(FULL + slot), policy);
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      // stopped: the copies in flight land (bounded) before shared memory is left
+      for (int s = 0; s < 2; ++s)
+        if (jobs[s]) (void)mbar_wait_bounded(bar(QFULL + s), (jobs[s] - 1) & 1u);
+      for (uint32_t x = pos > STAGES ? pos - STAGES : 0; x < pos; ++x)
+        (void)mbar_wait_bounded(bar(FULL + x % STAGES), (x / STAGES) & 1u);
+    }
+    __syncwarp();
+  } else if (warp == kSpMmaWarp) {
+    // ------------------------------------------------------------------
+    // MMAs.  Each stream's operations alternate: Q K^T of a key tile (its K
+    // tile copied, and Q for a job's first tile), then P V (P written, V
+    // copied).  The warp looks at both streams in turn and issues what is ready.
+    // ------------------------------------------------------------------
+    SpWalk w[2] = {walk, walk};
+    SpPiece wp[2];
+    SpJob job[2];
+    int turn[2] = {0, 0};
+    uint32_t base[2] = {0, 0};  // ring tiles before the stream's piece
+    uint32_t next_base[2] = {0, 0};
+    int k[2] = {0, 0};          // key tile of the job
+    uint32_t jobs[2] = {0, 0}, tiles[2] = {0, 0};
+    bool live[2], pv[2] = {false, false};
+    auto advance = [&](int s) -> bool {  // the stream's next job
+      while (true) {
+        base[s] = next_base[s];
+        if (!w[s].next(p, pl, c, wp[s])) return false;
+        next_base[s] += wp[s].n;
+        job[s] = sp_job(wp[s], s, 0, turn[s]);
+        if (job[s].n > 0) {
+          k[s] = 0;
+          return true;
+        }
+      }
+    };
+#pragma unroll
+    for (int s = 0; s < 2; ++s) live[s] = advance(s);
+    unsigned long long t0 = 0;
+    uint32_t idle = 0;
+    bool ok = true;
+    while ((live[0] || live[1]) && ok) {
+      bool progress = false;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (!live[s]) continue;
+        const uint32_t ring_tile = base[s] + job[s].first + k[s] * job[s].step;
+        const uint32_t pos = 2u * ring_tile + pv[s], slot = pos % STAGES;
+        bool ready = mbar_test_wait(bar(FULL + slot), (pos / STAGES) & 1u);
+        if (!pv[s]) {
+          if (ready && k[s] == 0) ready = mbar_test_wait(bar(QFULL + s), jobs[s] & 1u);
+          if (!__all_sync(0xffffffffu, ready)) continue;
+          tc_fence_after_sync();
+          const uint64_t a0 = smem_desc_sw128(ring + L::kQOffset + s * L::kTileBytes, 16, 1024);
+          const uint64_t b0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
+          const bool last = k[s] + 1 == job[s].n;
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint64_t a = a0 + (((kk >> 2) * kHalfTileBytes + (kk & 3) * 32) >> 4);
+              const uint64_t b = b0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4);
+              tc_mma_ss(tmem + s * 128, a, b, kIdescQK, kk > 0 ? 1u : 0u);
+            }
+            tc_commit(bar(SFULL + s));
+            tc_commit(bar(EMPTY + slot));
+            if (!wp[s].dual) tc_commit(bar(EMPTY + slot));
+            if (last) tc_commit(bar(QEMPTY + s));
+          }
+          __syncwarp();
+          pv[s] = true;
+        } else {
+          if (ready) ready = mbar_test_wait(bar(PFULL + s), tiles[s] & 1u);
+          if (!__all_sync(0xffffffffu, ready)) continue;
+          tc_fence_after_sync();
+          const uint64_t b0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
+          const bool last = k[s] + 1 == job[s].n;
+          const bool two = wp[s].t0 + job[s].first + k[s] * job[s].step == 0;  // P_hi + P_lo
+          if (elect_one()) {
+#pragma unroll
+            for (int j = 0; j < kSpTilePages; ++j)
+              tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + j * 8, b0 + (j * kPageBytes >> 4), kIdescPV,
+                        k[s] == 0 && j == 0 ? 0u : 1u);
+            if (two) {
+#pragma unroll
+              for (int j = 0; j < kSpTilePages; ++j)
+                tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + 64 + j * 8, b0 + (j * kPageBytes >> 4), kIdescPV, 1u);
+            }
+            tc_commit(bar(EMPTY + slot));
+            if (!wp[s].dual) tc_commit(bar(EMPTY + slot));
+            if (last) tc_commit(bar(ODONE + s));
+          }
+          __syncwarp();
+          pv[s] = false;
+          ++tiles[s];
+          if (last) {
+            ++jobs[s];
+            live[s] = advance(s);
+          } else {
+            ++k[s];
+          }
+        }
+        progress = true;
+      }
+      if (progress) {
+        t0 = 0;
+      } else {
+        if ((++idle & 15u) != 0u) continue;
+        if (t0 == 0) t0 = global_timer_ns();
+        if (*s_abort) ok = false;
+        else if (global_timer_ns() - t0 > kWaitBudgetNs) {
+          *s_abort = 1;
+          ok = false;
+        }
+        ok = __all_sync(0xffffffffu, ok);
+      }
+    }
+    // every MMA issued has completed once this arrives
+    if (elect_one()) tc_commit(bar(FIN));
+    __syncwarp();
+    (void)mbar_wait_bounded(bar(FIN), 0);
+  } else {
+    // ------------------------------------------------------------------
+    // softmax and partial results: stream s = warpgroup, thread = query row
+    // ------------------------------------------------------------------
+    const int s = warp >> 2, r = tid & 127;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + s * 128 + lanes, to = tmem + 256 + s * 128 + lanes;
+    auto wwait = [&](uint32_t b, uint32_t parity) -> bool {
+      const bool w = mbar_wait_or_abort(b, parity, s_abort);
+      return __all_sync(0xffffffffu, w);
+    };
+    uint32_t base = 0, tiles = 0, jobs = 0;
+    int turn = 0;
+    bool ok = true;
+    while (ok && walk.next(p, pl, c, pc)) {
+      const bool own = pc.e >= p.num_groups;
+      const SpEntity x = sp_entity(p, pl, pc.e);
+      const SpJob job = sp_job(pc, s, sp_rows(p, x, 2 * pc.pair), turn);
+      const uint32_t piece_base = base;
+      base += pc.n;
+      if (job.n == 0) continue;
+      const int rows = sp_rows(p, x, job.tile);
+      const bool valid = r < rows;
+      // last visible key of this row (rows past the tile's end see every key:
+      // their scores are not used)
+      int lim = 0x7fffff00;
+      if (valid) lim = own ? x.keys - p.n_q + r / p.group : x.keys - 1;
+      float ref = -INFINITY, l_run = 0.f;
+      for (int k = 0; k < job.n; ++k, ++tiles) {
+        if (!(ok = wwait(bar(SFULL + s), tiles & 1u))) break;
+        tc_fence_after_sync();
+        uint32_t sv[128];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t part[64];
+          tmem_ld_32x32b_x64(ts + 64 * q, part);
+#pragma unroll
+          for (int i = 0; i < 64; ++i) sv[64 * q + i] = part[i];
+        }
+        const int in_piece = job.first + k * job.step;
+        const int tile_pos = (pc.t0 + in_piece) * kSpTile;
+        const int valid_keys = x.keys - tile_pos;
+        if (valid_keys < kSpTile && (valid_keys & (SF_PAGE_SIZE - 1)) != 0) {
+          // V rows of the last page past the end hold whatever the page holds:
+          // zeros there, so that 0 * v stays 0 (whole pages past the end are
+          // zeros already)
+          const uint32_t pos = 2u * (piece_base + in_piece) + 1u, slot = pos % STAGES;
+          if (!(ok = wwait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
+          uint8_t *vt = smem + slot * L::kTileBytes + (valid_keys / SF_PAGE_SIZE) * kPageBytes;
+          const int tok0 = valid_keys & (SF_PAGE_SIZE - 1);
+          for (int idx = r; idx < (SF_PAGE_SIZE - tok0) * HALVES * 8; idx += 128) {
+            const int tok = tok0 + idx / (HALVES * 8), rem = idx % (HALVES * 8);
+            *reinterpret_cast<uint4 *>(vt + (rem >> 3) * kPageHalfBytes + tok * kRowBytes + (rem & 7) * 16) =
+                make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+        }
+        if (tile_pos + kSpTile - 1 > lim) {
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (tile_pos + i > lim) sv[i] = __float_as_uint(-INFINITY);
+        }
+        float a0 = __uint_as_float(sv[0]), a1 = __uint_as_float(sv[1]), a2 = __uint_as_float(sv[2]),
+              a3 = __uint_as_float(sv[3]);
+#pragma unroll
+        for (int i = 4; i < 128; i += 4) {
+          a0 = fmaxf(a0, __uint_as_float(sv[i]));
+          a1 = fmaxf(a1, __uint_as_float(sv[i + 1]));
+          a2 = fmaxf(a2, __uint_as_float(sv[i + 2]));
+          a3 = fmaxf(a3, __uint_as_float(sv[i + 3]));
+        }
+        const float mx = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * p.scale_log2;
+        float alpha = 1.f;
+        if (mx > ref + kSpRescaleLog2) {
+          if (ref != -INFINITY) alpha = exp2f(ref - mx);
+          ref = mx;
+        }
+        if (__any_sync(0xffffffffu, alpha != 1.f)) {
+          // O *= alpha: the P V before this tile's Q K^T has completed with it
+#pragma unroll 1
+          for (int ch = 0; ch < D / 16; ++ch) {
+            uint32_t ov[16];
+            tmem_ld_32x32b_x16(to + ch * 16, ov);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * alpha);
+            tmem_st_32x32b_x16(to + ch * 16, ov);
+          }
+        }
+        const float mu = ref == -INFINITY ? 0.f : ref;
+        float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float p0 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i]), p.scale_log2, -mu));
+            const float p1 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i + 1]), p.scale_log2, -mu));
+            w[i] = pack_bf16x2(p0, p1);
+            sum0 += p0;
+            sum1 += p1;
+          }
+          tmem_st_32x32b_x16(ts + 16 * ch, w);
+        }
+        if (tile_pos == 0) {
+          // the first key tile: what P's rounding to bf16 left, as a second term
+#pragma unroll
+          for (int ch = 0; ch < 4; ++ch) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float p0 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i]), p.scale_log2, -mu));
+              const float p1 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i + 1]), p.scale_log2, -mu));
+              uint32_t hi;
+              split_bf16x2(p0, p1, hi, w[i]);
+            }
+            tmem_st_32x32b_x16(ts + 64 + 16 * ch, w);
+          }
+        }
+        l_run = l_run * alpha + (sum0 + sum1);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(PFULL + s));
+      }
+      if (ok) ok = wwait(bar(ODONE + s), jobs & 1u);
+      if (!ok) break;
+      ++jobs;
+      tc_fence_after_sync();
+      float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(job.slot) * D) + r;
+#pragma unroll 1
+      for (int ch = 0; ch < D / 32; ++ch) {
+        uint32_t ov[32];
+        tmem_ld_32x32b_x32(to + ch * 32, ov);
+        if (valid) {
+#pragma unroll
+          for (int q4 = 0; q4 < 8; ++q4)
+            dst[static_cast<size_t>(ch * 8 + q4) * rows] =
+                make_float4(__uint_as_float(ov[4 * q4]), __uint_as_float(ov[4 * q4 + 1]),
+                            __uint_as_float(ov[4 * q4 + 2]), __uint_as_float(ov[4 * q4 + 3]));
+        }
+      }
+      if (valid) p.part_ml[job.slot + r] = make_float2(ref, l_run);
+      tc_fence_before_sync();
+    }
+    tc_fence_before_sync();
+  }
+
+  __syncthreads();
+  if (*s_abort && tid == 0) set_status(p.status, SF_DEVICE_TIMEOUT);
+  if (warp == kSpMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, kSpTmemCols);
+  }
+}
+
+// --------------------------------------------------------------------------
+// The partials of every row, joined in piece order (deterministic):
+//   M = max_q m_q,  L = sum_q l_q 2^(m_q - M),  O = sum_q 2^(m_q - M) O_q / L,
+//   lse = (M + log2 L) ln 2.
+// One item per output quad (row, 4 columns); consecutive threads take
+// consecutive rows of one quad, as the partials lie.
+// --------------------------------------------------------------------------
+struct SpJoin {
+  float M, L;
+  float4 acc;
+  __device__ __forceinline__ void add(float2 ml, float4 o) {
+    const float top = fmaxf(M, ml.x);
+    const float a = fast_exp2(M - top), w = fast_exp2(ml.x - top);
+    if (top == -INFINITY) return;  // no visible key so far
+    L = L * a + ml.y * w;
+    acc.x = acc.x * a + o.x * w;
+    acc.y = acc.y * a + o.y * w;
+    acc.z = acc.z * a + o.z * w;
+    acc.w = acc.w * a + o.w * w;
+    M = top;
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void sp_join_segment(const SpParams &p, const SpPlan &pl, int e, const SpEntity &x, int h,
+                                                int tile, int r, int c4, SpJoin &jn) {
+  const int pair = tile >> 1, dual = 2 * pair + 1 < x.tiles, rows = sp_rows(p, x, tile);
+  const uint32_t unit = (1u + dual) * kSpCostTile;
+  const uint32_t base = pl.cost[e] + h * x.head_cost + pair * (kSpCostSeg + 2u * x.key_tiles * kSpCostTile);
+  const uint32_t seg_slot = pl.slot[e] + (h * x.pairs + pair) * x.slot_rows;
+  const int c1 = pl.owner(base + kSpCostSeg + unit * x.key_tiles - 1);
+  for (int c = pl.owner(base); c <= c1; ++c) {
+    const int n = sp_tile_at(pl.begin(c + 1), base, unit, x.key_tiles) - sp_tile_at(pl.begin(c), base, unit, x.key_tiles);
+    if (n <= 0) continue;
+    const int subs = dual || n == 1 ? 1 : 2;
+    for (int u = 0; u < subs; ++u) {
+      const size_t slot = seg_slot + 2u * kSpTile * c + (dual ? (tile & 1) * kSpTile : u * rows);
+      const float2 ml = p.part_ml[slot + r];
+      const float4 o = (reinterpret_cast<const float4 *>(p.part_o + slot * D) + r)[static_cast<size_t>(c4) * rows];
+      jn.add(ml, o);
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(const __grid_constant__ SpParams p) {
+  constexpr float kLn2 = 0.6931471805599453f;
+  constexpr int C4 = D / 4;
+  extern __shared__ int s_plan[];
+  __shared__ uint32_t s_warp[kSpMergeThreads / 32][2];
+  grid_launch_dependents();
+  const SpPlan pl = sp_plan<kSpMergeThreads>(p, s_plan, s_warp);
+  grid_dependency_wait();
+  const int R = p.n_q * p.group, per = R * C4;
+  const int units_per = (per + kSpMergeThreads - 1) / kSpMergeThreads;
+  const int units = p.B * p.H_kv * units_per;
+#pragma unroll 1
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int seg = unit / units_per, item = (unit - seg * units_per) * kSpMergeThreads + threadIdx.x;
+    if (item >= per) continue;
+    const int b = seg / p.H_kv, h = seg - b * p.H_kv;
+    const int c4 = item / R, r = item - c4 * R, i = r / p.group, j = r - i * p.group;
+    SpJoin jn;
+    jn.M = -INFINITY;
+    jn.L = 0.f;
+    jn.acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int e = p.num_groups + b;
+    const SpEntity own = sp_entity(p, pl, e);
+    if (own.keys > 0) {
+      int lo = 0, hi = p.num_groups;  // last group that starts at or before b
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (pl.start[mid] <= b) lo = mid + 1; else hi = mid;
+      }
+      const int g = lo - 1;
+      const SpEntity pre = sp_entity(p, pl, g);
+      if (pre.head_cost > 0) {
+        const int token = b * p.n_q + i - pre.token0, tile = token / p.tokens_per_tile;
+        sp_join_segment<D>(p, pl, g, pre, h, tile, (token - tile * p.tokens_per_tile) * p.group + j, c4, jn);
+      }
+      sp_join_segment<D>(p, pl, e, own, h, 0, r, c4, jn);
+    }
+    const size_t row = (static_cast<size_t>(b) * p.n_q + i) * p.H_q + static_cast<size_t>(h) * p.group + j;
+    const float inv = own.keys > 0 ? 1.f / jn.L : 0.f;
+    uint2 packed;
+    packed.x = pack_bf16x2(jn.acc.x * inv, jn.acc.y * inv);
+    packed.y = pack_bf16x2(jn.acc.z * inv, jn.acc.w * inv);
+    *reinterpret_cast<uint2 *>(p.out + row * D + 4 * c4) = packed;
+    if (p.lse && c4 == 0) p.lse[row] = own.keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
+  }
+}
+
+// --------------------------------------------------------------------------
+// host side
+// --------------------------------------------------------------------------
 static int check_sp_shapes(int B, int n_q, int H_q, int H_kv, int D, int num_groups, int max_prefix_pages,
                            int max_pages, int page_size) {
   if (B < 1 || B > SF_MAX_BATCH) return fail(SF_ERR_INVALID_ARG, "B=%d outside [1, %d]", B, SF_MAX_BATCH);
@@ -115,6 +861,109 @@ static int check_sp_shapes(int B, int n_q, int H_q, int H_kv, int D, int num_gro
   return SF_OK;
 }
 
+// Upper bounds over all groupings of B sequences into num_groups groups.
+struct SpBounds {
+  long long cost;  // length of the partition's axis
+  long long rows;  // partial rows
+};
+
+static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int max_prefix_pages, int max_pages, int G) {
+  const long long group = H_q / H_kv, per_tile = kSpTile / group, tokens = (long long)B * n_q;
+  const long long prefix_tiles = ((long long)max_prefix_pages + kSpTilePages - 1) / kSpTilePages;
+  const long long own_tiles = ((long long)max_pages + kSpTilePages - 1) / kSpTilePages;
+  // a group of t tokens has ceil(t / per_tile) <= t / per_tile + 1 row tiles, and
+  // at most half of that plus one pairs, of at most 2 * kSpTile partial rows each
+  const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
+  SpBounds b;
+  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostTile + B * (kSpCostSeg + own_tiles * kSpCostTile));
+  b.rows = H_kv * (pairs * 2 * kSpTile + 2 * tokens * group) + 2LL * kSpTile * G;
+  return b;
+}
+
+struct SpLayout {
+  size_t ml_off, o_off, total;
+};
+
+static SpLayout sp_layout(const SpBounds &b, int D) {
+  SpLayout l;
+  l.ml_off = 256;
+  l.o_off = round_up(l.ml_off + static_cast<size_t>(b.rows) * sizeof(float2), 256);
+  l.total = l.o_off + static_cast<size_t>(b.rows) * D * sizeof(float);
+  return l;
+}
+
+static int sp_grid(int *G) {
+  DeviceInfo dev;
+  const int st = current_device(&dev);
+  if (st != SF_OK) return st;
+  if (dev.max_smem_optin < kSpSmemMax)
+    return fail(SF_ERR_UNSUPPORTED, "needs %d B shared memory, device allows %d", kSpSmemMax, dev.max_smem_optin);
+  *G = dev.sm_count;
+  return SF_OK;
+}
+
+using SpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const SpParams);
+
+template <int D, int STAGES>
+static bool sp_variant(int plan_bytes, SpKernel *fn, int *smem) {
+  *fn = shared_prefix_split_kernel<D, STAGES>;
+  *smem = SpSmem<D, STAGES>::kPlanOffset + plan_bytes;
+  return *smem <= kSpSmemMax;
+}
+
+// The deepest ring that leaves room for the plan of B sequences.
+static void sp_select(int D, int B, int num_groups, SpKernel *fn, int *smem) {
+  const int plan = sp_plan_bytes(B, num_groups);
+  if (D == 128) {
+    if (!sp_variant<128, 5>(plan, fn, smem)) sp_variant<128, 4>(plan, fn, smem);
+  } else {
+    if (!sp_variant<64, 10>(plan, fn, smem)) sp_variant<64, 8>(plan, fn, smem);
+  }
+}
+
+static int sp_setup(int device) {
+  static std::mutex mu;
+  static bool done[64] = {};
+  if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
+  std::lock_guard<std::mutex> lock(mu);
+  if (done[device]) return SF_OK;
+  for (SpKernel fn : {static_cast<SpKernel>(shared_prefix_split_kernel<128, 5>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<128, 4>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 10>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 8>)}) {
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSpSmemMax);
+    if (e != cudaSuccess) return fail(SF_ERR_CUDA, "cudaFuncSetAttribute (shared prefix): %s", cudaGetErrorString(e));
+  }
+  done[device] = true;
+  return SF_OK;
+}
+
+// Tensor maps of one call: a page of K as [8-token group][half][8 tokens][128 B],
+// a page of V as [half][16 tokens][128 B], 64 columns of a row tile of Q.
+static int sp_maps(CUtensorMap (&m)[4], const void *k, const void *v, const void *q, uint64_t rows, int B, int n_q,
+                   int H_q, int H_kv, int D, int tokens_per_tile) {
+  int st;
+  if (D == 128) {
+    const uint64_t kd[4] = {64, 8, 2, rows / 8}, ks[3] = {256, 128, 2048};
+    const uint32_t kb[4] = {64, 8, 2, 2};
+    if ((st = encode_tensor_map_bf16(&m[0], k, 4, kd, ks, kb)) != SF_OK) return st;
+    const uint64_t vd[3] = {64, rows, 2}, vs[2] = {256, 128};
+    const uint32_t vb[3] = {64, SF_PAGE_SIZE, 2};
+    if ((st = encode_tensor_map_bf16(&m[1], v, 3, vd, vs, vb)) != SF_OK) return st;
+  } else {
+    const uint64_t d[2] = {64, rows}, s[1] = {128};
+    const uint32_t b[2] = {64, SF_PAGE_SIZE};
+    if ((st = encode_tensor_map_bf16(&m[0], k, 2, d, s, b)) != SF_OK) return st;
+    if ((st = encode_tensor_map_bf16(&m[1], v, 2, d, s, b)) != SF_OK) return st;
+  }
+  const uint64_t group = H_q / H_kv, e = 2ull * D;
+  const uint64_t qd[4] = {(uint64_t)D, group, (uint64_t)H_kv, (uint64_t)B * n_q}, qs[3] = {e, group * e, H_q * e};
+  const uint32_t qb[4] = {64, (uint32_t)group, 1, (uint32_t)tokens_per_tile};
+  if ((st = encode_tensor_map_bf16(&m[2], q, 4, qd, qs, qb)) != SF_OK) return st;
+  const uint32_t ob[4] = {64, (uint32_t)group, 1, (uint32_t)n_q};
+  return encode_tensor_map_bf16(&m[3], q, 4, qd, qs, ob);
+}
+
 }  // namespace sf
 
 extern "C" {
@@ -122,10 +971,12 @@ extern "C" {
 size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_kv, int head_dim,
                                                  int num_groups, int max_prefix_pages,
                                                  int max_pages_per_seq, int page_size) {
-  if (sf::check_sp_shapes(B, n_q, H_q, H_kv, head_dim, num_groups, max_prefix_pages, max_pages_per_seq,
-                          page_size) != SF_OK)
+  using namespace sf;
+  int G = 0;
+  if (check_sp_shapes(B, n_q, H_q, H_kv, head_dim, num_groups, max_prefix_pages, max_pages_per_seq, page_size) != SF_OK ||
+      sp_grid(&G) != SF_OK)
     return 0;
-  return 256;
+  return sp_layout(sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G), head_dim).total;
 }
 
 int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v_cache,
@@ -153,15 +1004,20 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
     return fail(SF_ERR_INVALID_ARG, "softmax_scale must be finite and >= 0");
   if (!workspace || !aligned(workspace, 256))
     return fail(SF_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
-  const size_t need = sf_shared_prefix_attention_workspace_size(B, n_q, H_q, H_kv, head_dim, num_groups,
-                                                                max_prefix_pages, max_pages_per_seq, page_size);
-  if (need == 0) return SF_ERR_CUDA;  // (sf_last_error says why)
-  if (workspace_bytes < need)
-    return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  DeviceInfo dev;
+  int G = 0;
+  if ((st = sp_grid(&G)) != SF_OK || (st = current_device(&dev)) != SF_OK) return st;
+  const SpBounds bounds = sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G);
+  if (bounds.cost >= (1LL << 31) || bounds.rows >= (1LL << 31))
+    return fail(SF_ERR_UNSUPPORTED, "up to %lld tiles and %lld partial rows (limits 2^31)", bounds.cost, bounds.rows);
+  const SpLayout lay = sp_layout(bounds, head_dim);
+  if (workspace_bytes < lay.total)
+    return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, lay.total);
+  if ((st = sp_setup(dev.ordinal)) != SF_OK) return st;
+
+  const uint64_t rows = (uint64_t)num_pages * H_kv * SF_PAGE_SIZE;
   SpParams p;
-  p.q = static_cast<const __nv_bfloat16 *>(q);
-  p.k_cache = static_cast<const __nv_bfloat16 *>(k_cache);
-  p.v_cache = static_cast<const __nv_bfloat16 *>(v_cache);
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
   p.prefix_table = prefix_table;
   p.prefix_lens = prefix_lens;
   p.group_starts = group_starts;
@@ -169,7 +1025,9 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.seq_lens = seq_lens;
   p.out = static_cast<__nv_bfloat16 *>(out);
   p.lse = lse;
-  p.status = static_cast<uint32_t *>(workspace);
+  p.status = reinterpret_cast<uint32_t *>(ws);
+  p.part_ml = reinterpret_cast<float2 *>(ws + lay.ml_off);
+  p.part_o = reinterpret_cast<float *>(ws + lay.o_off);
   p.B = B;
   p.n_q = n_q;
   p.H_q = H_q;
@@ -179,14 +1037,36 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.num_groups = num_groups;
   p.max_prefix_pages = max_prefix_pages;
   p.max_pages = max_pages_per_seq;
+  p.tokens_per_tile = kSpTile / p.group;
+  p.oob_row = static_cast<int>(rows);
+  p.G = G;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   p.scale_log2 = scale * 1.4426950408889634f;
-  const long long rows = static_cast<long long>(B) * n_q * H_q;
-  const unsigned grid = static_cast<unsigned>((rows + kSpThreads / 32 - 1) / (kSpThreads / 32));
-  if (head_dim == 128) shared_prefix_kernel<128><<<grid, kSpThreads, 0, stream>>>(p);
-  else shared_prefix_kernel<64><<<grid, kSpThreads, 0, stream>>>(p);
-  const cudaError_t e = cudaGetLastError();
+  CUtensorMap m[4];
+  if ((st = sp_maps(m, k_cache, v_cache, q, rows, B, n_q, H_q, H_kv, head_dim, p.tokens_per_tile)) != SF_OK) return st;
+
+  SpKernel fn;
+  int smem;
+  sp_select(head_dim, B, num_groups, &fn, &smem);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(G);
+  cfg.blockDim = dim3(kSpThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, fn, m[0], m[1], m[2], m[3], p);
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix attention launch: %s", cudaGetErrorString(e));
+  const long long units = (long long)B * H_kv * ((n_q * p.group * (head_dim / 4) + kSpMergeThreads - 1) / kSpMergeThreads);
+  cfg.gridDim = dim3(static_cast<unsigned>(units < 4LL * G ? units : 4LL * G));
+  cfg.blockDim = dim3(kSpMergeThreads);
+  cfg.dynamicSmemBytes = sp_plan_bytes(B, num_groups);
+  e = head_dim == 128 ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128>, p)
+                      : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64>, p);
+  if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix merge launch: %s", cudaGetErrorString(e));
   return SF_OK;
 }
 
