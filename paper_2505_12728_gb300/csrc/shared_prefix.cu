@@ -25,7 +25,11 @@
 // stream's softmax runs, the tensor cores work for the other.
 // P = exp2(S') goes back over the scores as bf16 (the A operand of O += P V), so
 // a stream's next Q K^T is issued behind its P V; tcgen05 MMAs of one thread
-// execute in issue order.  One warp issues every MMA, one every copy.
+// execute in issue order.  Each stream has a warp that issues its MMAs (one warp
+// for both, looking for what is ready, left the tensor cores idle for 300 cycles
+// before every operation: shared_long 349 -> XXX us); one warp copies K and V
+// and one Q, which has to wait for the stream's previous job while keys of the
+// next can be copied ahead.
 // K and V tiles go through one ring of 32 KB slots (16 KB with 64-wide heads).
 //
 // The running maximum is a reference that moves when a row's new maximum
@@ -45,8 +49,8 @@ namespace sf {
 
 constexpr int kSpTile = 128;     // keys per tile, query rows per row tile
 constexpr int kSpTilePages = kSpTile / SF_PAGE_SIZE;
-constexpr int kSpThreads = 320;  // two softmax warpgroups, MMA warp, copy warp
-constexpr int kSpMmaWarp = 8, kSpCopyWarp = 9;
+constexpr int kSpThreads = 384;  // two softmax warpgroups, two MMA warps, two copy warps
+constexpr int kSpMmaWarp = 8, kSpCopyWarp = 10, kSpQueryWarp = 11;
 constexpr int kSpMaxRegs = 168;  // three warps share a sub-partition's 16K registers
 constexpr uint32_t kSpTmemCols = 512;
 constexpr float kSpRescaleLog2 = 8.f;
@@ -320,16 +324,37 @@ struct SpSmem {
   static constexpr int kTileBytes = kSpTile * D * 2;  // a K, V or Q tile
   static constexpr int kQOffset = STAGES * kTileBytes;
   static constexpr int kBarOffset = kQOffset + 2 * kTileBytes;
-  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full, o_done; fin
-  static constexpr int kNumBars = 2 * STAGES + 11;
-  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars + 8;  // TMEM base, abort word, scan scratch
+  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full[2], o_done, fin, turn
+  static constexpr int kNumBars = 2 * STAGES + 16;
+  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word, scan scratch
   static constexpr int kPlanOffset = kMiscOffset + 16 + 8 * (kSpThreads / 32);
 };
 
-template <int N>
-__device__ __forceinline__ void sp_tmem_st(uint32_t taddr, const uint32_t (&v)[N]) {
-  if constexpr (N == 32) tmem_st_32x32b_x32(taddr, v);
-  else tmem_st_32x32b_x16(taddr, v);
+// max of three in one instruction (a NaN is ignored, as by fmaxf)
+__device__ __forceinline__ float sp_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// Two fp32 values in one 64-bit register: one instruction for both.
+__device__ __forceinline__ unsigned long long sp_pair(float x, float y) {
+  unsigned long long v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+  return v;
+}
+__device__ __forceinline__ void sp_unpair(unsigned long long v, float &x, float &y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long sp_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ unsigned long long sp_add2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
 
 template <int D, int STAGES>
@@ -347,7 +372,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kSpTile, 0, 0);
   constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, 0, 1);
   constexpr int FULL = 0, EMPTY = STAGES, QFULL = 2 * STAGES, QEMPTY = QFULL + 2, SFULL = QEMPTY + 2,
-                PFULL = SFULL + 2, ODONE = PFULL + 2, FIN = ODONE + 2;
+                PFULL = SFULL + 2, ODONE = PFULL + 4, FIN = ODONE + 2, TURN = FIN + 2;
 
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t ring = smem_addr(smem);
@@ -365,10 +390,12 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       mbar_init(bar(QFULL + s), 1);
       mbar_init(bar(QEMPTY + s), 1);
       mbar_init(bar(SFULL + s), 1);
-      mbar_init(bar(PFULL + s), 4);
+      mbar_init(bar(PFULL + 2 * s), 4);
+      mbar_init(bar(PFULL + 2 * s + 1), 4);
       mbar_init(bar(ODONE + s), 1);
+      mbar_init(bar(FIN + s), 1);
+      mbar_init(bar(TURN + s), 1);
     }
-    mbar_init(bar(FIN), 1);
     fence_mbar_init();
     prefetch_tensormap(&tmap_k);
     prefetch_tensormap(&tmap_v);
@@ -395,33 +422,27 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   walk.init(p, pl, c);
   SpPiece pc;
 
-  if (warp == kSpCopyWarp) {
+  if (warp == kSpQueryWarp) {
     // ------------------------------------------------------------------
-    // copies: a piece's Q tiles, then its key tiles' K and V, one box a page
+    // Q tiles, one per job, as soon as the stream's last Q K^T has read its Q
     // ------------------------------------------------------------------
-    const uint64_t once = l2_policy_evict_first(), again = l2_policy_evict_last();
-    uint32_t pos = 0;           // ring slots filled
-    uint32_t jobs[2] = {0, 0};  // Q tiles copied per stream
+    const uint64_t again = l2_policy_evict_last();
+    uint32_t jobs[2] = {0, 0};
     int turn = 0;
     bool ok = true;
-    // every lane gets the answer of lane 0's bounded wait
-    auto wait = [&](uint32_t b, uint32_t parity) -> bool {
-      int w = 1;
-      if (lane == 0) w = mbar_wait_or_abort(b, parity, s_abort);
-      return __shfl_sync(0xffffffffu, w, 0) != 0;
-    };
     while (ok && walk.next(p, pl, c, pc)) {
       const bool own = pc.e >= p.num_groups;
       const SpEntity x = sp_entity(p, pl, pc.e);
-      const int rows0 = sp_rows(p, x, 2 * pc.pair);
       const int turn0 = turn;
-      for (int s = 0; s < 2 && ok; ++s) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
         int tn = turn0;
-        const SpJob j = sp_job(pc, s, rows0, tn);
+        const SpJob j = sp_job(pc, s, 0, tn);
         turn = tn;
-        if (j.n == 0) continue;
-        if (jobs[s] > 0) ok = wait(bar(QEMPTY + s), (jobs[s] - 1) & 1u);
-        if (!ok) break;
+        if (j.n == 0 || !ok) continue;
+        int w = 1;
+        if (lane == 0 && jobs[s] > 0) w = mbar_wait_or_abort(bar(QEMPTY + s), (jobs[s] - 1) & 1u, s_abort);
+        if (!(ok = __shfl_sync(0xffffffffu, w, 0) != 0)) continue;
         if (lane == 0) {
           const int tokens = own ? p.n_q : p.tokens_per_tile;
           mbar_arrive_expect_tx(bar(QFULL + s), static_cast<uint32_t>(tokens * p.group * D * 2));
@@ -433,6 +454,29 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         __syncwarp();
         ++jobs[s];
       }
+    }
+    if (!ok && lane == 0) {  // stopped: the copies in flight land (bounded) before shared memory is left
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (jobs[s]) (void)mbar_wait_bounded(bar(QFULL + s), (jobs[s] - 1) & 1u);
+    }
+    __syncwarp();
+  } else if (warp == kSpCopyWarp) {
+    // ------------------------------------------------------------------
+    // K and V of the pieces' key tiles, one box a page
+    // ------------------------------------------------------------------
+    const uint64_t once = l2_policy_evict_first(), again = l2_policy_evict_last();
+    uint32_t pos = 0;  // ring slots filled
+    bool ok = true;
+    // every lane gets the answer of lane 0's bounded wait
+    auto wait = [&](uint32_t b, uint32_t parity) -> bool {
+      int w = 1;
+      if (lane == 0) w = mbar_wait_or_abort(b, parity, s_abort);
+      return __shfl_sync(0xffffffffu, w, 0) != 0;
+    };
+    while (ok && walk.next(p, pl, c, pc)) {
+      const bool own = pc.e >= p.num_groups;
+      const SpEntity x = sp_entity(p, pl, pc.e);
       const int32_t *table = own ? p.block_table + static_cast<size_t>(pc.e - p.num_groups) * p.max_pages
                                  : p.prefix_table + static_cast<size_t>(pc.e) * p.max_prefix_pages;
       // (a prefix with more than one pair of row tiles is read again)
@@ -473,124 +517,99 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       }
     }
     if (!ok && lane == 0) {
-      // stopped: the copies in flight land (bounded) before shared memory is left
-      for (int s = 0; s < 2; ++s)
-        if (jobs[s]) (void)mbar_wait_bounded(bar(QFULL + s), (jobs[s] - 1) & 1u);
       for (uint32_t x = pos > STAGES ? pos - STAGES : 0; x < pos; ++x)
         (void)mbar_wait_bounded(bar(FULL + x % STAGES), (x / STAGES) & 1u);
     }
     __syncwarp();
-  } else if (warp == kSpMmaWarp) {
+  } else if (warp >= kSpMmaWarp) {
     // ------------------------------------------------------------------
-    // MMAs.  Each stream's operations alternate: Q K^T of a key tile (its K
-    // tile copied, and Q for a job's first tile), then P V (P written, V
-    // copied).  The warp looks at both streams in turn and issues what is ready.
+    // MMAs of one stream, in order: Q K^T of a key tile (its K tile copied, and
+    // Q for a job's first tile), then P V of its first and second 64 keys
+    // (those weights written, V copied).  What the issuing branch needs is made
+    // warp-uniform outside of it.
+    // Two row tiles of one piece take turns: a stream issues P V of a tile and
+    // Q K^T of the next, then the other does.  Left to themselves both streams
+    // fall into step (the tensor cores serve them alternately, so both finish
+    // together) and the softmaxes run side by side while the tensor cores wait.
     // ------------------------------------------------------------------
-    SpWalk w[2] = {walk, walk};
-    SpPiece wp[2];
-    SpJob job[2];
-    int turn[2] = {0, 0};
-    uint32_t base[2] = {0, 0};  // ring tiles before the stream's piece
-    uint32_t next_base[2] = {0, 0};
-    int k[2] = {0, 0};          // key tile of the job
-    uint32_t jobs[2] = {0, 0}, tiles[2] = {0, 0};
-    bool live[2], pv[2] = {false, false};
-    auto advance = [&](int s) -> bool {  // the stream's next job
-      while (true) {
-        base[s] = next_base[s];
-        if (!w[s].next(p, pl, c, wp[s])) return false;
-        next_base[s] += wp[s].n;
-        job[s] = sp_job(wp[s], s, 0, turn[s]);
-        if (job[s].n > 0) {
-          k[s] = 0;
-          return true;
-        }
-      }
+    const int s = warp - kSpMmaWarp;
+    const uint32_t ts = __shfl_sync(0xffffffffu, tmem, 0) + s * 128u, to = ts + 256u;
+    const uint64_t q0 = smem_desc_sw128(ring + L::kQOffset + s * L::kTileBytes, 16, 1024);
+    auto wait = [&](uint32_t b, uint32_t parity) -> bool {
+      const bool w = mbar_wait_or_abort(b, parity, s_abort);
+      return __all_sync(0xffffffffu, w);
     };
-#pragma unroll
-    for (int s = 0; s < 2; ++s) live[s] = advance(s);
-    unsigned long long t0 = 0;
-    uint32_t idle = 0;
+    uint32_t base = 0, tiles = 0, jobs = 0, turns = 0;
+    int turn = 0;
     bool ok = true;
-    while ((live[0] || live[1]) && ok) {
-      bool progress = false;
+    // stream 1's i-th turn follows stream 0's, stream 0's next follows that
+    auto take_turn = [&]() -> bool {
+      const bool w = s == 0 ? (turns == 0 || wait(bar(TURN), (turns - 1) & 1u)) : wait(bar(TURN + 1), turns & 1u);
+      ++turns;
+      return w;
+    };
+    while (ok && walk.next(p, pl, c, pc)) {
+      const SpJob j = sp_job(pc, s, 0, turn);
+      uint32_t tile = __shfl_sync(0xffffffffu, base + j.first, 0);
+      base += pc.n;
+      const int n = __shfl_sync(0xffffffffu, j.n, 0), step = __shfl_sync(0xffffffffu, j.step, 0);
+      if (n == 0) continue;
+      const bool dual = __shfl_sync(0xffffffffu, pc.dual, 0) != 0;
+      bool two = __shfl_sync(0xffffffffu, pc.t0 + j.first, 0) == 0;  // the segment's first key tile: P_hi + P_lo
+      if (!(ok = wait(bar(QFULL + s), jobs & 1u))) break;
+      ++jobs;
+      for (int k = 0; k < n; ++k, tile += step, ++tiles) {
+        const bool last = k + 1 == n;
+        uint32_t pos = 2u * tile, slot = pos % STAGES;
+        if (!(ok = wait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
+        if (k == 0 && dual && !(ok = take_turn())) break;
+        tc_fence_after_sync();
+        const uint64_t k0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
+        if (elect_one()) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (!live[s]) continue;
-        const uint32_t ring_tile = base[s] + job[s].first + k[s] * job[s].step;
-        const uint32_t pos = 2u * ring_tile + pv[s], slot = pos % STAGES;
-        bool ready = mbar_test_wait(bar(FULL + slot), (pos / STAGES) & 1u);
-        if (!pv[s]) {
-          if (ready && k[s] == 0) ready = mbar_test_wait(bar(QFULL + s), jobs[s] & 1u);
-          if (!__all_sync(0xffffffffu, ready)) continue;
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_ss(ts, q0 + (((kk >> 2) * kHalfTileBytes + (kk & 3) * 32) >> 4),
+                      k0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), kIdescQK, kk > 0 ? 1u : 0u);
+          tc_commit(bar(SFULL + s));
+          tc_commit(bar(EMPTY + slot));
+          if (!dual) mbar_arrive(bar(EMPTY + slot));
+          if (last) tc_commit(bar(QEMPTY + s));
+          if (dual) mbar_arrive(bar(TURN + 1 - s));
+        }
+        __syncwarp();
+        ++pos;
+        slot = pos % STAGES;
+        if (!(ok = wait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
+        const uint64_t v0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (!(ok = wait(bar(PFULL + 2 * s + half), tiles & 1u))) break;
+          if (half == 0 && dual && !(ok = take_turn())) break;
           tc_fence_after_sync();
-          const uint64_t a0 = smem_desc_sw128(ring + L::kQOffset + s * L::kTileBytes, 16, 1024);
-          const uint64_t b0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
-          const bool last = k[s] + 1 == job[s].n;
           if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint64_t a = a0 + (((kk >> 2) * kHalfTileBytes + (kk & 3) * 32) >> 4);
-              const uint64_t b = b0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4);
-              tc_mma_ss(tmem + s * 128, a, b, kIdescQK, kk > 0 ? 1u : 0u);
+            for (int j = 0; j < kSpTilePages; ++j) {
+              if (j / (kSpTilePages / 2) != half) continue;
+              tc_mma_ts(to, ts + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, k > 0 || j > 0 ? 1u : 0u);
+              if (two) tc_mma_ts(to, ts + 64 + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, 1u);
             }
-            tc_commit(bar(SFULL + s));
-            tc_commit(bar(EMPTY + slot));
-            if (!wp[s].dual) tc_commit(bar(EMPTY + slot));
-            if (last) tc_commit(bar(QEMPTY + s));
+            if (half == 1) {
+              tc_commit(bar(EMPTY + slot));
+              if (!dual) mbar_arrive(bar(EMPTY + slot));
+              if (last) tc_commit(bar(ODONE + s));
+              if (last && dual) mbar_arrive(bar(TURN + 1 - s));
+            }
           }
           __syncwarp();
-          pv[s] = true;
-        } else {
-          if (ready) ready = mbar_test_wait(bar(PFULL + s), tiles[s] & 1u);
-          if (!__all_sync(0xffffffffu, ready)) continue;
-          tc_fence_after_sync();
-          const uint64_t b0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
-          const bool last = k[s] + 1 == job[s].n;
-          const bool two = wp[s].t0 + job[s].first + k[s] * job[s].step == 0;  // P_hi + P_lo
-          if (elect_one()) {
-#pragma unroll
-            for (int j = 0; j < kSpTilePages; ++j)
-              tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + j * 8, b0 + (j * kPageBytes >> 4), kIdescPV,
-                        k[s] == 0 && j == 0 ? 0u : 1u);
-            if (two) {
-#pragma unroll
-              for (int j = 0; j < kSpTilePages; ++j)
-                tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + 64 + j * 8, b0 + (j * kPageBytes >> 4), kIdescPV, 1u);
-            }
-            tc_commit(bar(EMPTY + slot));
-            if (!wp[s].dual) tc_commit(bar(EMPTY + slot));
-            if (last) tc_commit(bar(ODONE + s));
-          }
-          __syncwarp();
-          pv[s] = false;
-          ++tiles[s];
-          if (last) {
-            ++jobs[s];
-            live[s] = advance(s);
-          } else {
-            ++k[s];
-          }
         }
-        progress = true;
-      }
-      if (progress) {
-        t0 = 0;
-      } else {
-        if ((++idle & 15u) != 0u) continue;
-        if (t0 == 0) t0 = global_timer_ns();
-        if (*s_abort) ok = false;
-        else if (global_timer_ns() - t0 > kWaitBudgetNs) {
-          *s_abort = 1;
-          ok = false;
-        }
-        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        two = false;
       }
     }
     // every MMA issued has completed once this arrives
-    if (elect_one()) tc_commit(bar(FIN));
+    if (elect_one()) tc_commit(bar(FIN + s));
     __syncwarp();
-    (void)mbar_wait_bounded(bar(FIN), 0);
+    (void)mbar_wait_bounded(bar(FIN + s), 0);
   } else {
     // ------------------------------------------------------------------
     // softmax and partial results: stream s = warpgroup, thread = query row
@@ -656,12 +675,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         float a0 = __uint_as_float(sv[0]), a1 = __uint_as_float(sv[1]), a2 = __uint_as_float(sv[2]),
               a3 = __uint_as_float(sv[3]);
 #pragma unroll
-        for (int i = 4; i < 128; i += 4) {
-          a0 = fmaxf(a0, __uint_as_float(sv[i]));
-          a1 = fmaxf(a1, __uint_as_float(sv[i + 1]));
-          a2 = fmaxf(a2, __uint_as_float(sv[i + 2]));
-          a3 = fmaxf(a3, __uint_as_float(sv[i + 3]));
+        for (int i = 4; i < 124; i += 8) {
+          a0 = sp_max3(a0, __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+          a1 = sp_max3(a1, __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+          a2 = sp_max3(a2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+          a3 = sp_max3(a3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
         }
+        a0 = sp_max3(a0, __uint_as_float(sv[124]), __uint_as_float(sv[125]));
+        a1 = sp_max3(a1, __uint_as_float(sv[126]), __uint_as_float(sv[127]));
         const float mx = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * p.scale_log2;
         float alpha = 1.f;
         if (mx > ref + kSpRescaleLog2) {
@@ -681,39 +702,74 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         }
         const float mu = ref == -INFINITY ? 0.f : ref;
         float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float p0 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i]), p.scale_log2, -mu));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i + 1]), p.scale_log2, -mu));
-            w[i] = pack_bf16x2(p0, p1);
-            sum0 += p0;
-            sum1 += p1;
-          }
-          tmem_st_32x32b_x16(ts + 16 * ch, w);
-        }
-        if (tile_pos == 0) {
-          // the first key tile: what P's rounding to bf16 left, as a second term
+        if (tile_pos != 0) {
+          const unsigned long long scale2 = sp_pair(p.scale_log2, p.scale_log2), mu2 = sp_pair(-mu, -mu);
+          unsigned long long sum = 0ull;
 #pragma unroll
           for (int ch = 0; ch < 4; ++ch) {
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float p0 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i]), p.scale_log2, -mu));
-              const float p1 = fast_exp2(fmaf(__uint_as_float(sv[32 * ch + 2 * i + 1]), p.scale_log2, -mu));
-              uint32_t hi;
-              split_bf16x2(p0, p1, hi, w[i]);
+              const int k0 = 32 * ch + 2 * i;
+              float x0, x1;
+              sp_unpair(sp_fma2(sp_pair(__uint_as_float(sv[k0]), __uint_as_float(sv[k0 + 1])), scale2, mu2), x0, x1);
+              const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+              w[i] = pack_bf16x2(p0, p1);
+              sum = sp_add2(sum, sp_pair(p0, p1));
             }
-            tmem_st_32x32b_x16(ts + 64 + 16 * ch, w);
+            tmem_st_32x32b_x16(ts + 16 * ch, w);
+            if (ch == 1) {  // P V of the first 64 keys may begin
+              tmem_wait_st();
+              tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(PFULL + 2 * s));
+            }
+          }
+          sp_unpair(sum, sum0, sum1);
+        } else {
+          // A segment's first key tile: what P's rounding to bf16 left goes to
+          // columns [64, 128) as a second term.  The scores are read again, 64 at a
+          // time, so that the two terms need no more registers than the scores do
+          // above.
+          uint32_t hi[64];
+#pragma unroll
+          for (int q = 1; q >= 0; --q) {
+            uint32_t lo[64];
+            tmem_ld_32x32b_x64(ts + 64 * q, lo);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const int k0 = 64 * q + 2 * i;
+              const float p0 = k0 > lim ? 0.f : fast_exp2(fmaf(__uint_as_float(lo[2 * i]), p.scale_log2, -mu));
+              const float p1 = k0 + 1 > lim ? 0.f : fast_exp2(fmaf(__uint_as_float(lo[2 * i + 1]), p.scale_log2, -mu));
+              sum0 += p0;
+              sum1 += p1;
+              split_bf16x2(p0, p1, hi[32 * q + i], lo[i]);
+            }
+#pragma unroll
+            for (int x = 0; x < 32; x += 16) {
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[i] = lo[x + i];
+              // (keys 64 .. 127 are read first: their low parts replace their scores)
+              tmem_st_32x32b_x16(ts + 64 + 32 * q + x, w);
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < 64; x += 16) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = hi[x + i];
+            tmem_st_32x32b_x16(ts + x, w);
           }
         }
         l_run = l_run * alpha + (sum0 + sum1);
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(PFULL + s));
+        if (lane == 0) {
+          if (tile_pos == 0) mbar_arrive(bar(PFULL + 2 * s));
+          mbar_arrive(bar(PFULL + 2 * s + 1));
+        }
       }
       if (ok) ok = wwait(bar(ODONE + s), jobs & 1u);
       if (!ok) break;
