@@ -56,9 +56,11 @@ constexpr uint32_t kSpTmemCols = 512;
 constexpr float kSpRescaleLog2 = 8.f;
 constexpr int kSpMergeThreads = 256;
 constexpr int kSpSmemMax = 227 * 1024;
-// Cost of a piece on the partition's axis: kSpCostSeg for a segment (its Q copy,
-// pipeline start and epilogue), kSpCostTile for a key tile of one row tile.
-constexpr uint32_t kSpCostSeg = 1, kSpCostTile = 1;
+// Cost of a segment on the partition's axis, in key tiles of one row tile: one
+// for each of its row tiles' key tiles, and kSpCostSeg for itself (its Q copy,
+// pipeline start and epilogue).
+constexpr uint32_t kSpCostSeg = 2;
+constexpr int kSpItems = 4;      // pieces published ahead
 
 struct SpParams {
   const int32_t *prefix_table, *prefix_lens, *group_starts, *block_table, *seq_lens;
@@ -67,267 +69,96 @@ struct SpParams {
   uint32_t *status;
   float *part_o;   // unnormalised outputs, [D / 4][rows] float4 per piece and row tile
   float2 *part_ml; // maximum (base-2 units) and sum of every row of a partial
+  uint4 *plan;     // [num_groups + B] for the merge kernel: cost base, partial rows
+                   // before, keys (0 without rows), and a sequence's group or a group's first sequence
+  uint32_t *total; // length of the axis
   int B, n_q, H_q, H_kv, group, num_pages, num_groups, max_prefix_pages, max_pages;
-  int tokens_per_tile;  // floor(128 / group)
+  int tokens_per_tile;  // floor(128 / group), at least 16
+  uint32_t tile_magic;
   int oob_row;          // a tensor-map row beyond the pool: loads as zeros
   int G;                // CTAs of the split kernel
   float scale_log2;
 };
 
-// The segments, in shared memory of every CTA of both kernels.  Entities are the
-// groups' prefixes, then the sequences' own tokens.
-struct SpPlan {
-  uint32_t *cost;  // [E + 1] cost of the entities before
-  uint32_t *slot;  // [E + 1] partial rows of the entities before
-  int *len;        // [E] keys
-  int *start;      // [num_groups + 1] first sequence of each group
-  uint32_t Tot, q, r;
-  int G;
-  // CTA c's range of the axis begins at start(c); c * r < G^2
-  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * q + c * r / static_cast<uint32_t>(G); }
-  __device__ __forceinline__ int owner(uint32_t x) const {
-    int c = static_cast<int>((static_cast<float>(x) + 0.5f) * (static_cast<float>(G) / static_cast<float>(Tot)));
-    c = c < 0 ? 0 : (c >= G ? G - 1 : c);
-    while (c > 0 && begin(c) > x) --c;
-    while (c + 1 < G && begin(c + 1) <= x) ++c;
-    return c;
-  }
-};
-
-__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) {
-  return 4 * (3 * (B + num_groups) + 2 + num_groups + 1);
-}
-
-// One entity: `tokens` query tokens from token0 on (rows of all its sequences)
-// against `keys` keys.
+// The segments: entity e < num_groups is a group's prefix, entity num_groups + b
+// sequence b's own tokens.  `tokens` query tokens from token0 on, in `tiles` row
+// tiles, against `keys` keys.
 struct SpEntity {
-  int keys, tokens, token0, tiles, pairs, key_tiles;
+  int keys, token0, tokens, tiles, pairs, key_tiles;
   uint32_t head_cost;  // per KV head
   uint32_t slot_rows;  // partial rows of one piece
+  __device__ __forceinline__ uint32_t pair_cost() const { return kSpCostSeg + 2u * static_cast<uint32_t>(key_tiles); }
 };
 
-__device__ __forceinline__ SpEntity sp_entity(const SpParams &p, const SpPlan &pl, int e) {
+// n / tokens_per_tile for n < 2^25 (tile_magic = ceil(2^32 / tokens_per_tile))
+__device__ __forceinline__ int sp_tiles(const SpParams &p, int n) {
+  return static_cast<int>(__umulhi(static_cast<uint32_t>(n), p.tile_magic));
+}
+
+__device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int first, int sequences, int keys) {
   SpEntity x;
-  x.keys = pl.len[e];
-  if (e < p.num_groups) {
-    x.token0 = pl.start[e] * p.n_q;
-    x.tokens = (pl.start[e + 1] - pl.start[e]) * p.n_q;
-  } else {
-    x.token0 = (e - p.num_groups) * p.n_q;
-    x.tokens = p.n_q;
-  }
-  x.tiles = (x.tokens + p.tokens_per_tile - 1) / p.tokens_per_tile;
+  x.keys = keys;
+  x.token0 = first * p.n_q;
+  x.tokens = sequences * p.n_q;
+  x.tiles = own ? 1 : sp_tiles(p, x.tokens + p.tokens_per_tile - 1);
   x.pairs = (x.tiles + 1) >> 1;
-  x.key_tiles = (x.keys + kSpTile - 1) / kSpTile;
-  x.head_cost = x.keys > 0 ? static_cast<uint32_t>(x.pairs) * kSpCostSeg +
-                                 static_cast<uint32_t>(x.key_tiles) * static_cast<uint32_t>(x.tiles) * kSpCostTile
-                           : 0u;
+  x.key_tiles = (keys + kSpTile - 1) / kSpTile;
+  x.head_cost = keys > 0 ? static_cast<uint32_t>(x.pairs) * kSpCostSeg +
+                               static_cast<uint32_t>(x.key_tiles) * static_cast<uint32_t>(x.tiles)
+                         : 0u;
   x.slot_rows = x.tiles > 1 ? 2u * kSpTile : 2u * static_cast<uint32_t>(x.tokens * p.group);
   return x;
 }
 
-// Lengths and prefix sums over the entities; every thread of the block calls it.
-template <int NT>
-__device__ SpPlan sp_plan(const SpParams &p, int *mem, uint32_t (*s_warp)[2]) {
-  const int E = p.num_groups + p.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  SpPlan pl;
-  pl.cost = reinterpret_cast<uint32_t *>(mem);
-  pl.slot = pl.cost + E + 1;
-  pl.len = reinterpret_cast<int *>(pl.slot + E + 1);
-  pl.start = pl.len + E;
-  int bad = 0;
-  for (int g = tid; g <= p.num_groups; g += NT) {
-    const int s = p.group_starts[g];
-    pl.start[g] = s;
-    bad |= g == 0 ? s != 0 : s < p.group_starts[g - 1];
-    bad |= g == p.num_groups && s != p.B;
-  }
-  for (int e = tid; e < E; e += NT) {
-    const bool own = e >= p.num_groups;
-    int n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
-    const int least = own ? p.n_q : 0, most = (own ? p.max_pages : p.max_prefix_pages) * SF_PAGE_SIZE;
-    if ((n < least || n > most) && n != 0) {
-      set_status(p.status, SF_DEVICE_BAD_SEQLEN);
-      n = n < least ? least : most;
-    }
-    pl.len[e] = n;
-  }
-  bad = __syncthreads_or(bad);
-  if (bad) {  // malformed groups: no sequence has a prefix
-    for (int g = tid; g <= p.num_groups; g += NT) pl.start[g] = 0;
-    if (tid == 0) set_status(p.status, SF_DEVICE_BAD_INDEX);
-    __syncthreads();
-  }
-  const int per = (E + NT - 1) / NT, e0 = tid * per;
-  uint32_t c = 0, s = 0;
-  for (int e = e0; e < e0 + per && e < E; ++e) {
-    const SpEntity x = sp_entity(p, pl, e);
-    c += x.head_cost * p.H_kv;
-    if (x.head_cost) s += x.slot_rows * x.pairs * p.H_kv;
-  }
-  uint32_t ci = c, si = s;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t a = __shfl_up_sync(0xffffffffu, ci, o), b = __shfl_up_sync(0xffffffffu, si, o);
-    if (lane >= o) {
-      ci += a;
-      si += b;
-    }
-  }
-  if (lane == 31) {
-    s_warp[warp][0] = ci;
-    s_warp[warp][1] = si;
-  }
-  __syncthreads();
-  uint32_t co = ci - c, so = si - s;
-  pl.Tot = 0;
-  for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) {
-      co += s_warp[w][0];
-      so += s_warp[w][1];
-    }
-    pl.Tot += s_warp[w][0];
-  }
-  for (int e = e0; e < e0 + per && e < E; ++e) {
-    const SpEntity x = sp_entity(p, pl, e);
-    pl.cost[e] = co;
-    pl.slot[e] = so;
-    co += x.head_cost * p.H_kv;
-    if (x.head_cost) so += x.slot_rows * x.pairs * p.H_kv;
-  }
-  if (tid == 0) pl.cost[E] = pl.Tot;
-  pl.G = pl.Tot < static_cast<uint32_t>(p.G) ? static_cast<int>(pl.Tot) : p.G;
-  pl.q = pl.G ? pl.Tot / pl.G : 0;
-  pl.r = pl.G ? pl.Tot % pl.G : 0;
-  __syncthreads();
-  return pl;
-}
+// The axis of length Tot in ranges of `chunk`, one per CTA (the last ones shorter
+// or empty: the longest is what counts).
+struct SpCut {
+  uint32_t Tot, chunk;
+  __device__ __forceinline__ SpCut(uint32_t tot, int G) : Tot(tot), chunk((tot + G - 1) / G) {}
+  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * chunk < Tot ? c * chunk : Tot; }
+  __device__ __forceinline__ int owner(uint32_t x) const { return static_cast<int>(x / chunk); }
+};
 
-// First key tile of a segment (cost base `base`, `unit` per key tile) at or
+// First key tile of a segment (cost base `base`; 1 << dual per key tile) at or
 // behind position x of the axis.
-__device__ __forceinline__ int sp_tile_at(uint32_t x, uint32_t base, uint32_t unit, int key_tiles) {
+__device__ __forceinline__ int sp_tile_at(uint32_t x, uint32_t base, int dual, int key_tiles) {
   const uint32_t b = base + kSpCostSeg;
   if (x <= b) return 0;
-  const uint32_t t = (x - b + unit - 1) / unit;
+  const uint32_t t = (x - b + dual) >> dual;
   return t < static_cast<uint32_t>(key_tiles) ? static_cast<int>(t) : key_tiles;
 }
-
-// The pieces of one CTA, in order.
-struct SpPiece {
-  int e, h, pair, dual;   // dual: two row tiles, one per stream
-  int t0, n;              // key tiles
-  uint32_t slot;          // its first partial row
-};
-
-struct SpWalk {
-  uint32_t at, end;       // the CTA's range
-  uint32_t base;          // cost base of the current segment
-  uint32_t slot;          // partial rows before the current segment
-  int e, h, pair;
-  SpEntity x;
-
-  __device__ __forceinline__ void init(const SpParams &p, const SpPlan &pl, int c) {
-    const int E = p.num_groups + p.B;
-    e = E;
-    at = end = 0;
-    if (c >= pl.G) return;
-    at = pl.begin(c);
-    end = pl.begin(c + 1);
-    int lo = 0, hi = E - 1;  // last entity whose cost base is <= at
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (pl.cost[mid] <= at) lo = mid; else hi = mid - 1;
-    }
-    e = lo;
-    x = sp_entity(p, pl, e);
-    const uint32_t in = at - pl.cost[e], pair_cost = kSpCostSeg + 2u * x.key_tiles * kSpCostTile;
-    h = static_cast<int>(in / x.head_cost);
-    pair = static_cast<int>((in - h * x.head_cost) / pair_cost);
-    base = pl.cost[e] + h * x.head_cost + pair * pair_cost;
-    slot = pl.slot[e] + (h * x.pairs + pair) * x.slot_rows;
-  }
-
-  // The next piece with keys; false behind the last.
-  __device__ __forceinline__ bool next(const SpParams &p, const SpPlan &pl, int c, SpPiece &pc) {
-    const int E = p.num_groups + p.B;
-    while (e < E && base < end) {
-      const int dual = 2 * pair + 1 < x.tiles;
-      const uint32_t unit = (1u + dual) * kSpCostTile;
-      const int t0 = sp_tile_at(at, base, unit, x.key_tiles), t1 = sp_tile_at(end, base, unit, x.key_tiles);
-      pc.e = e;
-      pc.h = h;
-      pc.pair = pair;
-      pc.dual = dual;
-      pc.t0 = t0;
-      pc.n = t1 - t0;
-      pc.slot = slot + 2u * kSpTile * c;
-      // the next segment
-      base += kSpCostSeg + unit * x.key_tiles;
-      slot += x.slot_rows;
-      if (++pair == x.pairs) {
-        pair = 0;
-        if (++h == p.H_kv) {
-          h = 0;
-          do ++e;
-          while (e < E && pl.cost[e + 1] == pl.cost[e]);  // entities without keys or rows
-          if (e < E) {
-            x = sp_entity(p, pl, e);
-            slot = pl.slot[e];
-          }
-        }
-      }
-      if (pc.n > 0) return true;
-    }
-    return false;
-  }
-};
-
-// What stream s does of a piece: its row tile and key tiles t0 + first, + step, ..
-struct SpJob {
-  int tile;         // row tile of the entity
-  int first, step;  // key tiles within the piece
-  int n;            // number of them (0: nothing for this stream)
-  uint32_t slot;    // first partial row
-};
 
 __device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int tile) {
   const int left = x.tokens - tile * p.tokens_per_tile;
   return (left < p.tokens_per_tile ? left : p.tokens_per_tile) * p.group;
 }
 
-// `turn`: the stream of the next piece of one row tile and one key tile.
-__device__ __forceinline__ SpJob sp_job(const SpPiece &pc, int s, int rows0, int &turn) {
-  SpJob j;
-  j.tile = 2 * pc.pair + (pc.dual ? s : 0);
-  if (pc.dual) {
-    j.first = 0;
-    j.step = 1;
-    j.n = pc.n;
-    j.slot = pc.slot + s * kSpTile;
-  } else if (pc.n > 1) {
-    j.first = s;
-    j.step = 2;
-    j.n = (pc.n + 1 - s) >> 1;
-    j.slot = pc.slot + s * rows0;
-  } else {
-    j.first = 0;
-    j.step = 1;
-    j.n = turn == s;
-    j.slot = pc.slot;
-    turn ^= 1;
-  }
-  return j;
-}
+// A piece, as its CTA's warps read it from shared memory.
+struct SpItem {
+  int n, t0, keys;  // key tiles t0 .. t0 + n - 1 of the segment's keys; n = 0: no more pieces
+  int own, row, h;  // row of block_table (own) or prefix_table
+  int dual, again;  // both streams read every tile; the keys are read again by other pieces
+  struct {
+    int n, first, step;    // the stream's key tiles within the piece (n = 0: none)
+    int token, rows;       // first query token and rows of its row tile
+    uint32_t slot;         // first row of its partial
+  } s[2];
+};
+
+// Bytes of shared memory behind the barriers for the lengths of all entities.
+__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) { return 4 * (B + 2 * num_groups + 1); }
 
 template <int D, int STAGES>
 struct SpSmem {
   static constexpr int kTileBytes = kSpTile * D * 2;  // a K, V or Q tile
   static constexpr int kQOffset = STAGES * kTileBytes;
   static constexpr int kBarOffset = kQOffset + 2 * kTileBytes;
-  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full[2], o_done, fin, turn
-  static constexpr int kNumBars = 2 * STAGES + 16;
-  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word, scan scratch
-  static constexpr int kPlanOffset = kMiscOffset + 16 + 8 * (kSpThreads / 32);
+  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full[2], o_done, fin, turn;
+  // item_full, item_empty per published piece
+  static constexpr int kNumBars = 2 * STAGES + 16 + 2 * kSpItems;
+  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word
+  static constexpr int kItemOffset = kMiscOffset + 16;
+  static constexpr int kPlanOffset = kItemOffset + kSpItems * static_cast<int>(sizeof(SpItem));
 };
 
 // max of three in one instruction (a NaN is ignored, as by fmaxf)
@@ -372,7 +203,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   constexpr uint32_t kIdescQK = idesc_bf16_f32(128, kSpTile, 0, 0);
   constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, 0, 1);
   constexpr int FULL = 0, EMPTY = STAGES, QFULL = 2 * STAGES, QEMPTY = QFULL + 2, SFULL = QEMPTY + 2,
-                PFULL = SFULL + 2, ODONE = PFULL + 4, FIN = ODONE + 2, TURN = FIN + 2;
+                PFULL = SFULL + 2, ODONE = PFULL + 4, FIN = ODONE + 2, TURN = FIN + 2,
+                IFULL = TURN + 2, IEMPTY = IFULL + kSpItems;
 
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t ring = smem_addr(smem);
@@ -384,7 +216,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(bar(FULL + s), 1);
-      mbar_init(bar(EMPTY + s), 2);  // one arrival per stream that reads the tile, or two
+      mbar_init(bar(EMPTY + s), 2);  // one arrival per stream
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar(QFULL + s), 1);
@@ -396,6 +228,10 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       mbar_init(bar(FIN + s), 1);
       mbar_init(bar(TURN + s), 1);
     }
+    for (int i = 0; i < kSpItems; ++i) {
+      mbar_init(bar(IFULL + i), 1);
+      mbar_init(bar(IEMPTY + i), kSpThreads / 32 - 1);  // every warp but the publishing one
+    }
     fence_mbar_init();
     prefetch_tensormap(&tmap_k);
     prefetch_tensormap(&tmap_v);
@@ -404,58 +240,212 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     s_misc[1] = 0;
   }
   grid_dependency_wait();
-  // (behind the wait: the merge kernel reads the lengths as soon as it starts)
   grid_launch_dependents();
-  const SpPlan pl = sp_plan<kSpThreads>(p, reinterpret_cast<int *>(smem + L::kPlanOffset),
-                                        reinterpret_cast<uint32_t(*)[2]>(s_misc + 4));
   if (warp == kSpMmaWarp) {
     tmem_alloc(smem_addr(s_misc), kSpTmemCols);
     tmem_relinquish_alloc_permit();
     tc_fence_before_sync();
   }
+  // lengths of all entities, and the groups' first sequences
+  const int E = p.num_groups + p.B;
+  int *s_len = reinterpret_cast<int *>(smem + L::kPlanOffset), *s_start = s_len + E;
+  for (int e = tid; e < E; e += kSpThreads) {
+    const bool own = e >= p.num_groups;
+    int n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
+    if (!own) s_start[e] = p.group_starts[e];
+    const int least = own ? p.n_q : 0, most = (own ? p.max_pages : p.max_prefix_pages) * SF_PAGE_SIZE;
+    if ((n < least || n > most) && n != 0) {
+      set_status(p.status, SF_DEVICE_BAD_SEQLEN);
+      n = n < least ? least : most;
+    }
+    s_len[e] = n;
+  }
+  if (tid == 0) s_start[p.num_groups] = p.group_starts[p.num_groups];
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = static_cast<uint32_t>(s_misc[0]);
-  const int c = static_cast<int>(blockIdx.x);
-
-  SpWalk walk;
-  walk.init(p, pl, c);
-  SpPiece pc;
+  SpItem *items = reinterpret_cast<SpItem *>(smem + L::kItemOffset);
+  uint32_t seen = 0;  // pieces read
+  // The next piece; null behind the last one (or after a timeout).  The warp
+  // gives the entry back with release_item.
+  auto next_item = [&]() -> const SpItem * {
+    const uint32_t i = seen % kSpItems;
+    const bool w = mbar_wait_or_abort(bar(IFULL + i), (seen / kSpItems) & 1u, s_abort);
+    ++seen;
+    return __all_sync(0xffffffffu, w) && items[i].n > 0 ? items + i : nullptr;
+  };
+  auto release_item = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(IEMPTY + (seen - 1) % kSpItems));
+  };
 
   if (warp == kSpQueryWarp) {
     // ------------------------------------------------------------------
-    // Q tiles, one per job, as soon as the stream's last Q K^T has read its Q
+    // The CTA's pieces, published one after the other, each followed by the
+    // copies of its Q tiles as soon as the streams' last Q K^T have read theirs.
     // ------------------------------------------------------------------
+    bool bad = false;
+    for (int g = lane; g <= p.num_groups; g += 32)
+      bad |= g == 0 ? s_start[0] != 0 : s_start[g] < s_start[g - 1] || (g == p.num_groups && s_start[g] != p.B);
+    if (__any_sync(0xffffffffu, bad)) {  // malformed groups: no sequence has a prefix
+      for (int g = lane; g <= p.num_groups; g += 32) s_start[g] = 0;
+      if (lane == 0) set_status(p.status, SF_DEVICE_BAD_INDEX);
+      __syncwarp();
+    }
+    auto entity = [&](int e) -> SpEntity {
+      const bool own = e >= p.num_groups;
+      const int first = own ? e - p.num_groups : s_start[e];
+      return sp_entity(p, own, first, own ? 1 : s_start[e + 1] - first, s_len[e]);
+    };
+    uint32_t sum = 0;
+    for (int e = lane; e < E; e += 32) sum += entity(e).head_cost;
+    const SpCut cut(__reduce_add_sync(0xffffffffu, sum) * p.H_kv, p.G);
+    const uint32_t c = blockIdx.x;
+    const bool writes = c == gridDim.x - 1;  // this CTA leaves the plan for the merge kernel
+    const uint32_t at = cut.begin(c), end = cut.begin(c + 1);
+    // the entity that position `at` lies in, with the costs and partial rows before it
+    int e = E;
+    uint32_t e_cost = 0, e_slot = 0, cost = 0, slot = 0;
+    for (int e0 = 0; e0 < E && (e == E || writes); e0 += 32) {
+      const int k = e0 + lane;
+      SpEntity x{};
+      if (k < E) x = entity(k);
+      uint32_t ci = x.head_cost * p.H_kv, si = x.head_cost ? x.slot_rows * x.pairs * p.H_kv : 0u;
+      const uint32_t mine = ci, rows = si;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, ci, o), v = __shfl_up_sync(0xffffffffu, si, o);
+        if (lane >= o) {
+          ci += u;
+          si += v;
+        }
+      }
+      const uint32_t before = cost + ci - mine, slots = slot + si - rows;
+      const unsigned in = __ballot_sync(0xffffffffu, mine > 0 && before <= at && at < before + mine);
+      if (in) {
+        const int l = __ffs(in) - 1;
+        e = e0 + l;
+        e_cost = __shfl_sync(0xffffffffu, before, l);
+        e_slot = __shfl_sync(0xffffffffu, slots, l);
+      }
+      if (writes && k < E) {
+        int other;
+        if (k < p.num_groups) {
+          other = s_start[k];
+        } else {
+          int lo = 0, hi = p.num_groups;  // the sequence's group: the last that starts at or before it
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_start[mid] <= k - p.num_groups) lo = mid + 1; else hi = mid;
+          }
+          other = lo - 1;
+        }
+        p.plan[k] = make_uint4(before, slots, x.head_cost ? static_cast<uint32_t>(x.keys) : 0u,
+                               static_cast<uint32_t>(other));
+      }
+      cost += __shfl_sync(0xffffffffu, ci, 31);
+      slot += __shfl_sync(0xffffffffu, si, 31);
+    }
+    if (writes && lane == 0) *p.total = cut.Tot;
+    SpEntity x{};
+    int h = 0, pair = 0;
+    uint32_t base = 0;
+    slot = 0;
+    if (e < E) {
+      x = entity(e);
+      const uint32_t in = at - e_cost;
+      h = static_cast<int>(in / x.head_cost);
+      pair = x.pairs > 1 ? static_cast<int>((in - h * x.head_cost) / x.pair_cost()) : 0;
+      base = e_cost + h * x.head_cost + pair * x.pair_cost();
+      slot = e_slot + (h * x.pairs + pair) * x.slot_rows + 2u * kSpTile * c;
+    }
     const uint64_t again = l2_policy_evict_last();
-    uint32_t jobs[2] = {0, 0};
+    uint32_t published = 0, jobs[2] = {0, 0};
     int turn = 0;
-    bool ok = true;
-    while (ok && walk.next(p, pl, c, pc)) {
-      const bool own = pc.e >= p.num_groups;
-      const SpEntity x = sp_entity(p, pl, pc.e);
-      const int turn0 = turn;
+    bool ok = true, more = true;
+    auto wait = [&](uint32_t b, uint32_t parity) -> bool {
+      int w = 1;
+      if (lane == 0) w = mbar_wait_or_abort(b, parity, s_abort);
+      return __shfl_sync(0xffffffffu, w, 0) != 0;
+    };
+    while (ok && more) {
+      SpItem it;
+      it.n = 0;
+      while (it.n == 0 && e < E && base < end) {
+        const int dual = 2 * pair + 1 < x.tiles;
+        it.t0 = sp_tile_at(at, base, dual, x.key_tiles);
+        it.n = sp_tile_at(end, base, dual, x.key_tiles) - it.t0;
+        if (it.n > 0) {
+          const bool own = e >= p.num_groups;
+          it.keys = x.keys;
+          it.own = own;
+          it.row = own ? e - p.num_groups : e;
+          it.h = h;
+          it.dual = dual;
+          it.again = x.pairs > 1;
+          const int rows0 = sp_rows(p, x, 2 * pair), tok0 = x.token0 + 2 * pair * p.tokens_per_tile;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            auto &j = it.s[s];
+            j.token = tok0;
+            j.rows = rows0;
+            j.slot = slot;
+            j.first = 0;
+            j.step = 1;
+            j.n = it.n;
+            if (dual) {  // a row tile each
+              if (s == 1) {
+                j.token += p.tokens_per_tile;
+                j.rows = sp_rows(p, x, 2 * pair + 1);
+                j.slot += kSpTile;
+              }
+            } else if (it.n > 1) {  // even and odd key tiles
+              j.first = s;
+              j.step = 2;
+              j.n = (it.n + 1 - s) >> 1;
+              j.slot += s * rows0;
+            } else {  // one key tile: the streams in turn
+              j.n = turn == s;
+            }
+          }
+          if (!dual && it.n == 1) turn ^= 1;
+        }
+        // the next segment
+        base += kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual);
+        slot += x.slot_rows;
+        if (++pair == x.pairs) {
+          pair = 0;
+          if (++h == p.H_kv) {
+            h = 0;
+            do x = ++e < E ? entity(e) : x;
+            while (e < E && x.head_cost == 0);  // entities without keys or rows
+          }
+        }
+      }
+      more = it.n > 0;
+      const uint32_t i = published % kSpItems;
+      if (published >= kSpItems && !(ok = wait(bar(IEMPTY + i), (published / kSpItems - 1) & 1u))) break;
+      if (lane == 0) {
+        items[i] = it;
+        mbar_arrive(bar(IFULL + i));
+      }
+      ++published;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        int tn = turn0;
-        const SpJob j = sp_job(pc, s, 0, tn);
-        turn = tn;
-        if (j.n == 0 || !ok) continue;
-        int w = 1;
-        if (lane == 0 && jobs[s] > 0) w = mbar_wait_or_abort(bar(QEMPTY + s), (jobs[s] - 1) & 1u, s_abort);
-        if (!(ok = __shfl_sync(0xffffffffu, w, 0) != 0)) continue;
+        if (!more || !ok || it.s[s].n == 0) continue;
+        if (jobs[s] > 0 && !(ok = wait(bar(QEMPTY + s), (jobs[s] - 1) & 1u))) continue;
         if (lane == 0) {
-          const int tokens = own ? p.n_q : p.tokens_per_tile;
-          mbar_arrive_expect_tx(bar(QFULL + s), static_cast<uint32_t>(tokens * p.group * D * 2));
-          const int token = x.token0 + j.tile * p.tokens_per_tile;
+          mbar_arrive_expect_tx(bar(QFULL + s),
+                                static_cast<uint32_t>((it.own ? p.n_q : p.tokens_per_tile) * p.group * D * 2));
           for (int hf = 0; hf < HALVES; ++hf)
-            tma_load_4d(ring + L::kQOffset + s * L::kTileBytes + hf * kHalfTileBytes, own ? &tmap_q_own : &tmap_q_tile,
-                        64 * hf, 0, pc.h, token, bar(QFULL + s), again);
+            tma_load_4d(ring + L::kQOffset + s * L::kTileBytes + hf * kHalfTileBytes, it.own ? &tmap_q_own : &tmap_q_tile,
+                        64 * hf, 0, it.h, it.s[s].token, bar(QFULL + s), again);
         }
         __syncwarp();
         ++jobs[s];
       }
     }
-    if (!ok && lane == 0) {  // stopped: the copies in flight land (bounded) before shared memory is left
+    if (*s_abort && lane == 0) {  // stopped: the copies in flight land (bounded) before shared memory is left
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         if (jobs[s]) (void)mbar_wait_bounded(bar(QFULL + s), (jobs[s] - 1) & 1u);
@@ -474,18 +464,19 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       if (lane == 0) w = mbar_wait_or_abort(b, parity, s_abort);
       return __shfl_sync(0xffffffffu, w, 0) != 0;
     };
-    while (ok && walk.next(p, pl, c, pc)) {
-      const bool own = pc.e >= p.num_groups;
-      const SpEntity x = sp_entity(p, pl, pc.e);
-      const int32_t *table = own ? p.block_table + static_cast<size_t>(pc.e - p.num_groups) * p.max_pages
-                                 : p.prefix_table + static_cast<size_t>(pc.e) * p.max_prefix_pages;
-      // (a prefix with more than one pair of row tiles is read again)
-      const uint64_t policy = !own && x.pairs > 1 ? again : once;
+    while (ok) {
+      const SpItem *item = next_item();
+      if (!item) break;
+      const int n = item->n, t0 = item->t0, keys = item->keys, h = item->h;
+      const int32_t *table = item->own ? p.block_table + static_cast<size_t>(item->row) * p.max_pages
+                                       : p.prefix_table + static_cast<size_t>(item->row) * p.max_prefix_pages;
+      const uint64_t policy = item->again ? again : once;
+      release_item();
       int ids = kBeyondEnd;
-      for (int it = 0; it < pc.n && ok; ++it) {
+      for (int it = 0; it < n && ok; ++it) {
         if ((it & 3) == 0) {  // page ids of the next four tiles, one a lane
-          const int lt = it + (lane >> 3), page = (pc.t0 + lt) * kSpTilePages + (lane & 7);
-          ids = lt < pc.n && page * SF_PAGE_SIZE < x.keys ? table[page] : kBeyondEnd;
+          const int lt = it + (lane >> 3), page = (t0 + lt) * kSpTilePages + (lane & 7);
+          ids = lt < n && page * SF_PAGE_SIZE < keys ? table[page] : kBeyondEnd;
         }
         const int phys = __shfl_sync(0xffffffffu, ids, ((it & 3) << 3) + (lane & 7));
         int row = p.oob_row;  // pages past the end or outside the pool load as zeros
@@ -493,7 +484,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           if (phys < 0 || phys >= p.num_pages) {
             if (lane < kSpTilePages) set_status(p.status, SF_DEVICE_BAD_PAGE);
           } else {
-            row = (phys * p.H_kv + pc.h) * SF_PAGE_SIZE;
+            row = (phys * p.H_kv + h) * SF_PAGE_SIZE;
           }
         }
         for (int kv = 0; kv < 2 && ok; ++kv, ++pos) {
@@ -516,7 +507,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         }
       }
     }
-    if (!ok && lane == 0) {
+    if (*s_abort && lane == 0) {
       for (uint32_t x = pos > STAGES ? pos - STAGES : 0; x < pos; ++x)
         (void)mbar_wait_bounded(bar(FULL + x % STAGES), (x / STAGES) & 1u);
     }
@@ -539,8 +530,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const bool w = mbar_wait_or_abort(b, parity, s_abort);
       return __all_sync(0xffffffffu, w);
     };
-    uint32_t base = 0, tiles = 0, jobs = 0, turns = 0;
-    int turn = 0;
+    uint32_t pos = 0, tiles = 0, jobs = 0, turns = 0;  // pos: ring slots passed
     bool ok = true;
     // stream 1's i-th turn follows stream 0's, stream 0's next follows that
     auto take_turn = [&]() -> bool {
@@ -548,21 +538,37 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       ++turns;
       return w;
     };
-    while (ok && walk.next(p, pl, c, pc)) {
-      const SpJob j = sp_job(pc, s, 0, turn);
-      uint32_t tile = __shfl_sync(0xffffffffu, base + j.first, 0);
-      base += pc.n;
-      const int n = __shfl_sync(0xffffffffu, j.n, 0), step = __shfl_sync(0xffffffffu, j.step, 0);
-      if (n == 0) continue;
-      const bool dual = __shfl_sync(0xffffffffu, pc.dual, 0) != 0;
-      bool two = __shfl_sync(0xffffffffu, pc.t0 + j.first, 0) == 0;  // the segment's first key tile: P_hi + P_lo
-      if (!(ok = wait(bar(QFULL + s), jobs & 1u))) break;
-      ++jobs;
-      for (int k = 0; k < n; ++k, tile += step, ++tiles) {
-        const bool last = k + 1 == n;
-        uint32_t pos = 2u * tile, slot = pos % STAGES;
+    while (ok) {
+      const SpItem *item = next_item();
+      if (!item) break;
+      const int total = __shfl_sync(0xffffffffu, item->n, 0), n = __shfl_sync(0xffffffffu, item->s[s].n, 0);
+      const int step = __shfl_sync(0xffffffffu, item->s[s].step, 0);
+      const bool dual = __shfl_sync(0xffffffffu, item->dual, 0) != 0;
+      int mine = n > 0 ? __shfl_sync(0xffffffffu, item->s[s].first, 0) : total;  // the stream's next key tile
+      bool two = __shfl_sync(0xffffffffu, item->t0 + mine, 0) == 0;  // the segment's first key tile: P_hi + P_lo
+      int left = n;
+      release_item();
+      for (int t = 0; t < total; ++t, pos += 2) {
+        uint32_t slot = pos % STAGES;
         if (!(ok = wait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
-        if (k == 0 && dual && !(ok = take_turn())) break;
+        if (t != mine) {
+          // The other stream's tile: this stream gives its slots back too.  Both
+          // streams pass every tile, so neither is ever two rounds of the ring
+          // from the copies, where the parity of a slot's barrier says nothing.
+          const uint32_t slot_v = (pos + 1) % STAGES;
+          if (lane == 0) mbar_arrive(bar(EMPTY + slot));
+          if (!(ok = wait(bar(FULL + slot_v), ((pos + 1) / STAGES) & 1u))) break;
+          if (lane == 0) mbar_arrive(bar(EMPTY + slot_v));
+          continue;
+        }
+        const bool first = left == n, last = left == 1;
+        mine += step;
+        --left;
+        if (first) {
+          if (!(ok = wait(bar(QFULL + s), jobs & 1u))) break;
+          ++jobs;
+          if (dual && !(ok = take_turn())) break;
+        }
         tc_fence_after_sync();
         const uint64_t k0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
         if (elect_one()) {
@@ -572,14 +578,12 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                       k0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), kIdescQK, kk > 0 ? 1u : 0u);
           tc_commit(bar(SFULL + s));
           tc_commit(bar(EMPTY + slot));
-          if (!dual) mbar_arrive(bar(EMPTY + slot));
           if (last) tc_commit(bar(QEMPTY + s));
           if (dual) mbar_arrive(bar(TURN + 1 - s));
         }
         __syncwarp();
-        ++pos;
-        slot = pos % STAGES;
-        if (!(ok = wait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
+        slot = (pos + 1) % STAGES;
+        if (!(ok = wait(bar(FULL + slot), ((pos + 1) / STAGES) & 1u))) break;
         const uint64_t v0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -590,12 +594,11 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll
             for (int j = 0; j < kSpTilePages; ++j) {
               if (j / (kSpTilePages / 2) != half) continue;
-              tc_mma_ts(to, ts + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, k > 0 || j > 0 ? 1u : 0u);
+              tc_mma_ts(to, ts + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, !first || j > 0 ? 1u : 0u);
               if (two) tc_mma_ts(to, ts + 64 + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, 1u);
             }
             if (half == 1) {
               tc_commit(bar(EMPTY + slot));
-              if (!dual) mbar_arrive(bar(EMPTY + slot));
               if (last) tc_commit(bar(ODONE + s));
               if (last && dual) mbar_arrive(bar(TURN + 1 - s));
             }
@@ -604,6 +607,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         }
         if (!ok) break;
         two = false;
+        ++tiles;
       }
     }
     // every MMA issued has completed once this arrives
@@ -622,23 +626,23 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       return __all_sync(0xffffffffu, w);
     };
     uint32_t base = 0, tiles = 0, jobs = 0;
-    int turn = 0;
     bool ok = true;
-    while (ok && walk.next(p, pl, c, pc)) {
-      const bool own = pc.e >= p.num_groups;
-      const SpEntity x = sp_entity(p, pl, pc.e);
-      const SpJob job = sp_job(pc, s, sp_rows(p, x, 2 * pc.pair), turn);
-      const uint32_t piece_base = base;
-      base += pc.n;
-      if (job.n == 0) continue;
-      const int rows = sp_rows(p, x, job.tile);
+    while (ok) {
+      const SpItem *item = next_item();
+      if (!item) break;
+      const int n = item->s[s].n, step = item->s[s].step, rows = item->s[s].rows, keys = item->keys;
+      const uint32_t slot0 = item->s[s].slot;
+      uint32_t ring_tile = base + item->s[s].first;
+      int tile_pos = (item->t0 + item->s[s].first) * kSpTile;  // position of the tile's first key
+      base += item->n;
       const bool valid = r < rows;
       // last visible key of this row (rows past the tile's end see every key:
       // their scores are not used)
-      int lim = 0x7fffff00;
-      if (valid) lim = own ? x.keys - p.n_q + r / p.group : x.keys - 1;
+      const int lim = !valid ? 0x7fffff00 : item->own ? keys - p.n_q + r / p.group : keys - 1;
+      release_item();
+      if (n == 0) continue;
       float ref = -INFINITY, l_run = 0.f;
-      for (int k = 0; k < job.n; ++k, ++tiles) {
+      for (int k = 0; k < n; ++k, ++tiles, ring_tile += step, tile_pos += step * kSpTile) {
         if (!(ok = wwait(bar(SFULL + s), tiles & 1u))) break;
         tc_fence_after_sync();
         uint32_t sv[128];
@@ -649,14 +653,12 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll
           for (int i = 0; i < 64; ++i) sv[64 * q + i] = part[i];
         }
-        const int in_piece = job.first + k * job.step;
-        const int tile_pos = (pc.t0 + in_piece) * kSpTile;
-        const int valid_keys = x.keys - tile_pos;
+        const int valid_keys = keys - tile_pos;
         if (valid_keys < kSpTile && (valid_keys & (SF_PAGE_SIZE - 1)) != 0) {
           // V rows of the last page past the end hold whatever the page holds:
           // zeros there, so that 0 * v stays 0 (whole pages past the end are
           // zeros already)
-          const uint32_t pos = 2u * (piece_base + in_piece) + 1u, slot = pos % STAGES;
+          const uint32_t pos = 2u * ring_tile + 1u, slot = pos % STAGES;
           if (!(ok = wwait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
           uint8_t *vt = smem + slot * L::kTileBytes + (valid_keys / SF_PAGE_SIZE) * kPageBytes;
           const int tok0 = valid_keys & (SF_PAGE_SIZE - 1);
@@ -775,7 +777,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       if (!ok) break;
       ++jobs;
       tc_fence_after_sync();
-      float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(job.slot) * D) + r;
+      float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
 #pragma unroll 1
       for (int ch = 0; ch < D / 32; ++ch) {
         uint32_t ov[32];
@@ -788,7 +790,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                             __uint_as_float(ov[4 * q4 + 2]), __uint_as_float(ov[4 * q4 + 3]));
         }
       }
-      if (valid) p.part_ml[job.slot + r] = make_float2(ref, l_run);
+      if (valid) p.part_ml[slot0 + r] = make_float2(ref, l_run);
       tc_fence_before_sync();
     }
     tc_fence_before_sync();
@@ -806,91 +808,136 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 // The partials of every row, joined in piece order (deterministic):
 //   M = max_q m_q,  L = sum_q l_q 2^(m_q - M),  O = sum_q 2^(m_q - M) O_q / L,
 //   lse = (M + log2 L) ln 2.
-// One item per output quad (row, 4 columns); consecutive threads take
-// consecutive rows of one quad, as the partials lie.
+// A block takes one sequence and KV head (or a part of its rows): two warps list
+// where the partials of its rows lie -- the prefix's for the one or two row tiles
+// its tokens are in, then the own segment's -- and its threads walk the lists,
+// kSpJoinBatch partials in flight.  One item per output quad (row, 4 columns);
+// consecutive threads take consecutive rows of one quad, as the partials lie.
 // --------------------------------------------------------------------------
+constexpr int kSpJoinBatch = 8;
+constexpr int kSpMaxSms = 512;                // CTAs of the split kernel at most
+constexpr int kSpListMax = 4 * kSpMaxSms;     // two partials per CTA from the prefix, two from the own segment
+
 struct SpJoin {
   float M, L;
   float4 acc;
-  __device__ __forceinline__ void add(float2 ml, float4 o) {
-    const float top = fmaxf(M, ml.x);
-    const float a = fast_exp2(M - top), w = fast_exp2(ml.x - top);
+  // one batch: its weights relative to the new maximum
+  __device__ __forceinline__ void add(const float2 (&ml)[kSpJoinBatch], const float4 (&o)[kSpJoinBatch]) {
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < kSpJoinBatch; ++u) top = fmaxf(top, ml[u].x);
     if (top == -INFINITY) return;  // no visible key so far
-    L = L * a + ml.y * w;
-    acc.x = acc.x * a + o.x * w;
-    acc.y = acc.y * a + o.y * w;
-    acc.z = acc.z * a + o.z * w;
-    acc.w = acc.w * a + o.w * w;
+    const float a = fast_exp2(M - top);
+    L *= a;
+    acc.x *= a; acc.y *= a; acc.z *= a; acc.w *= a;
+#pragma unroll
+    for (int u = 0; u < kSpJoinBatch; ++u) {
+      const float w = fast_exp2(ml[u].x - top);
+      L += ml[u].y * w;
+      acc.x += o[u].x * w; acc.y += o[u].y * w; acc.z += o[u].z * w; acc.w += o[u].w * w;
+    }
     M = top;
   }
 };
 
-template <int D>
-__device__ __forceinline__ void sp_join_segment(const SpParams &p, const SpPlan &pl, int e, const SpEntity &x, int h,
-                                                int tile, int r, int c4, SpJoin &jn) {
-  const int pair = tile >> 1, dual = 2 * pair + 1 < x.tiles, rows = sp_rows(p, x, tile);
-  const uint32_t unit = (1u + dual) * kSpCostTile;
-  const uint32_t base = pl.cost[e] + h * x.head_cost + pair * (kSpCostSeg + 2u * x.key_tiles * kSpCostTile);
-  const uint32_t seg_slot = pl.slot[e] + (h * x.pairs + pair) * x.slot_rows;
-  const int c1 = pl.owner(base + kSpCostSeg + unit * x.key_tiles - 1);
-  for (int c = pl.owner(base); c <= c1; ++c) {
-    const int n = sp_tile_at(pl.begin(c + 1), base, unit, x.key_tiles) - sp_tile_at(pl.begin(c), base, unit, x.key_tiles);
-    if (n <= 0) continue;
-    const int subs = dual || n == 1 ? 1 : 2;
-    for (int u = 0; u < subs; ++u) {
-      const size_t slot = seg_slot + 2u * kSpTile * c + (dual ? (tile & 1) * kSpTile : u * rows);
-      const float2 ml = p.part_ml[slot + r];
-      const float4 o = (reinterpret_cast<const float4 *>(p.part_o + slot * D) + r)[static_cast<size_t>(c4) * rows];
-      jn.add(ml, o);
+// Appends the first partial rows of a row tile's partials of one segment to
+// list[n ..]; returns the new length.  A whole warp calls it.
+__device__ __forceinline__ int sp_list(const SpCut &cut, const SpParams &p, const uint4 &rec, const SpEntity &x, int h,
+                                       int tile, uint32_t *list, int n) {
+  if (x.head_cost == 0) return n;
+  const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
+  const uint32_t base = rec.x + h * x.head_cost + pair * x.pair_cost();
+  const uint32_t slot = rec.y + (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
+  const int rows = sp_rows(p, x, tile);
+  const int last = cut.owner(base + kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual) - 1);
+  for (int c0 = cut.owner(base); c0 <= last; c0 += 32) {
+    const int c = c0 + lane;
+    int k = 0;
+    if (c <= last) {
+      k = sp_tile_at(cut.begin(c + 1), base, dual, x.key_tiles) - sp_tile_at(cut.begin(c), base, dual, x.key_tiles);
+      k = dual ? min(k, 1) : min(k, 2);  // partials of this piece
     }
+    const unsigned one = __ballot_sync(0xffffffffu, k > 0), two = __ballot_sync(0xffffffffu, k > 1);
+    const unsigned below = (1u << lane) - 1u;
+    const int at = n + __popc(one & below) + __popc(two & below);
+    for (int u = 0; u < k; ++u) list[at + u] = slot + 2u * kSpTile * c + u * rows;
+    n += __popc(one) + __popc(two);
   }
+  return n;
 }
 
 template <int D>
 __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(const __grid_constant__ SpParams p) {
   constexpr float kLn2 = 0.6931471805599453f;
   constexpr int C4 = D / 4;
-  extern __shared__ int s_plan[];
-  __shared__ uint32_t s_warp[kSpMergeThreads / 32][2];
-  grid_launch_dependents();
-  const SpPlan pl = sp_plan<kSpMergeThreads>(p, s_plan, s_warp);
+  __shared__ uint32_t s_list[2][kSpListMax];
+  __shared__ int s_pre[2], s_all[2], s_rows[2];  // list lengths (prefix, all) and rows of the prefix's row tiles
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int b = blockIdx.x / p.H_kv, h = blockIdx.x - b * p.H_kv;
   grid_dependency_wait();
-  const int R = p.n_q * p.group, per = R * C4;
-  const int units_per = (per + kSpMergeThreads - 1) / kSpMergeThreads;
-  const int units = p.B * p.H_kv * units_per;
-#pragma unroll 1
-  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int seg = unit / units_per, item = (unit - seg * units_per) * kSpMergeThreads + threadIdx.x;
-    if (item >= per) continue;
-    const int b = seg / p.H_kv, h = seg - b * p.H_kv;
+  grid_launch_dependents();
+  const SpCut cut(*p.total, p.G);
+  const uint4 rec = p.plan[p.num_groups + b];
+  const int keys = static_cast<int>(rec.z), R = p.n_q * p.group, per = R * C4;
+  int tok0 = 0, tile0 = 0;  // the sequence's first token within its group's, and that token's row tile
+  if (keys > 0) {
+    const int g = static_cast<int>(rec.w);
+    const uint4 pre = p.plan[g];
+    const int first = static_cast<int>(pre.w);
+    tok0 = (b - first) * p.n_q;
+    tile0 = sp_tiles(p, tok0);
+    if (warp < 2) {
+      const int next = g + 1 < p.num_groups ? static_cast<int>(p.plan[g + 1].w) : p.B;
+      const SpEntity px = sp_entity(p, false, first, next - first, static_cast<int>(pre.z));
+      const int tile = tile0 + warp;
+      int n = 0, rows = 0;
+      if (tile < px.tiles) {
+        n = sp_list(cut, p, pre, px, h, tile, s_list[warp], 0);
+        rows = sp_rows(p, px, tile);
+      }
+      const int all = sp_list(cut, p, rec, sp_entity(p, true, b, 1, keys), h, 0, s_list[warp], n);
+      s_pre[warp] = n;
+      s_all[warp] = all;
+      s_rows[warp] = rows;
+    }
+    __syncthreads();
+  }
+  for (int item = blockIdx.y * kSpMergeThreads + tid; item < per; item += gridDim.y * kSpMergeThreads) {
     const int c4 = item / R, r = item - c4 * R, i = r / p.group, j = r - i * p.group;
+    const size_t row = (static_cast<size_t>(b) * p.n_q + i) * p.H_q + static_cast<size_t>(h) * p.group + j;
     SpJoin jn;
     jn.M = -INFINITY;
     jn.L = 0.f;
     jn.acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int e = p.num_groups + b;
-    const SpEntity own = sp_entity(p, pl, e);
-    if (own.keys > 0) {
-      int lo = 0, hi = p.num_groups;  // last group that starts at or before b
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (pl.start[mid] <= b) lo = mid + 1; else hi = mid;
+    float inv = 0.f;
+    if (keys > 0) {
+      const int sel = (tok0 + i >= (tile0 + 1) * p.tokens_per_tile);
+      const int row_pre = (tok0 + i - (tile0 + sel) * p.tokens_per_tile) * p.group + j;
+      const int pre = s_pre[sel], all = s_all[sel], rows_pre = s_rows[sel];
+      for (int k0 = 0; k0 < all; k0 += kSpJoinBatch) {
+        float2 ml[kSpJoinBatch];
+        float4 o[kSpJoinBatch];
+#pragma unroll
+        for (int u = 0; u < kSpJoinBatch; ++u) {
+          ml[u] = make_float2(-INFINITY, 0.f);
+          o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k0 + u < all) {
+            const bool in_pre = k0 + u < pre;
+            const uint32_t at = s_list[sel][k0 + u];
+            const int rr = in_pre ? row_pre : r, rows = in_pre ? rows_pre : R;
+            ml[u] = p.part_ml[at + rr];
+            o[u] = (reinterpret_cast<const float4 *>(p.part_o) + static_cast<size_t>(at) * C4 + rr)[static_cast<size_t>(c4) * rows];
+          }
+        }
+        jn.add(ml, o);
       }
-      const int g = lo - 1;
-      const SpEntity pre = sp_entity(p, pl, g);
-      if (pre.head_cost > 0) {
-        const int token = b * p.n_q + i - pre.token0, tile = token / p.tokens_per_tile;
-        sp_join_segment<D>(p, pl, g, pre, h, tile, (token - tile * p.tokens_per_tile) * p.group + j, c4, jn);
-      }
-      sp_join_segment<D>(p, pl, e, own, h, 0, r, c4, jn);
+      inv = 1.f / jn.L;
     }
-    const size_t row = (static_cast<size_t>(b) * p.n_q + i) * p.H_q + static_cast<size_t>(h) * p.group + j;
-    const float inv = own.keys > 0 ? 1.f / jn.L : 0.f;
     uint2 packed;
     packed.x = pack_bf16x2(jn.acc.x * inv, jn.acc.y * inv);
     packed.y = pack_bf16x2(jn.acc.z * inv, jn.acc.w * inv);
     *reinterpret_cast<uint2 *>(p.out + row * D + 4 * c4) = packed;
-    if (p.lse && c4 == 0) p.lse[row] = own.keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
+    if (p.lse && c4 == 0) p.lse[row] = keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
   }
 }
 
@@ -931,18 +978,20 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
   // at most half of that plus one pairs, of at most 2 * kSpTile partial rows each
   const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
   SpBounds b;
-  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostTile + B * (kSpCostSeg + own_tiles * kSpCostTile));
+  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles + B * (kSpCostSeg + own_tiles));
   b.rows = H_kv * (pairs * 2 * kSpTile + 2 * tokens * group) + 2LL * kSpTile * G;
   return b;
 }
 
 struct SpLayout {
-  size_t ml_off, o_off, total;
+  size_t total_off, plan_off, ml_off, o_off, total;
 };
 
-static SpLayout sp_layout(const SpBounds &b, int D) {
+static SpLayout sp_layout(const SpBounds &b, int D, int B, int num_groups) {
   SpLayout l;
-  l.ml_off = 256;
+  l.total_off = 128;
+  l.plan_off = 256;
+  l.ml_off = round_up(l.plan_off + static_cast<size_t>(B + num_groups) * sizeof(uint4), 256);
   l.o_off = round_up(l.ml_off + static_cast<size_t>(b.rows) * sizeof(float2), 256);
   l.total = l.o_off + static_cast<size_t>(b.rows) * D * sizeof(float);
   return l;
@@ -954,7 +1003,7 @@ static int sp_grid(int *G) {
   if (st != SF_OK) return st;
   if (dev.max_smem_optin < kSpSmemMax)
     return fail(SF_ERR_UNSUPPORTED, "needs %d B shared memory, device allows %d", kSpSmemMax, dev.max_smem_optin);
-  *G = dev.sm_count;
+  *G = dev.sm_count < kSpMaxSms ? dev.sm_count : kSpMaxSms;
   return SF_OK;
 }
 
@@ -1032,7 +1081,9 @@ size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_
   if (check_sp_shapes(B, n_q, H_q, H_kv, head_dim, num_groups, max_prefix_pages, max_pages_per_seq, page_size) != SF_OK ||
       sp_grid(&G) != SF_OK)
     return 0;
-  return sp_layout(sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G), head_dim).total;
+  return sp_layout(sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G), head_dim, B,
+                   num_groups)
+      .total;
 }
 
 int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v_cache,
@@ -1066,7 +1117,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   const SpBounds bounds = sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G);
   if (bounds.cost >= (1LL << 31) || bounds.rows >= (1LL << 31))
     return fail(SF_ERR_UNSUPPORTED, "up to %lld tiles and %lld partial rows (limits 2^31)", bounds.cost, bounds.rows);
-  const SpLayout lay = sp_layout(bounds, head_dim);
+  const SpLayout lay = sp_layout(bounds, head_dim, B, num_groups);
   if (workspace_bytes < lay.total)
     return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, lay.total);
   if ((st = sp_setup(dev.ordinal)) != SF_OK) return st;
@@ -1082,6 +1133,8 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.out = static_cast<__nv_bfloat16 *>(out);
   p.lse = lse;
   p.status = reinterpret_cast<uint32_t *>(ws);
+  p.total = reinterpret_cast<uint32_t *>(ws + lay.total_off);
+  p.plan = reinterpret_cast<uint4 *>(ws + lay.plan_off);
   p.part_ml = reinterpret_cast<float2 *>(ws + lay.ml_off);
   p.part_o = reinterpret_cast<float *>(ws + lay.o_off);
   p.B = B;
@@ -1094,6 +1147,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.max_prefix_pages = max_prefix_pages;
   p.max_pages = max_pages_per_seq;
   p.tokens_per_tile = kSpTile / p.group;
+  p.tile_magic = static_cast<uint32_t>(((1ull << 32) + p.tokens_per_tile - 1) / p.tokens_per_tile);
   p.oob_row = static_cast<int>(rows);
   p.G = G;
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
@@ -1116,10 +1170,14 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   cfg.numAttrs = 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, fn, m[0], m[1], m[2], m[3], p);
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix attention launch: %s", cudaGetErrorString(e));
-  const long long units = (long long)B * H_kv * ((n_q * p.group * (head_dim / 4) + kSpMergeThreads - 1) / kSpMergeThreads);
-  cfg.gridDim = dim3(static_cast<unsigned>(units < 4LL * G ? units : 4LL * G));
+  // one block per sequence and KV head, its rows over several where that leaves
+  // SMs without one
+  const int per = (n_q * p.group * (head_dim / 4) + kSpMergeThreads - 1) / kSpMergeThreads;
+  int parts = (4 * G + B * H_kv - 1) / (B * H_kv);
+  if (parts > per) parts = per;
+  cfg.gridDim = dim3(static_cast<unsigned>(B * H_kv), static_cast<unsigned>(parts));
   cfg.blockDim = dim3(kSpMergeThreads);
-  cfg.dynamicSmemBytes = sp_plan_bytes(B, num_groups);
+  cfg.dynamicSmemBytes = 0;
   e = head_dim == 128 ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128>, p)
                       : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64>, p);
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix merge launch: %s", cudaGetErrorString(e));
