@@ -8,7 +8,14 @@
 // included, and its upper 32 bits go through sincospif.  (fp32 angles are off by
 // 2^-24 of the angle, 2e-3 radians at position 32768.)
 //
-// One CTA per row.
+// Bound by HBM for prompts (q, k and v are read once, written once) and by latency
+// for a few draft rows.  A CTA takes up to kAppendRows rows: it computes their
+// cosines and sines once for all heads and finds their cache places (one warp a
+// row: a 32-ary search in row_starts), then its threads walk the heads of a row,
+// each with one 16-byte chunk of every head (and, for pairs (j, j + n), the chunk of
+// the partners), so that a thread's cosines and sines stay in registers.  Few rows
+// are spread over more CTAs by heads.  Tensors that 16-byte accesses cannot reach
+// take kv_append_any_kernel, one pair of elements at a time.
 #include <cmath>
 
 #include "sf_device.cuh"
@@ -17,6 +24,7 @@
 namespace sf {
 
 constexpr int kAppendThreads = 256;
+constexpr int kAppendRows = 8;      // rows of a CTA at most, one per warp for their places
 constexpr int kMaxHeadDim = 256;
 constexpr int kMaxHeads = 1024;
 
@@ -35,41 +43,48 @@ struct AppendParams {
   float amplitude;
 };
 
-// cos and sin (times the amplitude) of pair j of row t
-__device__ __forceinline__ float2 pair_turn(const AppendParams &p, int t, int j) {
-  int axis = p.freq_axis ? p.freq_axis[j] : 0;
+// The fraction of a turn per position of pair j, and the axis of its positions.
+__device__ __forceinline__ unsigned long long pair_step(const AppendParams &p, int j, int &axis) {
+  axis = p.freq_axis ? p.freq_axis[j] : 0;
   if (axis < 0 || axis >= p.axes) {
     set_status(p.status, SF_DEVICE_BAD_INDEX);
     axis = 0;
   }
   double turns = p.inv_freq[j] * 0.15915494309189535;  // 1 / (2 pi)
   turns -= floor(turns);
-  const unsigned long long step = __double2ull_rn(turns * 18446744073709551616.0);
-  const long long pos = p.positions[static_cast<size_t>(axis) * p.T + t];
-  const int hi = static_cast<int>(static_cast<unsigned long long>(pos) * step >> 32);
+  return __double2ull_rn(turns * 18446744073709551616.0);
+}
+
+// cos and sin (times the amplitude) at a position
+__device__ __forceinline__ float2 pair_turn(const AppendParams &p, unsigned long long step, int position) {
+  const int hi = static_cast<int>(static_cast<unsigned long long>(static_cast<long long>(position)) * step >> 32);
   float s, c;
   sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &s, &c);  // 2^-31: half turns
   return make_float2(c * p.amplitude, s * p.amplitude);
 }
 
-// The cache page and slot of row t: -1 where the row is not appended.
-__device__ __forceinline__ int row_place(const AppendParams &p, int t, int &slot) {
+// The cache row (page * H_kv * 16 + slot; head h adds h * 16) of row t, or -1
+// where the row is not appended.  A whole warp calls it.
+__device__ __forceinline__ long long row_place(const AppendParams &p, int t) {
+  const int lane = threadIdx.x & 31;
   int b, i, n;
   if (p.row_starts) {
-    int lo = 0, hi = p.B;  // last sequence that starts at or before t
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (p.row_starts[mid] <= t) lo = mid + 1; else hi = mid;
+    // the last sequence that starts at or before t: starts[b] <= t, by 32nds
+    int lo = 0, width = p.B + 1;  // candidates lo .. lo + width - 1
+    while (width > 1) {
+      const int step = (width + 31) >> 5, k = lo + lane * step;
+      const unsigned le = __ballot_sync(0xffffffffu, lane * step < width && p.row_starts[k < p.B ? k : p.B] <= t);
+      if (!(le & 1u)) break;  // (row_starts[0] > t, or not ascending)
+      const int hit = 31 - __clz(le);
+      width = min(step, width - hit * step);
+      lo += hit * step;
     }
-    b = lo - 1;
-    if (b < 0) {
-      set_status(p.status, SF_DEVICE_BAD_INDEX);
+    b = lo;
+    const int first = p.row_starts[b], end = b < p.B ? p.row_starts[b + 1] : first;
+    if (b == p.B) return -1;  // padding
+    if (t < first || t >= end) {
+      if (lane == 0) set_status(p.status, SF_DEVICE_BAD_INDEX);
       return -1;
-    }
-    const int first = p.row_starts[b], end = p.row_starts[b + 1];
-    if (t >= end) {
-      if (b != p.B - 1) set_status(p.status, SF_DEVICE_BAD_INDEX);
-      return -1;  // padding
     }
     i = t - first;
     n = end - first;
@@ -82,44 +97,160 @@ __device__ __forceinline__ int row_place(const AppendParams &p, int t, int &slot
   if (len == 0) return -1;  // idle slot
   const long long at = static_cast<long long>(len) - n + i;
   if (at < 0 || at >= static_cast<long long>(p.max_pages) * SF_PAGE_SIZE) {
-    set_status(p.status, SF_DEVICE_BAD_SEQLEN);
+    if (lane == 0) set_status(p.status, SF_DEVICE_BAD_SEQLEN);
     return -1;
   }
-  slot = static_cast<int>(at % SF_PAGE_SIZE);
   const int page = p.block_table[static_cast<size_t>(b) * p.max_pages + at / SF_PAGE_SIZE];
   if (page < 0 || page >= p.num_pages) {
-    set_status(p.status, SF_DEVICE_BAD_PAGE);
+    if (lane == 0) set_status(p.status, SF_DEVICE_BAD_PAGE);
     return -1;
   }
-  return page;
+  return static_cast<long long>(page) * p.H_kv * SF_PAGE_SIZE + at % SF_PAGE_SIZE;
 }
 
 __device__ __forceinline__ float load_as_float(const void *p, long long i, int wide) {
   return wide ? static_cast<const float *>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
 }
 
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendParams p) {
-  __shared__ float2 s_turn[kMaxHeadDim / 2];
-  __shared__ int s_place[2];
-  const int tid = threadIdx.x, t = blockIdx.x;
+// 8 neighbouring elements as fp32, and back as bf16
+template <bool kWide>
+__device__ __forceinline__ void load8(const void *base, long long at, float (&v)[8]) {
+  if constexpr (kWide) {
+    const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + at);
+    const float4 a = src[0], b = src[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(base) + at);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+
+__device__ __forceinline__ void store8(__nv_bfloat16 *dst, const float (&v)[8]) {
+  *reinterpret_cast<uint4 *>(dst) =
+      make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+
+// `rows` rows per CTA; blockIdx.y of gridDim.y takes every gridDim.y-th pass over
+// the heads.
+template <bool kWide, bool kInterleaved>
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendParams p, int rows) {
+  __shared__ float2 s_turn[kAppendRows][kMaxHeadDim / 2];
+  __shared__ long long s_place[kAppendRows];
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int t0 = blockIdx.x * rows, nr = min(rows, p.T - t0);
   grid_dependency_wait();
-  for (int j = tid; j < p.pairs; j += kAppendThreads) s_turn[j] = pair_turn(p, t, j);
-  if (tid == 0) {
-    int slot = 0;
-    s_place[0] = row_place(p, t, slot);
-    s_place[1] = slot;
+  grid_launch_dependents();
+  if (warp < nr) {
+    const long long place = row_place(p, t0 + warp);
+    if ((tid & 31) == 0) s_place[warp] = place;
+  }
+  // threads of one pair, kAppendThreads / pairs rows at a time
+  if (p.pairs > 0) {
+    const int j = tid % p.pairs, each = kAppendThreads / p.pairs;
+    if (tid < each * p.pairs) {
+      int axis;
+      const unsigned long long step = pair_step(p, j, axis);
+      for (int r = tid / p.pairs; r < nr; r += each)
+        s_turn[r][j] = pair_turn(p, step, p.positions[static_cast<size_t>(axis) * p.T + t0 + r]);
+    }
   }
   __syncthreads();
-  const int page = s_place[0], slot = s_place[1];
+  // units of a head: its rotated chunks (or pairs of chunks), then the others
+  const int turned = kInterleaved ? p.pairs / 4 : p.pairs / 8, rest = (p.D - 2 * p.pairs) / 8, units = turned + rest;
+  const int u = tid % units, lane_head = tid / units, heads_at_once = kAppendThreads / units;
+  if (lane_head < heads_at_once) {
+    for (int r = 0; r < nr; ++r) {
+      const int t = t0 + r;
+      const long long place = s_place[r];
+      const int heads = p.H_q + (place >= 0 ? p.H_kv : 0);
+      float2 w[8];
+      if (u < turned) {
+#pragma unroll
+        for (int i = 0; i < (kInterleaved ? 4 : 8); ++i) w[i] = s_turn[r][(kInterleaved ? 4 : 8) * u + i];
+      }
+#pragma unroll 2
+      for (int h = lane_head + blockIdx.y * heads_at_once; h < heads; h += heads_at_once * gridDim.y) {
+        const bool is_q = h < p.H_q;
+        const void *src = is_q ? p.q : p.k;
+        const long long so = is_q ? t * p.q_row + h * p.q_head : t * p.k_row + (h - p.H_q) * p.k_head;
+        __nv_bfloat16 *dst = is_q ? p.q_out + (static_cast<size_t>(t) * p.H_q + h) * p.D
+                                  : p.k_cache + static_cast<size_t>(place + (h - p.H_q) * SF_PAGE_SIZE) * p.D;
+        float a[8];
+        if (u >= turned) {
+          const int at = 2 * p.pairs + (u - turned) * 8;
+          load8<kWide>(src, so + at, a);
+          store8(dst + at, a);
+        } else if constexpr (kInterleaved) {
+          load8<kWide>(src, so + 8 * u, a);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = a[2 * i], y = a[2 * i + 1];
+            a[2 * i] = x * w[i].x - y * w[i].y;
+            a[2 * i + 1] = x * w[i].y + y * w[i].x;
+          }
+          store8(dst + 8 * u, a);
+        } else {
+          float b[8];
+          load8<kWide>(src, so + 8 * u, a);
+          load8<kWide>(src, so + p.pairs + 8 * u, b);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * w[i].x - y * w[i].y;
+            b[i] = x * w[i].y + y * w[i].x;
+          }
+          store8(dst + 8 * u, a);
+          store8(dst + p.pairs + 8 * u, b);
+        }
+      }
+    }
+  }
+  // values
+  const int chunks = p.D / 8, per_row = p.H_kv * chunks;
+  for (int x = tid + blockIdx.y * kAppendThreads; x < nr * per_row; x += kAppendThreads * gridDim.y) {
+    const int r = x / per_row, c = x - r * per_row, h = c / chunks, e = (c - h * chunks) * 8;
+    const long long place = s_place[r];
+    if (place < 0) continue;
+    float a[8];
+    load8<kWide>(p.v, (t0 + r) * p.v_row + h * p.v_head + e, a);
+    store8(p.v_cache + static_cast<size_t>(place + h * SF_PAGE_SIZE) * p.D + e, a);
+  }
+}
+
+// The same for any alignment, strides and number of pairs: one row per CTA, one
+// pair or element per thread.
+__global__ void __launch_bounds__(kAppendThreads) kv_append_any_kernel(const __grid_constant__ AppendParams p) {
+  __shared__ float2 s_turn[kMaxHeadDim / 2];
+  __shared__ long long s_place;
+  const int tid = threadIdx.x, t = blockIdx.x;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  for (int j = tid; j < p.pairs; j += kAppendThreads) {
+    int axis;
+    const unsigned long long step = pair_step(p, j, axis);
+    s_turn[j] = pair_turn(p, step, p.positions[static_cast<size_t>(axis) * p.T + t]);
+  }
+  if (tid >= kAppendThreads - 32) {
+    const long long place = row_place(p, t);
+    if (tid == kAppendThreads - 1) s_place = place;
+  }
+  __syncthreads();
+  const long long place = s_place;
   const int per = p.D - p.pairs;  // items of a rotated head: its pairs, then the single elements
-  const int heads = p.H_q + (page >= 0 ? p.H_kv : 0);
+  const int heads = p.H_q + (place >= 0 ? p.H_kv : 0);
   for (int x = tid; x < heads * per; x += kAppendThreads) {
     const int h = x / per, e = x - h * per;
     const bool is_q = h < p.H_q;
     const void *src = is_q ? p.q : p.k;
     const long long so = is_q ? t * p.q_row + h * p.q_head : t * p.k_row + (h - p.H_q) * p.k_head;
     __nv_bfloat16 *dst = is_q ? p.q_out + (static_cast<size_t>(t) * p.H_q + h) * p.D
-                              : p.k_cache + ((static_cast<size_t>(page) * p.H_kv + h - p.H_q) * SF_PAGE_SIZE + slot) * p.D;
+                              : p.k_cache + static_cast<size_t>(place + (h - p.H_q) * SF_PAGE_SIZE) * p.D;
     if (e < p.pairs) {
       const int i0 = p.interleaved ? 2 * e : e, i1 = p.interleaved ? 2 * e + 1 : e + p.pairs;
       const float a = load_as_float(src, so + i0, p.wide), b = load_as_float(src, so + i1, p.wide);
@@ -131,10 +262,10 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
       dst[i] = __float2bfloat16_rn(load_as_float(src, so + i, p.wide));
     }
   }
-  if (page < 0) return;
+  if (place < 0) return;
   for (int x = tid; x < p.H_kv * p.D; x += kAppendThreads) {
     const int h = x / p.D, e = x - h * p.D;
-    p.v_cache[((static_cast<size_t>(page) * p.H_kv + h) * SF_PAGE_SIZE + slot) * p.D + e] =
+    p.v_cache[static_cast<size_t>(place + h * SF_PAGE_SIZE) * p.D + e] =
         __float2bfloat16_rn(load_as_float(p.v, t * p.v_row + h * p.v_head + e, p.wide));
   }
 }
@@ -221,8 +352,41 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
   p.wide = dtype == SF_F32;
   p.rows = T / B;
   p.amplitude = amplitude;
-  kv_append_kernel<<<T, kAppendThreads, 0, stream>>>(p);
-  const cudaError_t err = cudaGetLastError();
+  DeviceInfo dev;
+  const int st = current_device(&dev);
+  if (st != SF_OK) return st;
+  // 16-byte accesses: whole chunks of 8 rotated elements, strides of whole chunks
+  const bool vec = p.pairs % (p.interleaved ? 4 : 8) == 0 && aligned(k, 16) && aligned(v, 16) && k_row_stride % 8 == 0 &&
+                   k_head_stride % 8 == 0 && v_row_stride % 8 == 0 && v_head_stride % 8 == 0 &&
+                   (H_q == 0 || (aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0));
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kAppendThreads);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t err;
+  if (vec) {
+    // as many rows a CTA as leave every SM several CTAs; few rows are cut by heads
+    int rows = static_cast<int>(T / (8LL * dev.sm_count));
+    rows = rows < 1 ? 1 : rows > kAppendRows ? kAppendRows : rows;
+    const int grid = (T + rows - 1) / rows;
+    const int passes = ((H_q + H_kv) * (head_dim / 8) + kAppendThreads - 1) / kAppendThreads;
+    int parts = dev.sm_count / grid;
+    parts = parts < 1 ? 1 : parts > passes ? passes : parts;
+    cfg.gridDim = dim3(grid, parts);
+    if (p.wide)
+      err = p.interleaved ? cudaLaunchKernelEx(&cfg, kv_append_kernel<true, true>, p, rows)
+                          : cudaLaunchKernelEx(&cfg, kv_append_kernel<true, false>, p, rows);
+    else
+      err = p.interleaved ? cudaLaunchKernelEx(&cfg, kv_append_kernel<false, true>, p, rows)
+                          : cudaLaunchKernelEx(&cfg, kv_append_kernel<false, false>, p, rows);
+  } else {
+    cfg.gridDim = dim3(T);
+    err = cudaLaunchKernelEx(&cfg, kv_append_any_kernel, p);
+  }
   if (err != cudaSuccess) return fail(SF_ERR_CUDA, "kv append launch: %s", cudaGetErrorString(err));
   return SF_OK;
 }
