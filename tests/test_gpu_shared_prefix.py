@@ -161,6 +161,30 @@ def test_calls_in_a_row_and_repeats_are_bit_identical():
         close(o, l, ref.shared_prefix(*(t.cpu() for t in a)))
 
 
+def test_many_calls_close_behind_each_other():
+    # pieces of one and two row tiles, of one key tile and of many, in turn: the
+    # streams of a CTA run ahead of each other by amounts that vary from call to call
+    require_gpu()
+    sets = [[a.cuda() for a in make([9, 3, 15, 5], [4800, 700, 4100, 130], [8 + (67 * b) % 500 for b in range(32)], 8, 28, 4,
+                                    128, seed=30)],
+            [a.cuda() for a in make([2, 1, 4, 1], [900, 40, 0, 3000], [2 + (91 * b) % 300 for b in range(8)], 2, 8, 8, 64,
+                                    seed=31)]]
+    first = [sfv.shared_prefix_attention(*a) for a in sets]
+    ws = [sfv.new_workspace(sfv.shared_prefix_attention_workspace_size(
+        *a[0].shape[:3], a[1].shape[1], a[0].shape[3], a[3].shape[0], a[3].shape[1], a[6].shape[1])) for a in sets]
+    outs = [[torch.empty_like(o), torch.empty_like(l)] for o, l in first]
+    for a, w, (o, l) in zip(sets, ws, outs):
+        for _ in range(400):
+            sfv.shared_prefix_attention(*a, out=o, lse=l, workspace=w)
+    for _ in range(400):
+        for a, w, (o, l) in zip(sets, ws, outs):
+            sfv.shared_prefix_attention(*a, out=o, lse=l, workspace=w)
+    for (o, l), (o2, l2), w in zip(first, outs, ws):
+        assert sfv.read_device_status(w) == 0
+        assert torch.equal(o, o2) and torch.equal(l, l2)
+    close(*first[1], ref.shared_prefix(*(t.cpu() for t in sets[1])))
+
+
 def test_agrees_with_verify_attention_where_nothing_is_shared():
     require_gpu()
     args = make([1, 1, 1], [0, 0, 0], [70, 500, 8], 8, 28, 4, 128, seed=17)
