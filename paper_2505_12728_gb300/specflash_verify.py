@@ -550,15 +550,16 @@ def visual_compress(queries, features, *, out=None, workspace=None, stream=None)
 # --------------------------------------------------------------------------- #
 # the decoder layer around the attention                                      #
 # --------------------------------------------------------------------------- #
-_DTYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float8_e4m3fn: 2}
+# Host time is most of a small call here, and every tensor's checks are on it: a
+# well-formed tensor takes one expression (no call of its own where that is
+# possible), and strides are asked for only where a tensor is not contiguous.
+_Tensor, _BF16, _F32, _E4M3 = torch.Tensor, torch.bfloat16, torch.float32, torch.float8_e4m3fn
+_I32, _F64 = torch.int32, torch.float64
 
 
-def _need_rows(t, name, dtype, shape):
-    """A CUDA tensor of this type and shape whose innermost dimension is
-    contiguous (its other strides are passed on)."""
-    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape
-            and (t.stride(-1) == 1 or t.shape[-1] == 1)):
-        return
+def _refuse_rows(t, name, dtype, shape):
+    """Raises what is wrong with a tensor that may be strided but for its last
+    dimension."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
@@ -567,8 +568,31 @@ def _need_rows(t, name, dtype, shape):
         raise ValueError(f"{name} must be a CUDA tensor")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.shape[-1] != 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
+    raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _row_stride(t, name, dtype, shape):
+    """Elements between the rows of a checked CUDA tensor [T][d]."""
+    if t.__class__ is _Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape:
+        if t.is_contiguous():
+            return shape[1]
+        row, last = t.stride()
+        if last == 1 or shape[1] == 1:
+            return row
+    elif isinstance(t, _Tensor) and t.__class__ is not _Tensor:  # a subclass, such as a Parameter
+        return _row_stride(t.detach().as_subclass(_Tensor), name, dtype, shape)
+    _refuse_rows(t, name, dtype, shape)
+
+
+def _head_strides(t, name, dtype, shape):
+    """Elements between the rows and heads of a checked CUDA tensor [T][H][d]."""
+    if t.__class__ is _Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape:
+        row, head, last = t.stride()
+        if last == 1 or shape[2] == 1:
+            return row, head
+    elif isinstance(t, _Tensor) and t.__class__ is not _Tensor:
+        return _head_strides(t.detach().as_subclass(_Tensor), name, dtype, shape)
+    _refuse_rows(t, name, dtype, shape)
 
 
 def _new(shape, dtype, device, stream, zero=False):
@@ -588,46 +612,52 @@ def add_rms_norm(x, weight, residual=None, *, eps=1e-6, out_dtype=torch.bfloat16
     scales, one per row (group 0) or per 128 columns (group 128).
     Returns (out [T][d], residual_out like x or None, scales [T][groups] or
     None).  residual_out may be the residual itself."""
-    if not isinstance(x, torch.Tensor):
+    if not isinstance(x, _Tensor):
         raise TypeError("x must be a torch.Tensor")
-    if x.dim() != 2:
-        raise ValueError(f"x has shape {tuple(x.shape)}, expected (T, d)")
     shape, kind = x.shape, x.dtype
+    if len(shape) != 2:
+        raise ValueError(f"x has shape {tuple(shape)}, expected (T, d)")
     T, d = shape
-    if kind is not torch.bfloat16 and kind is not torch.float32:
+    if kind is not _BF16 and kind is not _F32:
         raise TypeError(f"x must be bfloat16 or float32, got {kind}")
-    _need_rows(x, "x", kind, shape)
-    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.bfloat16, torch.float32):
+    x_row = _row_stride(x, "x", kind, shape)
+    if not isinstance(weight, _Tensor) or (weight.dtype is not _BF16 and weight.dtype is not _F32):
         raise TypeError("weight must be a bfloat16 or float32 torch.Tensor")
-    _need(weight, "weight", weight.dtype, (d,))
+    if not (weight.is_cuda and weight.is_contiguous() and weight.shape == (d,)):
+        _need(weight, "weight", weight.dtype, (d,))
+    r_ptr = ro_ptr = None
+    r_row = ro_row = 0
     if residual is not None:
-        _need_rows(residual, "residual", kind, shape)
+        r_row = _row_stride(residual, "residual", kind, shape)
         if residual_out is None:
             residual_out = _new(shape, kind, x.device, stream)
-        _need_rows(residual_out, "residual_out", kind, shape)
+        ro_row = _row_stride(residual_out, "residual_out", kind, shape)
+        r_ptr, ro_ptr = residual.data_ptr(), residual_out.data_ptr()
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     if out is None:
-        if out_dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        if out_dtype is not _BF16 and out_dtype is not _E4M3:
             raise TypeError(f"out_dtype must be bfloat16 or float8_e4m3fn, got {out_dtype}")
         out = _new(shape, out_dtype, x.device, stream)
-    elif not isinstance(out, torch.Tensor) or out.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+    elif not isinstance(out, _Tensor) or (out.dtype is not _BF16 and out.dtype is not _E4M3):
         raise TypeError("out must be a bfloat16 or float8_e4m3fn torch.Tensor")
-    _need_rows(out, "out", out.dtype, shape)
-    if out.dtype is torch.float8_e4m3fn:
-        if group not in (0, 128):
+    o_row = _row_stride(out, "out", out.dtype, shape)
+    o_type, s_ptr = 0, None
+    if out.dtype is _E4M3:
+        if group != 0 and group != 128:
             raise ValueError(f"group={group}: 0 (a scale per row) or 128 columns")
         groups = -(-d // group) if group else 1
         if scales is None:
-            scales = _new((T, groups), torch.float32, x.device, stream)
-        _need(scales, "scales", torch.float32, (T, groups))
+            scales = _new((T, groups), _F32, x.device, stream)
+        _need(scales, "scales", _F32, (T, groups))
+        o_type, s_ptr = 2, scales.data_ptr()
     elif scales is not None or group:
         raise ValueError("scales and group belong to float8_e4m3fn output")
-    _check(load_library().sf_add_rms_norm(
-        x.data_ptr(), _ptr(residual), weight.data_ptr(), _DTYPES[kind], _DTYPES[weight.dtype], T, d,
-        x.stride(0), 0 if residual is None else residual.stride(0), eps, _ptr(residual_out),
-        0 if residual_out is None else residual_out.stride(0), out.data_ptr(), _DTYPES[out.dtype],
-        out.stride(0), group, _ptr(scales), _stream_handle(stream)))
+    status = (_lib or load_library()).sf_add_rms_norm(
+        x.data_ptr(), r_ptr, weight.data_ptr(), kind is _F32, weight.dtype is _F32, T, d, x_row, r_row, eps, ro_ptr,
+        ro_row, out.data_ptr(), o_type, o_row, group, s_ptr, _stream_handle(stream))
+    if status:
+        _check(status)
     return out, residual_out, scales
 
 
@@ -646,61 +676,75 @@ def kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_l
     and seq_lens (counting the new rows) as for verify_attention; row_starts
     int32 [B + 1] for sequences of different numbers of new rows (None: T / B
     each).  Returns q_out bf16 [T][H_q][d] or None."""
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+    if not isinstance(k, _Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor [T][H_kv][d]")
-    T, H_kv, d = k.shape
-    kind = k.dtype
-    if kind is not torch.bfloat16 and kind is not torch.float32:
+    shape, kind = k.shape, k.dtype
+    T, H_kv, d = shape
+    if kind is not _BF16 and kind is not _F32:
         raise TypeError(f"k must be bfloat16 or float32, got {kind}")
-    _need_rows(k, "k", kind, k.shape)
-    _need_rows(v, "v", kind, k.shape)
-    dev = k.device
+    k_row, k_head = _head_strides(k, "k", kind, shape)
+    v_row, v_head = _head_strides(v, "v", kind, shape)
     H_q = q_row = q_head = 0
+    q_ptr = out_ptr = pos_ptr = freq_ptr = None
     if q is not None:
-        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        if not isinstance(q, _Tensor) or q.dim() != 3:
             raise ValueError("q must be a tensor [T][H_q][d] or None")
         H_q = q.shape[1]
-        _need_rows(q, "q", kind, (T, H_q, d))
-        q_row, q_head, _ = q.stride()
+        q_shape = (T, H_q, d)
+        q_row, q_head = _head_strides(q, "q", kind, q_shape)
         if q_out is None:
-            q_out = _new((T, H_q, d), torch.bfloat16, dev, stream)
-        _need(q_out, "q_out", torch.bfloat16, (T, H_q, d))
+            q_out = _new(q_shape, _BF16, k.device, stream)
+        _need(q_out, "q_out", _BF16, q_shape)
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out needs a q")
-    _need(block_table, "block_table", torch.int32)
-    if block_table.dim() != 2:
+    if not isinstance(block_table, _Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be [B][max_pages]")
     B, max_pages = block_table.shape
-    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+    if not isinstance(k_cache, _Tensor) or k_cache.dim() != 4:
         raise ValueError("k_cache must be a tensor [pages][H_kv][16][d]")
-    num_pages, page = k_cache.shape[0], k_cache.shape[2]
-    _need(k_cache, "k_cache", torch.bfloat16, (num_pages, H_kv, page, d))
-    _need(v_cache, "v_cache", torch.bfloat16, k_cache.shape)
-    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    cache = k_cache.shape
+    num_pages, heads, page, wide = cache
+    if heads != H_kv or wide != d:
+        raise ValueError(f"k_cache has shape {tuple(cache)}, expected (pages, {H_kv}, 16, {d})")
+    try:
+        fine = (k_cache.dtype is _BF16 and v_cache.dtype is _BF16 and block_table.dtype is _I32 and seq_lens.dtype is _I32
+                and k_cache.is_cuda and v_cache.is_cuda and block_table.is_cuda and seq_lens.is_cuda
+                and k_cache.is_contiguous() and v_cache.is_contiguous() and block_table.is_contiguous()
+                and seq_lens.is_contiguous() and v_cache.shape == cache and seq_lens.dim() == 1
+                and seq_lens.numel() == B)
+    except AttributeError:
+        fine = False
+    if not fine:
+        _need(k_cache, "k_cache", _BF16)
+        _need(v_cache, "v_cache", _BF16, cache)
+        _need(block_table, "block_table", _I32)
+        _need(seq_lens, "seq_lens", _I32, (B,))
     axes = pairs = 0
     if inv_freq is not None:
-        _need(inv_freq, "inv_freq", torch.float64)
-        if inv_freq.dim() != 1 or positions is None or positions.dim() != 2:
-            raise ValueError("inv_freq must be [rotary_dim / 2] and positions [axes][T]")
+        _need(inv_freq, "inv_freq", _F64)
+        if inv_freq.dim() != 1 or not isinstance(positions, _Tensor) or positions.dim() != 2:
+            raise ValueError("inv_freq must be [rotary_dim / 2] and positions a tensor [axes][T]")
         pairs, axes = inv_freq.shape[0], positions.shape[0]
-        _need(positions, "positions", torch.int32, (axes, T))
+        _need(positions, "positions", _I32, (axes, T))
+        pos_ptr, freq_ptr = positions.data_ptr(), inv_freq.data_ptr()
         if axis is not None:
-            _need(axis, "axis", torch.int32, (pairs,))
+            _need(axis, "axis", _I32, (pairs,))
     elif positions is not None or axis is not None:
         raise ValueError("positions and axis need inv_freq")
     if row_starts is not None:
-        _need(row_starts, "row_starts", torch.int32, (B + 1,))
+        _need(row_starts, "row_starts", _I32, (B + 1,))
     if workspace is None:
-        workspace = _new(kv_append_workspace_size(), torch.uint8, dev, stream, zero=True)
+        workspace = _new(kv_append_workspace_size(), torch.uint8, k.device, stream, zero=True)
     _need_workspace(workspace)
-    k_row, k_head, _ = k.stride()
-    v_row, v_head, _ = v.stride()
-    _check(load_library().sf_kv_append(
-        _ptr(q), k.data_ptr(), v.data_ptr(), _DTYPES[kind], q_row, q_head, k_row, k_head, v_row, v_head,
-        _ptr(positions), axes, _ptr(inv_freq), _ptr(axis), 2 * pairs, bool(interleaved), amplitude,
-        block_table.data_ptr(), seq_lens.data_ptr(), _ptr(row_starts), T, B, H_q, H_kv, d, page,
-        num_pages, max_pages, _ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    status = (_lib or load_library()).sf_kv_append(
+        q_ptr, k.data_ptr(), v.data_ptr(), kind is _F32, q_row, q_head, k_row, k_head, v_row, v_head,
+        pos_ptr, axes, freq_ptr, None if axis is None else axis.data_ptr(), 2 * pairs, interleaved, amplitude,
+        block_table.data_ptr(), seq_lens.data_ptr(), None if row_starts is None else row_starts.data_ptr(), T, B, H_q,
+        H_kv, d, page, num_pages, max_pages, out_ptr, k_cache.data_ptr(), v_cache.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+    if status:
+        _check(status)
     return q_out
 
 
@@ -725,43 +769,65 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     block_table int32 [B][pages] and seq_lens int32 [B] (0: idle slot) describe
     each sequence's own tokens, draft rows included.  Returns (out bf16
     [B][n_q][H_q][d], lse fp32 [B][n_q][H_q] or None)."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+    if not isinstance(q, _Tensor) or q.dim() != 4:
         raise ValueError("q must be a tensor [B][n_q][H_q][d]")
     B, n_q, H_q, d = shape = q.shape
-    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+    if not isinstance(k_cache, _Tensor) or k_cache.dim() != 4:
         raise ValueError("k_cache must be a tensor [pages][H_kv][16][d]")
-    num_pages, H_kv, page, d2 = k_cache.shape
+    cache = k_cache.shape
+    num_pages, H_kv, page, d2 = cache
     if d2 != d:
         # the library sizes the caches' tensor maps from q's head_dim
         raise ValueError("head_dim of q and caches differ")
-    _need(q, "q", torch.bfloat16)
-    _need(k_cache, "k_cache", torch.bfloat16)
-    _need(v_cache, "v_cache", torch.bfloat16, k_cache.shape)
-    _need(prefix_table, "prefix_table", torch.int32)
-    _need(block_table, "block_table", torch.int32)
+    try:
+        fine = (q.dtype is _BF16 and k_cache.dtype is _BF16 and v_cache.dtype is _BF16 and prefix_table.dtype is _I32
+                and block_table.dtype is _I32 and q.is_cuda and k_cache.is_cuda and v_cache.is_cuda
+                and prefix_table.is_cuda and block_table.is_cuda and q.is_contiguous() and k_cache.is_contiguous()
+                and v_cache.is_contiguous() and prefix_table.is_contiguous() and block_table.is_contiguous()
+                and v_cache.shape == cache)
+    except AttributeError:
+        fine = False
+    if not fine:
+        _need(q, "q", _BF16)
+        _need(k_cache, "k_cache", _BF16)
+        _need(v_cache, "v_cache", _BF16, cache)
+        _need(prefix_table, "prefix_table", _I32)
+        _need(block_table, "block_table", _I32)
     if prefix_table.dim() != 2 or block_table.dim() != 2:
         raise ValueError("prefix_table and block_table must be two-dimensional")
     G, max_prefix = prefix_table.shape
-    max_pages = block_table.shape[1]
-    if block_table.shape[0] != B:
+    rows, max_pages = block_table.shape
+    if rows != B:
         raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected ({B}, max_pages)")
-    _need(prefix_lens, "prefix_lens", torch.int32, (G,))
-    _need(group_starts, "group_starts", torch.int32, (G + 1,))
-    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    try:
+        fine = (prefix_lens.dtype is _I32 and group_starts.dtype is _I32 and seq_lens.dtype is _I32
+                and prefix_lens.is_cuda and group_starts.is_cuda and seq_lens.is_cuda and prefix_lens.is_contiguous()
+                and group_starts.is_contiguous() and seq_lens.is_contiguous() and prefix_lens.dim() == 1
+                and group_starts.dim() == 1 and seq_lens.dim() == 1 and prefix_lens.numel() == G
+                and group_starts.numel() == G + 1 and seq_lens.numel() == B)
+    except AttributeError:
+        fine = False
+    if not fine:
+        _need(prefix_lens, "prefix_lens", _I32, (G,))
+        _need(group_starts, "group_starts", _I32, (G + 1,))
+        _need(seq_lens, "seq_lens", _I32, (B,))
     if out is None:
-        out = _new(shape, torch.bfloat16, q.device, stream)
-    _need(out, "out", torch.bfloat16, shape)
+        out = _new(shape, _BF16, q.device, stream)
+    _need(out, "out", _BF16, shape)
     if lse is None and with_lse:
-        lse = _new((B, n_q, H_q), torch.float32, q.device, stream)
+        lse = _new((B, n_q, H_q), _F32, q.device, stream)
     if lse is not None:
-        _need(lse, "lse", torch.float32, (B, n_q, H_q))
+        _need(lse, "lse", _F32, (B, n_q, H_q))
     if workspace is None:
         workspace = _new(shared_prefix_attention_workspace_size(
             B, n_q, H_q, H_kv, d, G, max_prefix, max_pages, page), torch.uint8, q.device, stream, zero=True)
     _need_workspace(workspace)
-    _check(load_library().sf_shared_prefix_attention(
+    status = (_lib or load_library()).sf_shared_prefix_attention(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), prefix_table.data_ptr(),
         prefix_lens.data_ptr(), group_starts.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
         B, n_q, H_q, H_kv, d, page, num_pages, G, max_prefix, max_pages, softmax_scale,
-        out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+        out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        _stream_handle(stream))
+    if status:
+        _check(status)
     return out, lse
