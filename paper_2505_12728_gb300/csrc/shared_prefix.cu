@@ -35,9 +35,9 @@
 // The running maximum is a reference that moves when a row's new maximum
 // exceeds it by more than kSpRescaleLog2, so rescaling O is rare.  The row sums
 // are sums of the fp32 weights.  P V takes the weights rounded to bf16 (up to 2^-8
-// of a weight, which averages out over many keys), and on every segment's first
-// key tile also what that rounding left, as a second bf16 term: rows with a
-// handful of visible keys have them there.
+// of a weight, which averages out over many keys), and where rows may see fewer
+// than 128 keys outside a segment, on the segment's first key tile also what that
+// rounding left, as a second bf16 term.
 // Every wait is bounded; a timeout sets SF_DEVICE_TIMEOUT and stops every role.
 #include <cmath>
 #include <mutex>
@@ -62,6 +62,18 @@ constexpr int kSpSmemMax = 227 * 1024;
 constexpr uint32_t kSpCostSeg = 2;
 constexpr int kSpItems = 4;      // pieces published ahead
 
+// What the merge kernel has to know about a sequence: where its own segments and
+// its group's lie on the partition's axis.
+struct __align__(16) SpRecord {
+  uint32_t cost, slot;  // axis and partial rows before the own segments
+  int keys;             // own keys (0: idle)
+  uint32_t chunk;       // axis per CTA
+  uint32_t pre_cost, pre_slot;
+  int pre_keys;         // 0: no prefix
+  int first, sequences; // of the group
+  int pad[3];
+};
+
 struct SpParams {
   const int32_t *prefix_table, *prefix_lens, *group_starts, *block_table, *seq_lens;
   __nv_bfloat16 *out;
@@ -69,14 +81,13 @@ struct SpParams {
   uint32_t *status;
   float *part_o;   // unnormalised outputs, [D / 4][rows] float4 per piece and row tile
   float2 *part_ml; // maximum (base-2 units) and sum of every row of a partial
-  uint4 *plan;     // [num_groups + B] for the merge kernel: cost base, partial rows
-                   // before, keys (0 without rows), and a sequence's group or a group's first sequence
-  uint32_t *total; // length of the axis
+  SpRecord *plan;  // [B], for the merge kernel
   int B, n_q, H_q, H_kv, group, num_pages, num_groups, max_prefix_pages, max_pages;
   int tokens_per_tile;  // floor(128 / group), at least 16
   uint32_t tile_magic;
   int oob_row;          // a tensor-map row beyond the pool: loads as zeros
   int G;                // CTAs of the split kernel
+  float per_cta;        // 1 / G
   float scale_log2;
 };
 
@@ -110,14 +121,20 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
   return x;
 }
 
-// The axis of length Tot in ranges of `chunk`, one per CTA (the last ones shorter
-// or empty: the longest is what counts).
-struct SpCut {
-  uint32_t Tot, chunk;
-  __device__ __forceinline__ SpCut(uint32_t tot, int G) : Tot(tot), chunk((tot + G - 1) / G) {}
-  __device__ __forceinline__ uint32_t begin(uint32_t c) const { return c * chunk < Tot ? c * chunk : Tot; }
-  __device__ __forceinline__ int owner(uint32_t x) const { return static_cast<int>(x / chunk); }
-};
+// The axis in ranges of `chunk`, one per CTA (the last ones shorter or empty: the
+// longest is what counts).  At least ceil(Tot / G), and hardly more.
+__device__ __forceinline__ uint32_t sp_chunk(const SpParams &p, uint32_t Tot) {
+  const uint32_t q = static_cast<uint32_t>(static_cast<float>(Tot) * p.per_cta + 0.999f);
+  return q + (q >> 20) + (Tot > q * static_cast<uint32_t>(p.G));
+}
+
+// a / b for quotients below 2^20
+__device__ __forceinline__ uint32_t sp_div(uint32_t a, uint32_t b) {
+  uint32_t q = static_cast<uint32_t>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
+  if (q * b > a) --q;
+  if ((q + 1u) * b <= a) ++q;
+  return q;
+}
 
 // First key tile of a segment (cost base `base`; 1 << dual per key tile) at or
 // behind position x of the axis.
@@ -138,6 +155,8 @@ struct SpItem {
   int n, t0, keys;  // key tiles t0 .. t0 + n - 1 of the segment's keys; n = 0: no more pieces
   int own, row, h;  // row of block_table (own) or prefix_table
   int dual, again;  // both streams read every tile; the keys are read again by other pieces
+  int two;          // the first key tile's weights go to P V as two bf16 terms
+  int pad;
   struct {
     int n, first, step;    // the stream's key tiles within the piece (n = 0: none)
     int token, rows;       // first query token and rows of its row tile
@@ -145,8 +164,9 @@ struct SpItem {
   } s[2];
 };
 
-// Bytes of shared memory behind the barriers for the lengths of all entities.
-__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) { return 4 * (B + 2 * num_groups + 1); }
+// Bytes of shared memory behind the barriers: lengths of all entities, the groups'
+// first sequences, costs and partial rows.
+__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) { return 4 * (B + 4 * num_groups + 1); }
 
 template <int D, int STAGES>
 struct SpSmem {
@@ -239,33 +259,24 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     prefetch_tensormap(&tmap_q_own);
     s_misc[1] = 0;
   }
+  __syncthreads();
   grid_dependency_wait();
   grid_launch_dependents();
-  if (warp == kSpMmaWarp) {
-    tmem_alloc(smem_addr(s_misc), kSpTmemCols);
-    tmem_relinquish_alloc_permit();
-    tc_fence_before_sync();
-  }
-  // lengths of all entities, and the groups' first sequences
-  const int E = p.num_groups + p.B;
-  int *s_len = reinterpret_cast<int *>(smem + L::kPlanOffset), *s_start = s_len + E;
-  for (int e = tid; e < E; e += kSpThreads) {
-    const bool own = e >= p.num_groups;
-    int n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
-    if (!own) s_start[e] = p.group_starts[e];
-    const int least = own ? p.n_q : 0, most = (own ? p.max_pages : p.max_prefix_pages) * SF_PAGE_SIZE;
-    if ((n < least || n > most) && n != 0) {
-      set_status(p.status, SF_DEVICE_BAD_SEQLEN);
-      n = n < least ? least : most;
-    }
-    s_len[e] = n;
-  }
-  if (tid == 0) s_start[p.num_groups] = p.group_starts[p.num_groups];
-  __syncthreads();
-  tc_fence_after_sync();
-  const uint32_t tmem = static_cast<uint32_t>(s_misc[0]);
   SpItem *items = reinterpret_cast<SpItem *>(smem + L::kItemOffset);
   uint32_t seen = 0;  // pieces read
+  // tensor memory: allocated (behind the wait: a kernel that waits for its
+  // predecessor must not hold what that may need) by the first MMA warp
+  uint32_t tmem = 0;
+  if (warp < kSpCopyWarp) {
+    if (warp == kSpMmaWarp) {
+      tmem_alloc(smem_addr(s_misc), kSpTmemCols);
+      tmem_relinquish_alloc_permit();
+      tc_fence_before_sync();
+    }
+    named_bar_sync(1, 32 * kSpCopyWarp);
+    tc_fence_after_sync();
+    tmem = static_cast<uint32_t>(s_misc[0]);
+  }
   // The next piece; null behind the last one (or after a timeout).  The warp
   // gives the entry back with release_item.
   auto next_item = [&]() -> const SpItem * {
@@ -284,9 +295,29 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     // The CTA's pieces, published one after the other, each followed by the
     // copies of its Q tiles as soon as the streams' last Q K^T have read theirs.
     // ------------------------------------------------------------------
+    const int E = p.num_groups + p.B;
+    int *s_len = reinterpret_cast<int *>(smem + L::kPlanOffset), *s_start = s_len + E;
+    uint32_t *s_cost = reinterpret_cast<uint32_t *>(s_start + p.num_groups + 1), *s_slot = s_cost + p.num_groups;
     bool bad = false;
-    for (int g = lane; g <= p.num_groups; g += 32)
-      bad |= g == 0 ? s_start[0] != 0 : s_start[g] < s_start[g - 1] || (g == p.num_groups && s_start[g] != p.B);
+#pragma unroll 4
+    for (int e = lane; e <= E; e += 32) {
+      const bool own = e >= p.num_groups;
+      int n = 0, s = 0;
+      if (e < E) n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
+      if (e <= p.num_groups) s = p.group_starts[e];
+      const int least = own ? p.n_q : 0, most = (own ? p.max_pages : p.max_prefix_pages) * SF_PAGE_SIZE;
+      if ((n < least || n > most) && n != 0) {
+        set_status(p.status, SF_DEVICE_BAD_SEQLEN);
+        n = n < least ? least : most;
+      }
+      if (e < E) s_len[e] = n;
+      if (e <= p.num_groups) {
+        s_start[e] = s;
+        bad |= (e == 0 && s != 0) || (e == p.num_groups && s != p.B);
+      }
+    }
+    __syncwarp();
+    for (int g = lane; g < p.num_groups; g += 32) bad |= s_start[g + 1] < s_start[g];
     if (__any_sync(0xffffffffu, bad)) {  // malformed groups: no sequence has a prefix
       for (int g = lane; g <= p.num_groups; g += 32) s_start[g] = 0;
       if (lane == 0) set_status(p.status, SF_DEVICE_BAD_INDEX);
@@ -297,12 +328,20 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const int first = own ? e - p.num_groups : s_start[e];
       return sp_entity(p, own, first, own ? 1 : s_start[e + 1] - first, s_len[e]);
     };
+    auto group_of = [&](int b) -> int {  // the last group that starts at or before sequence b
+      int lo = 0, hi = p.num_groups;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_start[mid] <= b) lo = mid; else hi = mid;
+      }
+      return lo;
+    };
     uint32_t sum = 0;
     for (int e = lane; e < E; e += 32) sum += entity(e).head_cost;
-    const SpCut cut(__reduce_add_sync(0xffffffffu, sum) * p.H_kv, p.G);
+    const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum) * p.H_kv, chunk = sp_chunk(p, Tot);
     const uint32_t c = blockIdx.x;
-    const bool writes = c == gridDim.x - 1;  // this CTA leaves the plan for the merge kernel
-    const uint32_t at = cut.begin(c), end = cut.begin(c + 1);
+    const bool writes = c == gridDim.x - 1;  // this CTA (with the least to do) leaves the plan for the merge kernel
+    const uint32_t at = min(c * chunk, Tot), end = min(at + chunk, Tot);
     // the entity that position `at` lies in, with the costs and partial rows before it
     int e = E;
     uint32_t e_cost = 0, e_slot = 0, cost = 0, slot = 0;
@@ -328,25 +367,28 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         e_cost = __shfl_sync(0xffffffffu, before, l);
         e_slot = __shfl_sync(0xffffffffu, slots, l);
       }
-      if (writes && k < E) {
-        int other;
-        if (k < p.num_groups) {
-          other = s_start[k];
-        } else {
-          int lo = 0, hi = p.num_groups;  // the sequence's group: the last that starts at or before it
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (s_start[mid] <= k - p.num_groups) lo = mid + 1; else hi = mid;
-          }
-          other = lo - 1;
-        }
-        p.plan[k] = make_uint4(before, slots, x.head_cost ? static_cast<uint32_t>(x.keys) : 0u,
-                               static_cast<uint32_t>(other));
+      if (writes && k < p.num_groups) {
+        s_cost[k] = before;
+        s_slot[k] = slots;
+      }
+      __syncwarp();
+      if (writes && k >= p.num_groups && k < E) {
+        SpRecord rec;
+        const int g = group_of(k - p.num_groups);
+        rec.cost = before;
+        rec.slot = slots;
+        rec.keys = x.keys;
+        rec.chunk = chunk;
+        rec.pre_cost = s_cost[g];
+        rec.pre_slot = s_slot[g];
+        rec.first = s_start[g];
+        rec.sequences = s_start[g + 1] - rec.first;
+        rec.pre_keys = rec.sequences > 0 ? s_len[g] : 0;
+        p.plan[k - p.num_groups] = rec;
       }
       cost += __shfl_sync(0xffffffffu, ci, 31);
       slot += __shfl_sync(0xffffffffu, si, 31);
     }
-    if (writes && lane == 0) *p.total = cut.Tot;
     SpEntity x{};
     int h = 0, pair = 0;
     uint32_t base = 0;
@@ -354,8 +396,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     if (e < E) {
       x = entity(e);
       const uint32_t in = at - e_cost;
-      h = static_cast<int>(in / x.head_cost);
-      pair = x.pairs > 1 ? static_cast<int>((in - h * x.head_cost) / x.pair_cost()) : 0;
+      h = static_cast<int>(sp_div(in, x.head_cost));
+      pair = x.pairs > 1 ? static_cast<int>(sp_div(in - h * x.head_cost, x.pair_cost())) : 0;
       base = e_cost + h * x.head_cost + pair * x.pair_cost();
       slot = e_slot + (h * x.pairs + pair) * x.slot_rows + 2u * kSpTile * c;
     }
@@ -383,6 +425,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           it.h = h;
           it.dual = dual;
           it.again = x.pairs > 1;
+          // Rows that see few keys besides this segment's need more of its weights
+          // than 8 bits: over many keys the roundings average out.
+          int others = 0;
+          if (own) {
+            const int g = group_of(it.row);
+            others = s_start[g + 1] > s_start[g] ? s_len[g] : 0;
+          }
+          it.two = it.t0 == 0 && (own ? others : x.keys) < kSpTile;
           const int rows0 = sp_rows(p, x, 2 * pair), tok0 = x.token0 + 2 * pair * p.tokens_per_tile;
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
@@ -473,7 +523,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const uint64_t policy = item->again ? again : once;
       release_item();
       int ids = kBeyondEnd;
-      for (int it = 0; it < n && ok; ++it) {
+      for (int it = 0; it < n; ++it) {
         if ((it & 3) == 0) {  // page ids of the next four tiles, one a lane
           const int lt = it + (lane >> 3), page = (t0 + lt) * kSpTilePages + (lane & 7);
           ids = lt < n && page * SF_PAGE_SIZE < keys ? table[page] : kBeyondEnd;
@@ -487,24 +537,30 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             row = (phys * p.H_kv + h) * SF_PAGE_SIZE;
           }
         }
-        for (int kv = 0; kv < 2 && ok; ++kv, ++pos) {
+        int rows[kSpTilePages];  // the same in every lane: the copies' operands are warp-uniform
+#pragma unroll
+        for (int j = 0; j < kSpTilePages; ++j) rows[j] = __shfl_sync(0xffffffffu, row, j);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++pos) {
           const uint32_t slot = pos % STAGES;
-          if (pos >= STAGES) ok = wait(bar(EMPTY + slot), (pos / STAGES - 1) & 1u);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(bar(FULL + slot), L::kTileBytes);
-          __syncwarp();
-          if (lane < kSpTilePages) {
-            const uint32_t dst = ring + slot * L::kTileBytes + lane * kPageBytes;
-            if (kv == 0) {
-              if constexpr (HALVES == 2) tma_load_4d(dst, &tmap_k, 0, 0, 0, row / 8, bar(FULL + slot), policy);
-              else tma_load_2d(dst, &tmap_k, 0, row, bar(FULL + slot), policy);
-            } else {
-              if constexpr (HALVES == 2) tma_load_3d(dst, &tmap_v, 0, row, 0, bar(FULL + slot), policy);
-              else tma_load_2d(dst, &tmap_v, 0, row, bar(FULL + slot), policy);
+          if (pos >= STAGES && !(ok = wait(bar(EMPTY + slot), (pos / STAGES - 1) & 1u))) break;
+          const uint32_t dst = ring + slot * L::kTileBytes, full = bar(FULL + slot);
+          if (elect_one()) {
+            mbar_arrive_expect_tx(full, L::kTileBytes);
+#pragma unroll
+            for (int j = 0; j < kSpTilePages; ++j) {
+              if (kv == 0) {
+                if constexpr (HALVES == 2) tma_load_4d(dst + j * kPageBytes, &tmap_k, 0, 0, 0, rows[j] / 8, full, policy);
+                else tma_load_2d(dst + j * kPageBytes, &tmap_k, 0, rows[j], full, policy);
+              } else {
+                if constexpr (HALVES == 2) tma_load_3d(dst + j * kPageBytes, &tmap_v, 0, rows[j], 0, full, policy);
+                else tma_load_2d(dst + j * kPageBytes, &tmap_v, 0, rows[j], full, policy);
+              }
             }
           }
           __syncwarp();
         }
+        if (!ok) break;
       }
     }
     if (*s_abort && lane == 0) {
@@ -545,7 +601,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const int step = __shfl_sync(0xffffffffu, item->s[s].step, 0);
       const bool dual = __shfl_sync(0xffffffffu, item->dual, 0) != 0;
       int mine = n > 0 ? __shfl_sync(0xffffffffu, item->s[s].first, 0) : total;  // the stream's next key tile
-      bool two = __shfl_sync(0xffffffffu, item->t0 + mine, 0) == 0;  // the segment's first key tile: P_hi + P_lo
+      bool two = __shfl_sync(0xffffffffu, item->two, 0) != 0 && mine == 0;  // P_hi + P_lo on the segment's first key tile
       int left = n;
       release_item();
       for (int t = 0; t < total; ++t, pos += 2) {
@@ -632,6 +688,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       if (!item) break;
       const int n = item->s[s].n, step = item->s[s].step, rows = item->s[s].rows, keys = item->keys;
       const uint32_t slot0 = item->s[s].slot;
+      bool two = item->two && item->s[s].first == 0;
       uint32_t ring_tile = base + item->s[s].first;
       int tile_pos = (item->t0 + item->s[s].first) * kSpTile;  // position of the tile's first key
       base += item->n;
@@ -674,6 +731,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           for (int i = 0; i < 128; ++i)
             if (tile_pos + i > lim) sv[i] = __float_as_uint(-INFINITY);
         }
+        float mu = ref == -INFINITY ? 0.f : ref;
         float a0 = __uint_as_float(sv[0]), a1 = __uint_as_float(sv[1]), a2 = __uint_as_float(sv[2]),
               a3 = __uint_as_float(sv[3]);
 #pragma unroll
@@ -702,9 +760,9 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             tmem_st_32x32b_x16(to + ch * 16, ov);
           }
         }
-        const float mu = ref == -INFINITY ? 0.f : ref;
+        mu = ref == -INFINITY ? 0.f : ref;
         float sum0 = 0.f, sum1 = 0.f;
-        if (tile_pos != 0) {
+        if (!two) {
           const unsigned long long scale2 = sp_pair(p.scale_log2, p.scale_log2), mu2 = sp_pair(-mu, -mu);
           unsigned long long sum = 0ull;
 #pragma unroll
@@ -729,7 +787,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
           sp_unpair(sum, sum0, sum1);
         } else {
-          // A segment's first key tile: what P's rounding to bf16 left goes to
+          // A first key tile with two terms: what P's rounding to bf16 left goes to
           // columns [64, 128) as a second term.  The scores are read again, 64 at a
           // time, so that the two terms need no more registers than the scores do
           // above.
@@ -769,9 +827,10 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          if (tile_pos == 0) mbar_arrive(bar(PFULL + 2 * s));
+          if (two) mbar_arrive(bar(PFULL + 2 * s));
           mbar_arrive(bar(PFULL + 2 * s + 1));
         }
+        two = false;
       }
       if (ok) ok = wwait(bar(ODONE + s), jobs & 1u);
       if (!ok) break;
@@ -842,19 +901,20 @@ struct SpJoin {
 
 // Appends the first partial rows of a row tile's partials of one segment to
 // list[n ..]; returns the new length.  A whole warp calls it.
-__device__ __forceinline__ int sp_list(const SpCut &cut, const SpParams &p, const uint4 &rec, const SpEntity &x, int h,
-                                       int tile, uint32_t *list, int n) {
+__device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32_t cost, uint32_t slot, const SpEntity &x,
+                                       int h, int tile, uint32_t *list, int n) {
   if (x.head_cost == 0) return n;
   const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
-  const uint32_t base = rec.x + h * x.head_cost + pair * x.pair_cost();
-  const uint32_t slot = rec.y + (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
+  const uint32_t base = cost + h * x.head_cost + pair * x.pair_cost();
+  slot += (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
   const int rows = sp_rows(p, x, tile);
-  const int last = cut.owner(base + kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual) - 1);
-  for (int c0 = cut.owner(base); c0 <= last; c0 += 32) {
+  const int last = static_cast<int>(sp_div(base + kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual) - 1, chunk));
+  for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
     int k = 0;
     if (c <= last) {
-      k = sp_tile_at(cut.begin(c + 1), base, dual, x.key_tiles) - sp_tile_at(cut.begin(c), base, dual, x.key_tiles);
+      // (a range's end may lie past the axis' end: no tile does)
+      k = sp_tile_at((c + 1) * chunk, base, dual, x.key_tiles) - sp_tile_at(c * chunk, base, dual, x.key_tiles);
       k = dual ? min(k, 1) : min(k, 2);  // partials of this piece
     }
     const unsigned one = __ballot_sync(0xffffffffu, k > 0), two = __ballot_sync(0xffffffffu, k > 1);
@@ -874,28 +934,25 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
   __shared__ int s_pre[2], s_all[2], s_rows[2];  // list lengths (prefix, all) and rows of the prefix's row tiles
   const int tid = threadIdx.x, warp = tid >> 5;
   const int b = blockIdx.x / p.H_kv, h = blockIdx.x - b * p.H_kv;
+  const int R = p.n_q * p.group, per = R * C4;
   grid_dependency_wait();
   grid_launch_dependents();
-  const SpCut cut(*p.total, p.G);
-  const uint4 rec = p.plan[p.num_groups + b];
-  const int keys = static_cast<int>(rec.z), R = p.n_q * p.group, per = R * C4;
+  const SpRecord rec = p.plan[b];
   int tok0 = 0, tile0 = 0;  // the sequence's first token within its group's, and that token's row tile
-  if (keys > 0) {
-    const int g = static_cast<int>(rec.w);
-    const uint4 pre = p.plan[g];
-    const int first = static_cast<int>(pre.w);
-    tok0 = (b - first) * p.n_q;
+  if (rec.keys > 0) {
+    tok0 = (b - rec.first) * p.n_q;
     tile0 = sp_tiles(p, tok0);
     if (warp < 2) {
-      const int next = g + 1 < p.num_groups ? static_cast<int>(p.plan[g + 1].w) : p.B;
-      const SpEntity px = sp_entity(p, false, first, next - first, static_cast<int>(pre.z));
       const int tile = tile0 + warp;
       int n = 0, rows = 0;
-      if (tile < px.tiles) {
-        n = sp_list(cut, p, pre, px, h, tile, s_list[warp], 0);
-        rows = sp_rows(p, px, tile);
+      if (rec.pre_keys > 0) {
+        const SpEntity px = sp_entity(p, false, rec.first, rec.sequences, rec.pre_keys);
+        if (tile < px.tiles) {
+          n = sp_list(rec.chunk, p, rec.pre_cost, rec.pre_slot, px, h, tile, s_list[warp], 0);
+          rows = sp_rows(p, px, tile);
+        }
       }
-      const int all = sp_list(cut, p, rec, sp_entity(p, true, b, 1, keys), h, 0, s_list[warp], n);
+      const int all = sp_list(rec.chunk, p, rec.cost, rec.slot, sp_entity(p, true, b, 1, rec.keys), h, 0, s_list[warp], n);
       s_pre[warp] = n;
       s_all[warp] = all;
       s_rows[warp] = rows;
@@ -910,7 +967,7 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     jn.L = 0.f;
     jn.acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float inv = 0.f;
-    if (keys > 0) {
+    if (rec.keys > 0) {
       const int sel = (tok0 + i >= (tile0 + 1) * p.tokens_per_tile);
       const int row_pre = (tok0 + i - (tile0 + sel) * p.tokens_per_tile) * p.group + j;
       const int pre = s_pre[sel], all = s_all[sel], rows_pre = s_rows[sel];
@@ -937,7 +994,7 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     packed.x = pack_bf16x2(jn.acc.x * inv, jn.acc.y * inv);
     packed.y = pack_bf16x2(jn.acc.z * inv, jn.acc.w * inv);
     *reinterpret_cast<uint2 *>(p.out + row * D + 4 * c4) = packed;
-    if (p.lse && c4 == 0) p.lse[row] = keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
+    if (p.lse && c4 == 0) p.lse[row] = rec.keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
   }
 }
 
@@ -984,14 +1041,13 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
 }
 
 struct SpLayout {
-  size_t total_off, plan_off, ml_off, o_off, total;
+  size_t plan_off, ml_off, o_off, total;
 };
 
-static SpLayout sp_layout(const SpBounds &b, int D, int B, int num_groups) {
+static SpLayout sp_layout(const SpBounds &b, int D, int B) {
   SpLayout l;
-  l.total_off = 128;
   l.plan_off = 256;
-  l.ml_off = round_up(l.plan_off + static_cast<size_t>(B + num_groups) * sizeof(uint4), 256);
+  l.ml_off = round_up(l.plan_off + static_cast<size_t>(B) * sizeof(SpRecord), 256);
   l.o_off = round_up(l.ml_off + static_cast<size_t>(b.rows) * sizeof(float2), 256);
   l.total = l.o_off + static_cast<size_t>(b.rows) * D * sizeof(float);
   return l;
@@ -1081,8 +1137,7 @@ size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_
   if (check_sp_shapes(B, n_q, H_q, H_kv, head_dim, num_groups, max_prefix_pages, max_pages_per_seq, page_size) != SF_OK ||
       sp_grid(&G) != SF_OK)
     return 0;
-  return sp_layout(sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G), head_dim, B,
-                   num_groups)
+  return sp_layout(sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G), head_dim, B)
       .total;
 }
 
@@ -1117,7 +1172,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   const SpBounds bounds = sp_bounds(B, n_q, H_q, H_kv, num_groups, max_prefix_pages, max_pages_per_seq, G);
   if (bounds.cost >= (1LL << 31) || bounds.rows >= (1LL << 31))
     return fail(SF_ERR_UNSUPPORTED, "up to %lld tiles and %lld partial rows (limits 2^31)", bounds.cost, bounds.rows);
-  const SpLayout lay = sp_layout(bounds, head_dim, B, num_groups);
+  const SpLayout lay = sp_layout(bounds, head_dim, B);
   if (workspace_bytes < lay.total)
     return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, lay.total);
   if ((st = sp_setup(dev.ordinal)) != SF_OK) return st;
@@ -1133,8 +1188,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.out = static_cast<__nv_bfloat16 *>(out);
   p.lse = lse;
   p.status = reinterpret_cast<uint32_t *>(ws);
-  p.total = reinterpret_cast<uint32_t *>(ws + lay.total_off);
-  p.plan = reinterpret_cast<uint4 *>(ws + lay.plan_off);
+  p.plan = reinterpret_cast<SpRecord *>(ws + lay.plan_off);
   p.part_ml = reinterpret_cast<float2 *>(ws + lay.ml_off);
   p.part_o = reinterpret_cast<float *>(ws + lay.o_off);
   p.B = B;
@@ -1150,6 +1204,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.tile_magic = static_cast<uint32_t>(((1ull << 32) + p.tokens_per_tile - 1) / p.tokens_per_tile);
   p.oob_row = static_cast<int>(rows);
   p.G = G;
+  p.per_cta = 1.f / static_cast<float>(G);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   p.scale_log2 = scale * 1.4426950408889634f;
   CUtensorMap m[4];
