@@ -56,10 +56,11 @@ constexpr uint32_t kSpTmemCols = 512;
 constexpr float kSpRescaleLog2 = 8.f;
 constexpr int kSpMergeThreads = 256;
 constexpr int kSpSmemMax = 227 * 1024;
-// Cost of a segment on the partition's axis, in key tiles of one row tile: one
-// for each of its row tiles' key tiles, and kSpCostSeg for itself (its Q copy,
-// pipeline start and epilogue).
-constexpr uint32_t kSpCostSeg = 2;
+// Cost of a segment on the partition's axis: kSpCostTile[dual] for each of its key
+// tiles (one row tile, or two), and kSpCostSeg for itself (its Q copy, pipeline
+// start and epilogue).  Measured: 0.42 us a unit.
+constexpr uint32_t kSpCostSeg = 3, kSpCostOne = 3, kSpCostTwo = 4;
+constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
 constexpr int kSpItems = 4;      // pieces published ahead
 
 // What the merge kernel has to know about a sequence: where its own segments and
@@ -98,7 +99,7 @@ struct SpEntity {
   int keys, token0, tokens, tiles, pairs, key_tiles;
   uint32_t head_cost;  // per KV head
   uint32_t slot_rows;  // partial rows of one piece
-  __device__ __forceinline__ uint32_t pair_cost() const { return kSpCostSeg + 2u * static_cast<uint32_t>(key_tiles); }
+  __device__ __forceinline__ uint32_t pair_cost() const { return kSpCostSeg + kSpCostTwo * static_cast<uint32_t>(key_tiles); }
 };
 
 // n / tokens_per_tile for n < 2^25 (tile_magic = ceil(2^32 / tokens_per_tile))
@@ -115,7 +116,8 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
   x.pairs = (x.tiles + 1) >> 1;
   x.key_tiles = (keys + kSpTile - 1) / kSpTile;
   x.head_cost = keys > 0 ? static_cast<uint32_t>(x.pairs) * kSpCostSeg +
-                               static_cast<uint32_t>(x.key_tiles) * static_cast<uint32_t>(x.tiles)
+                               static_cast<uint32_t>(x.key_tiles) *
+                                   (kSpCostTwo * static_cast<uint32_t>(x.tiles >> 1) + kSpCostOne * (x.tiles & 1))
                          : 0u;
   x.slot_rows = x.tiles > 1 ? 2u * kSpTile : 2u * static_cast<uint32_t>(x.tokens * p.group);
   return x;
@@ -136,13 +138,17 @@ __device__ __forceinline__ uint32_t sp_div(uint32_t a, uint32_t b) {
   return q;
 }
 
-// First key tile of a segment (cost base `base`; 1 << dual per key tile) at or
-// behind position x of the axis.
+// First key tile of a segment at or behind position x of the axis.
 __device__ __forceinline__ int sp_tile_at(uint32_t x, uint32_t base, int dual, int key_tiles) {
   const uint32_t b = base + kSpCostSeg;
   if (x <= b) return 0;
-  const uint32_t t = (x - b + dual) >> dual;
+  const uint32_t t = dual ? (x - b + kSpCostTwo - 1) / kSpCostTwo : (x - b + kSpCostOne - 1) / kSpCostOne;
   return t < static_cast<uint32_t>(key_tiles) ? static_cast<int>(t) : key_tiles;
+}
+
+// Length of a segment on the axis.
+__device__ __forceinline__ uint32_t sp_cost(int dual, int key_tiles) {
+  return kSpCostSeg + (dual ? kSpCostTwo : kSpCostOne) * static_cast<uint32_t>(key_tiles);
 }
 
 __device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int tile) {
@@ -461,7 +467,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           if (!dual && it.n == 1) turn ^= 1;
         }
         // the next segment
-        base += kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual);
+        base += sp_cost(dual, x.key_tiles);
         slot += x.slot_rows;
         if (++pair == x.pairs) {
           pair = 0;
@@ -588,6 +594,23 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     };
     uint32_t pos = 0, tiles = 0, jobs = 0, turns = 0;  // pos: ring slots passed
     bool ok = true;
+    // one thread issues: Q K^T of a tile ..
+    auto issue_qk = [&](uint64_t k0) {
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        tc_mma_ss(ts, q0 + (((kk >> 2) * kHalfTileBytes + (kk & 3) * 32) >> 4),
+                  k0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), kIdescQK, kk > 0 ? 1u : 0u);
+      tc_commit(bar(SFULL + s));
+    };
+    // .. and P V of a part of a tile's keys (`more`: not the job's first tile)
+    auto issue_pv = [&](uint64_t v0, int part, uint32_t more, bool two) {
+#pragma unroll
+      for (int j = part ? kSpFirstPages : 0; j < (part ? kSpTilePages : kSpFirstPages); ++j) {
+        const uint64_t v = v0 + (j * kPageBytes >> 4);
+        tc_mma_ts(to, ts + j * 8, v, kIdescPV, j == 0 ? more : 1u);
+        if (two) tc_mma_ts(to, ts + 64 + j * 8, v, kIdescPV, 1u);
+      }
+    };
     // stream 1's i-th turn follows stream 0's, stream 0's next follows that
     auto take_turn = [&]() -> bool {
       const bool w = s == 0 ? (turns == 0 || wait(bar(TURN), (turns - 1) & 1u)) : wait(bar(TURN + 1), turns & 1u);
@@ -603,6 +626,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       int mine = n > 0 ? __shfl_sync(0xffffffffu, item->s[s].first, 0) : total;  // the stream's next key tile
       bool two = __shfl_sync(0xffffffffu, item->two, 0) != 0 && mine == 0;  // P_hi + P_lo on the segment's first key tile
       int left = n;
+      bool ahead = false;  // the tile's Q K^T is issued already
       release_item();
       for (int t = 0; t < total; ++t, pos += 2) {
         uint32_t slot = pos % STAGES;
@@ -625,43 +649,48 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           ++jobs;
           if (dual && !(ok = take_turn())) break;
         }
-        tc_fence_after_sync();
-        const uint64_t k0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            tc_mma_ss(ts, q0 + (((kk >> 2) * kHalfTileBytes + (kk & 3) * 32) >> 4),
-                      k0 + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), kIdescQK, kk > 0 ? 1u : 0u);
-          tc_commit(bar(SFULL + s));
-          tc_commit(bar(EMPTY + slot));
-          if (last) tc_commit(bar(QEMPTY + s));
-          if (dual) mbar_arrive(bar(TURN + 1 - s));
-        }
-        __syncwarp();
-        slot = (pos + 1) % STAGES;
-        if (!(ok = wait(bar(FULL + slot), ((pos + 1) / STAGES) & 1u))) break;
-        const uint64_t v0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (!(ok = wait(bar(PFULL + 2 * s + half), tiles & 1u))) break;
-          if (half == 0 && dual && !(ok = take_turn())) break;
+        if (!ahead) {
           tc_fence_after_sync();
+          const uint64_t k0 = smem_desc_sw128(ring + slot * L::kTileBytes, 16, kKSbo);
           if (elect_one()) {
-#pragma unroll
-            for (int j = 0; j < kSpTilePages; ++j) {
-              if (j / (kSpTilePages / 2) != half) continue;
-              tc_mma_ts(to, ts + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, !first || j > 0 ? 1u : 0u);
-              if (two) tc_mma_ts(to, ts + 64 + j * 8, v0 + (j * kPageBytes >> 4), kIdescPV, 1u);
-            }
-            if (half == 1) {
-              tc_commit(bar(EMPTY + slot));
-              if (last) tc_commit(bar(ODONE + s));
-              if (last && dual) mbar_arrive(bar(TURN + 1 - s));
-            }
+            issue_qk(k0);
+            tc_commit(bar(EMPTY + slot));
+            if (last) tc_commit(bar(QEMPTY + s));
+            if (dual) mbar_arrive(bar(TURN + 1 - s));
           }
           __syncwarp();
         }
-        if (!ok) break;
+        ahead = false;
+        slot = (pos + 1) % STAGES;
+        if (!(ok = wait(bar(FULL + slot), ((pos + 1) / STAGES) & 1u))) break;
+        const uint64_t v0 = smem_desc_sw128(ring + slot * L::kTileBytes, kPageHalfBytes, 1024);
+        const uint32_t more = first ? 0u : 1u;
+        if (!(ok = wait(bar(PFULL + 2 * s), tiles & 1u))) break;
+        if (dual && !(ok = take_turn())) break;
+        tc_fence_after_sync();
+        if (elect_one()) issue_pv(v0, 0, more, two);
+        __syncwarp();
+        // of two row tiles the next Q K^T goes along where its K tile is there
+        const uint32_t slot_n = (pos + 2) % STAGES;
+        if (dual && !last) ahead = mbar_test_wait(bar(FULL + slot_n), ((pos + 2) / STAGES) & 1u);
+        ahead = __all_sync(0xffffffffu, ahead);
+        const bool last_n = left == 1;
+        const uint64_t kn = smem_desc_sw128(ring + slot_n * L::kTileBytes, 16, kKSbo);
+        if (!(ok = wait(bar(PFULL + 2 * s + 1), tiles & 1u))) break;
+        tc_fence_after_sync();
+        if (elect_one()) {
+          issue_pv(v0, 1, more, two);
+          tc_commit(bar(EMPTY + slot));
+          if (last) tc_commit(bar(ODONE + s));
+          if (last && dual) mbar_arrive(bar(TURN + 1 - s));
+          if (ahead) {
+            issue_qk(kn);
+            tc_commit(bar(EMPTY + slot_n));
+            if (last_n) tc_commit(bar(QEMPTY + s));
+            mbar_arrive(bar(TURN + 1 - s));
+          }
+        }
+        __syncwarp();
         two = false;
         ++tiles;
       }
@@ -908,7 +937,7 @@ __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32
   const uint32_t base = cost + h * x.head_cost + pair * x.pair_cost();
   slot += (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
   const int rows = sp_rows(p, x, tile);
-  const int last = static_cast<int>(sp_div(base + kSpCostSeg + (static_cast<uint32_t>(x.key_tiles) << dual) - 1, chunk));
+  const int last = static_cast<int>(sp_div(base + sp_cost(dual, x.key_tiles) - 1, chunk));
   for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
     int k = 0;
@@ -1035,7 +1064,7 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
   // at most half of that plus one pairs, of at most 2 * kSpTile partial rows each
   const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
   SpBounds b;
-  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles + B * (kSpCostSeg + own_tiles));
+  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostOne + B * (kSpCostSeg + own_tiles * kSpCostOne));
   b.rows = H_kv * (pairs * 2 * kSpTile + 2 * tokens * group) + 2LL * kSpTile * G;
   return b;
 }
