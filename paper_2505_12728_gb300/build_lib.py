@@ -5,6 +5,10 @@ Each .cu file under csrc/ is compiled separately (in parallel) with
 with the static CUDA runtime into ``_build/libspecflash_verify.so``, so the
 library needs only the NVIDIA driver at run time.  Rebuilds only when a
 source or header is newer than the library.
+
+csrc/layer_calls.cpp (the decoder-layer operators' calls from Python without the
+detour through ctypes) is compiled beside it with g++ and torch's headers into
+``_build/_layer_calls.so``; where that fails, the binding does without.
 """
 from __future__ import annotations
 
@@ -13,6 +17,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -21,6 +26,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libspecflash_verify.so")
+CALLS_SOURCE = os.path.join(CSRC, "layer_calls.cpp")
+CALLS = os.path.join(BUILD, "_layer_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2",
               "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]
@@ -49,10 +56,41 @@ def up_to_date() -> bool:
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
+def build_calls(force: bool = False) -> str | None:
+    """Compile _layer_calls.so against the installed torch; its path, or None where
+    that is not possible (the reason goes to stderr)."""
+    header = os.path.join(INCLUDE, "specflash_verify.h")
+    if not force and os.path.exists(CALLS) and \
+            os.path.getmtime(CALLS) >= max(os.path.getmtime(CALLS_SOURCE), os.path.getmtime(header)):
+        return CALLS
+    try:
+        import torch
+        root = os.path.join(os.path.dirname(torch.__file__))
+        inc = os.path.join(root, "include")
+        lib = os.path.join(root, "lib")
+        cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+        tmp = CALLS + f".{os.getpid()}.tmp"
+        cmd = ["g++", "-O2", "-shared", "-fPIC", "-std=c++17", "-fvisibility=hidden",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+               "-I", sysconfig.get_paths()["include"], "-isystem", cuda, "-isystem", inc,
+               "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), CALLS_SOURCE, "-o", tmp,
+               "-L", lib, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{lib}"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except (ImportError, AttributeError, OSError) as e:
+        print(f"_layer_calls is not built: {e}", file=sys.stderr)
+        return None
+    if r.returncode != 0:
+        print(f"_layer_calls is not built:\n{r.stderr[-2000:]}", file=sys.stderr)
+        return None
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    if not force and up_to_date():
-        return LIB
     os.makedirs(BUILD, exist_ok=True)
+    if not force and up_to_date():
+        build_calls()
+        return LIB
     nvcc = _nvcc()
 
     def compile_one(src):
@@ -68,7 +106,9 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:
+        calls = ex.submit(build_calls, force)
         objs = list(ex.map(compile_one, sources()))
+        calls.result()
     tmp = LIB + f".{os.getpid()}.tmp"
     cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

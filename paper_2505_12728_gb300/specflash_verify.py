@@ -10,6 +10,7 @@ first call raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import threading
 
@@ -42,6 +43,7 @@ EXPORTED_SYMBOLS = (
 
 _lock = threading.Lock()
 _lib = None
+_calls = None  # csrc/layer_calls.cpp, once the library is loaded (and if it was built)
 
 
 class SFError(RuntimeError):
@@ -131,8 +133,26 @@ def load_library(path: str | None = None):
         lib.sf_shared_prefix_attention.argtypes = [P, P, P, P, P, P, P, P, I, I, I, I, I, I, I, I,
                                                    I, I, F, P, P, P, S, P]
         lib.sf_shared_prefix_attention.restype = I
+        _load_calls(lib)
         _lib = lib
         return lib
+
+
+def _load_calls(lib):
+    """The decoder-layer operators' direct calls, where they were built for this
+    torch."""
+    global _calls
+    if not os.path.exists(build_lib.CALLS):
+        return
+    spec = importlib.util.spec_from_file_location("_layer_calls", build_lib.CALLS)
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:  # built for another torch: build() has not run since
+        return
+    module.set_entries(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.sf_add_rms_norm, lib.sf_kv_append, lib.sf_shared_prefix_attention)))
+    _calls = module
 
 
 def _check(status: int):
@@ -550,9 +570,10 @@ def visual_compress(queries, features, *, out=None, workspace=None, stream=None)
 # --------------------------------------------------------------------------- #
 # the decoder layer around the attention                                      #
 # --------------------------------------------------------------------------- #
-# Host time is most of a small call here, and every tensor's checks are on it: a
-# well-formed tensor takes one expression (no call of its own where that is
-# possible), and strides are asked for only where a tensor is not contiguous.
+# Host time is most of a small call here.  A call that brings its outputs and its
+# workspace goes through csrc/layer_calls.cpp, which looks at the tensors directly;
+# where that finds anything missing or not as it should be (or was not built) the
+# functions below go through the arguments themselves.
 _Tensor, _BF16, _F32, _E4M3 = torch.Tensor, torch.bfloat16, torch.float32, torch.float8_e4m3fn
 _I32, _F64 = torch.int32, torch.float64
 
@@ -612,6 +633,12 @@ def add_rms_norm(x, weight, residual=None, *, eps=1e-6, out_dtype=torch.bfloat16
     scales, one per row (group 0) or per 128 columns (group 128).
     Returns (out [T][d], residual_out like x or None, scales [T][groups] or
     None).  residual_out may be the residual itself."""
+    if _calls is not None and out is not None and stream is None:
+        status = _calls.add_rms_norm(x, weight, residual, eps, group, out, residual_out, scales)
+        if status is not None:
+            if status:
+                _check(status)
+            return out, residual_out, scales
     if not isinstance(x, _Tensor):
         raise TypeError("x must be a torch.Tensor")
     shape, kind = x.shape, x.dtype
@@ -676,6 +703,13 @@ def kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_l
     and seq_lens (counting the new rows) as for verify_attention; row_starts
     int32 [B + 1] for sequences of different numbers of new rows (None: T / B
     each).  Returns q_out bf16 [T][H_q][d] or None."""
+    if _calls is not None and workspace is not None and stream is None and (q is None) == (q_out is None):
+        status = _calls.kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_lens, axis,
+                                  row_starts, interleaved, amplitude, q_out, workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return q_out
     if not isinstance(k, _Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor [T][H_kv][d]")
     shape, kind = k.shape, k.dtype
@@ -707,19 +741,10 @@ def kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_l
     num_pages, heads, page, wide = cache
     if heads != H_kv or wide != d:
         raise ValueError(f"k_cache has shape {tuple(cache)}, expected (pages, {H_kv}, 16, {d})")
-    try:
-        fine = (k_cache.dtype is _BF16 and v_cache.dtype is _BF16 and block_table.dtype is _I32 and seq_lens.dtype is _I32
-                and k_cache.is_cuda and v_cache.is_cuda and block_table.is_cuda and seq_lens.is_cuda
-                and k_cache.is_contiguous() and v_cache.is_contiguous() and block_table.is_contiguous()
-                and seq_lens.is_contiguous() and v_cache.shape == cache and seq_lens.dim() == 1
-                and seq_lens.numel() == B)
-    except AttributeError:
-        fine = False
-    if not fine:
-        _need(k_cache, "k_cache", _BF16)
-        _need(v_cache, "v_cache", _BF16, cache)
-        _need(block_table, "block_table", _I32)
-        _need(seq_lens, "seq_lens", _I32, (B,))
+    _need(k_cache, "k_cache", _BF16)
+    _need(v_cache, "v_cache", _BF16, cache)
+    _need(block_table, "block_table", _I32)
+    _need(seq_lens, "seq_lens", _I32, (B,))
     axes = pairs = 0
     if inv_freq is not None:
         _need(inv_freq, "inv_freq", _F64)
@@ -769,6 +794,14 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     block_table int32 [B][pages] and seq_lens int32 [B] (0: idle slot) describe
     each sequence's own tokens, draft rows included.  Returns (out bf16
     [B][n_q][H_q][d], lse fp32 [B][n_q][H_q] or None)."""
+    if _calls is not None and out is not None and workspace is not None and stream is None and (
+            lse is not None or not with_lse):
+        status = _calls.shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_starts,
+                                                block_table, seq_lens, softmax_scale, out, lse, workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return out, lse
     if not isinstance(q, _Tensor) or q.dim() != 4:
         raise ValueError("q must be a tensor [B][n_q][H_q][d]")
     B, n_q, H_q, d = shape = q.shape
@@ -779,38 +812,20 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     if d2 != d:
         # the library sizes the caches' tensor maps from q's head_dim
         raise ValueError("head_dim of q and caches differ")
-    try:
-        fine = (q.dtype is _BF16 and k_cache.dtype is _BF16 and v_cache.dtype is _BF16 and prefix_table.dtype is _I32
-                and block_table.dtype is _I32 and q.is_cuda and k_cache.is_cuda and v_cache.is_cuda
-                and prefix_table.is_cuda and block_table.is_cuda and q.is_contiguous() and k_cache.is_contiguous()
-                and v_cache.is_contiguous() and prefix_table.is_contiguous() and block_table.is_contiguous()
-                and v_cache.shape == cache)
-    except AttributeError:
-        fine = False
-    if not fine:
-        _need(q, "q", _BF16)
-        _need(k_cache, "k_cache", _BF16)
-        _need(v_cache, "v_cache", _BF16, cache)
-        _need(prefix_table, "prefix_table", _I32)
-        _need(block_table, "block_table", _I32)
+    _need(q, "q", _BF16)
+    _need(k_cache, "k_cache", _BF16)
+    _need(v_cache, "v_cache", _BF16, cache)
+    _need(prefix_table, "prefix_table", _I32)
+    _need(block_table, "block_table", _I32)
     if prefix_table.dim() != 2 or block_table.dim() != 2:
         raise ValueError("prefix_table and block_table must be two-dimensional")
     G, max_prefix = prefix_table.shape
     rows, max_pages = block_table.shape
     if rows != B:
         raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected ({B}, max_pages)")
-    try:
-        fine = (prefix_lens.dtype is _I32 and group_starts.dtype is _I32 and seq_lens.dtype is _I32
-                and prefix_lens.is_cuda and group_starts.is_cuda and seq_lens.is_cuda and prefix_lens.is_contiguous()
-                and group_starts.is_contiguous() and seq_lens.is_contiguous() and prefix_lens.dim() == 1
-                and group_starts.dim() == 1 and seq_lens.dim() == 1 and prefix_lens.numel() == G
-                and group_starts.numel() == G + 1 and seq_lens.numel() == B)
-    except AttributeError:
-        fine = False
-    if not fine:
-        _need(prefix_lens, "prefix_lens", _I32, (G,))
-        _need(group_starts, "group_starts", _I32, (G + 1,))
-        _need(seq_lens, "seq_lens", _I32, (B,))
+    _need(prefix_lens, "prefix_lens", _I32, (G,))
+    _need(group_starts, "group_starts", _I32, (G + 1,))
+    _need(seq_lens, "seq_lens", _I32, (B,))
     if out is None:
         out = _new(shape, _BF16, q.device, stream)
     _need(out, "out", _BF16, shape)
