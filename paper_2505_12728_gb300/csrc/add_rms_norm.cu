@@ -121,8 +121,10 @@ __device__ __forceinline__ float norm_scale(unsigned top, float inv) {
   return s < kLeastScale ? kLeastScale : s;
 }
 
-template <bool kWide, bool kE4m3, bool kVec, int kChunks>
-__global__ void __launch_bounds__(kChunks == 1 ? kNormMaxThreads / 2 : kNormMaxThreads)
+// kAhead: the weights stay in registers and the next row is loaded ahead (blocks of
+// at most 512 threads: the registers of 1024 do not hold that).
+template <bool kWide, bool kE4m3, bool kVec, int kChunks, bool kAhead>
+__global__ void __launch_bounds__(kAhead ? kNormMaxThreads / 2 : kNormMaxThreads)
 add_rms_norm_kernel(const __grid_constant__ NormParams p) {
   __shared__ float s_sum[2][kNormMaxThreads / 32];
   __shared__ unsigned s_top[2][kNormMaxThreads / 32];
@@ -137,13 +139,12 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
     return p.weight_wide ? static_cast<const float *>(p.weight)[col]
                          : __bfloat162float(static_cast<const __nv_bfloat16 *>(p.weight)[col]);
   };
-  // One chunk a thread: the weights stay in registers, and the next row is loaded
-  // ahead.  With more, the registers of 1024 threads do not hold that.
-  constexpr bool kAhead = kChunks == 1;
-  float w[8];
+  float w[kChunks][8];
   if constexpr (kAhead) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = weight(0, i);
+    for (int k = 0; k < kChunks; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[k][i] = weight(k, i);
   }
   NormChunk<kWide> x[kChunks], r[kChunks];
   auto load_row = [&](int row) {
@@ -174,7 +175,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sum = fmaf(h[k][i], h[k][i], sum);
-        h[k][i] *= kAhead ? w[i] : weight(k, i);
+        h[k][i] *= kAhead ? w[k][i] : weight(k, i);
         if constexpr (kE4m3) top = max(top, magnitude_bits(h[k][i]));
       }
     }
@@ -265,16 +266,19 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
 using NormKernel = void (*)(const NormParams);
 
 template <bool kWide, bool kE4m3, bool kVec>
-static NormKernel norm_kernel(int chunks) {
-  if (chunks == 1) return add_rms_norm_kernel<kWide, kE4m3, kVec, 1>;
-  if (chunks == 2) return add_rms_norm_kernel<kWide, kE4m3, kVec, 2>;
-  return add_rms_norm_kernel<kWide, kE4m3, kVec, 4>;
+static NormKernel norm_kernel(int chunks, bool ahead) {
+  if (chunks == 1) return add_rms_norm_kernel<kWide, kE4m3, kVec, 1, true>;
+  if constexpr (kVec && !kWide) {
+    if (ahead) return add_rms_norm_kernel<kWide, kE4m3, true, 2, true>;
+  }
+  if (chunks == 2) return add_rms_norm_kernel<kWide, kE4m3, kVec, 2, false>;
+  return add_rms_norm_kernel<kWide, kE4m3, kVec, 4, false>;
 }
 
-// Registers per thread of a variant (0 .. 23), looked up once per device.
+// Registers per thread of a variant (0 .. 31), looked up once per device.
 static int norm_registers(NormKernel fn, int device, int variant, int *regs) {
   static std::mutex mu;
-  static int known[64][24] = {};
+  static int known[64][32] = {};
   if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
   std::lock_guard<std::mutex> lock(mu);
   if (known[device][variant] == 0) {
@@ -345,17 +349,24 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
                    (!residual || (residual_stride % 8 == 0 && residual_out_stride % 8 == 0 && aligned(residual, 16) &&
                                   aligned(residual_out, 16)));
   const int items = (d + 7) / 8;
-  const int chunks = items <= 512 ? 1 : items <= 2 * kNormMaxThreads ? 2 : 4;
+  // One chunk a thread for rows of up to 4096, and two chunks, still with the next
+  // row loaded ahead, for long bf16 rows in number: half the threads wait at a row's
+  // barrier, and four CTAs of an SM are at different points of theirs (32768 x 3584
+  // to e4m3 143 -> 131 us, 4096 x 8192 50 -> 39, 2048 x 3584 to bf16 13.2 -> 11.6; but
+  // 16384 x 4096 to bf16 84 -> 88,
+  // and 128 x 3584, one row a CTA, 2.8 -> 3.2).
+  const bool two = vec && !wide && items > 256 && items <= kNormMaxThreads && T > 4 * dev.sm_count;
+  const int chunks = two ? 2 : items <= 512 ? 1 : items <= 2 * kNormMaxThreads ? 2 : 4;
   const int threads = ((items + chunks - 1) / chunks + 31) / 32 * 32;
   NormKernel fn;
   if (wide)
-    fn = e4m3 ? (vec ? norm_kernel<true, true, true>(chunks) : norm_kernel<true, true, false>(chunks))
-              : (vec ? norm_kernel<true, false, true>(chunks) : norm_kernel<true, false, false>(chunks));
+    fn = e4m3 ? (vec ? norm_kernel<true, true, true>(chunks, two) : norm_kernel<true, true, false>(chunks, two))
+              : (vec ? norm_kernel<true, false, true>(chunks, two) : norm_kernel<true, false, false>(chunks, two));
   else
-    fn = e4m3 ? (vec ? norm_kernel<false, true, true>(chunks) : norm_kernel<false, true, false>(chunks))
-              : (vec ? norm_kernel<false, false, true>(chunks) : norm_kernel<false, false, false>(chunks));
+    fn = e4m3 ? (vec ? norm_kernel<false, true, true>(chunks, two) : norm_kernel<false, true, false>(chunks, two))
+              : (vec ? norm_kernel<false, false, true>(chunks, two) : norm_kernel<false, false, false>(chunks, two));
   int regs = 0;
-  const int rst = norm_registers(fn, dev.ordinal, (wide ? 1 : 0) | (e4m3 ? 2 : 0) | (vec ? 4 : 0) | (chunks / 2) << 3, &regs);
+  const int rst = norm_registers(fn, dev.ordinal, (wide ? 1 : 0) | (e4m3 ? 2 : 0) | (vec ? 4 : 0) | (two ? 3 : chunks / 2) << 3, &regs);
   if (rst != SF_OK) return rst;
   // CTAs that are resident together, each for several rows where there are more
   long long per_sm = 65536 / (static_cast<long long>(threads) * ((regs + 7) / 8 * 8));
