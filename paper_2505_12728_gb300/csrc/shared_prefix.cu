@@ -20,17 +20,27 @@
 // query row a thread), a score buffer and an accumulator:
 //     TMEM columns  S_0 [0, 128)  S_1 [128, 256)  O_0 [256, 384)  O_1 [384, 512).
 // A piece with two row tiles gives one to each stream; a piece with one row tile
-// gives its even key tiles to stream 0 and its odd ones to stream 1 (two
-// partials), or, with one key tile, goes to the streams in turn.  So while one
-// stream's softmax runs, the tensor cores work for the other.
+// gives its even key tiles to stream 0 and its odd ones to stream 1, whose results
+// are joined in the CTA, or, with one key tile, goes to the streams in turn.  So
+// while one stream's softmax runs, the tensor cores work for the other.
 // P = exp2(S') goes back over the scores as bf16 (the A operand of O += P V), so
 // a stream's next Q K^T is issued behind its P V; tcgen05 MMAs of one thread
 // execute in issue order.  Each stream has a warp that issues its MMAs (one warp
-// for both, looking for what is ready, left the tensor cores idle for 300 cycles
-// before every operation: shared_long 349 -> XXX us); one warp copies K and V
-// and one Q, which has to wait for the stream's previous job while keys of the
-// next can be copied ahead.
-// K and V tiles go through one ring of 32 KB slots (16 KB with 64-wide heads).
+// for both, looking for what is ready, left the tensor cores idle for some 300
+// cycles before every operation); one warp copies K and V, and one publishes the
+// pieces and copies Q, which has to wait for the stream's previous job while keys of
+// the next can be copied ahead.  K and V tiles go through one ring of 32 KB slots (16
+// KB with 64-wide heads), which both streams pass in order.
+//
+// What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
+// 32768 tokens: 195 us, 1.26 PFLOP/s): the MMAs.  A key tile of two row tiles is 32 of
+// them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K, V
+// and the copies together read and write shared memory at its full 128 bytes a
+// cycle; a tile takes 2,800 cycles with what the turns leave idle.  One row tile (8
+// sequences of 5 rows, 32 / 32 heads, 3008 tokens: 26 us for 62.5 MB, 2.4 TB/s) and
+// few keys: the start (the cut of the axis takes 3 us from cold instructions, the
+// first keys 2), the partials' way through L2 and the merge kernel (5 us behind the
+// last piece).
 //
 // The running maximum is a reference that moves when a row's new maximum
 // exceeds it by more than kSpRescaleLog2, so rescaling O is rare.  The row sums
@@ -56,10 +66,13 @@ constexpr uint32_t kSpTmemCols = 512;
 constexpr float kSpRescaleLog2 = 8.f;
 constexpr int kSpMergeThreads = 256;
 constexpr int kSpSmemMax = 227 * 1024;
-// Cost of a segment on the partition's axis: kSpCostTile[dual] for each of its key
-// tiles (one row tile, or two), and kSpCostSeg for itself (its Q copy, pipeline
-// start and epilogue).  Measured: 0.42 us a unit.
-constexpr uint32_t kSpCostSeg = 3, kSpCostOne = 3, kSpCostTwo = 4;
+// Cost of a segment on the partition's axis: kSpCostOne or kSpCostTwo for each of its
+// key tiles (one row tile, or two), and kSpCostSeg for itself (its Q copy, pipeline
+// start and epilogue).  Measured, least squares over the CTAs of three workloads: 1.3
+// to 1.5 us for a key tile of two row tiles, 0.9 to 1.8 of one, 2 to 4 for a piece.
+// With one unit for every row tile's key tile and two a segment the longest CTA of
+// the workload of 64 sequences took 18 % more than the mean (225 us, now 195).
+constexpr uint32_t kSpCostSeg = 5, kSpCostOne = 3, kSpCostTwo = 4;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
 constexpr int kSpItems = 4;      // pieces published ahead
 
@@ -119,7 +132,7 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
                                static_cast<uint32_t>(x.key_tiles) *
                                    (kSpCostTwo * static_cast<uint32_t>(x.tiles >> 1) + kSpCostOne * (x.tiles & 1))
                          : 0u;
-  x.slot_rows = x.tiles > 1 ? 2u * kSpTile : 2u * static_cast<uint32_t>(x.tokens * p.group);
+  x.slot_rows = x.tiles > 1 ? 2u * kSpTile : static_cast<uint32_t>(x.tokens * p.group);
   return x;
 }
 
@@ -180,11 +193,12 @@ struct SpSmem {
   static constexpr int kQOffset = STAGES * kTileBytes;
   static constexpr int kBarOffset = kQOffset + 2 * kTileBytes;
   // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full[2], o_done, fin, turn;
-  // item_full, item_empty per published piece
-  static constexpr int kNumBars = 2 * STAGES + 16 + 2 * kSpItems;
+  // item_full, item_empty per published piece; joint, read per stream
+  static constexpr int kNumBars = 2 * STAGES + 16 + 2 * kSpItems + 4;
   static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word
   static constexpr int kItemOffset = kMiscOffset + 16;
-  static constexpr int kPlanOffset = kItemOffset + kSpItems * static_cast<int>(sizeof(SpItem));
+  static constexpr int kMlOffset = kItemOffset + kSpItems * static_cast<int>(sizeof(SpItem));  // float2 [2][128]
+  static constexpr int kPlanOffset = kMlOffset + 2 * 8 * kSpTile;
 };
 
 // max of three in one instruction (a NaN is ignored, as by fmaxf)
@@ -230,7 +244,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   constexpr uint32_t kIdescPV = idesc_bf16_f32(128, D, 0, 1);
   constexpr int FULL = 0, EMPTY = STAGES, QFULL = 2 * STAGES, QEMPTY = QFULL + 2, SFULL = QEMPTY + 2,
                 PFULL = SFULL + 2, ODONE = PFULL + 4, FIN = ODONE + 2, TURN = FIN + 2,
-                IFULL = TURN + 2, IEMPTY = IFULL + kSpItems;
+                IFULL = TURN + 2, IEMPTY = IFULL + kSpItems, JOINT = IEMPTY + kSpItems, READ = JOINT + 2;
 
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t ring = smem_addr(smem);
@@ -253,6 +267,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       mbar_init(bar(ODONE + s), 1);
       mbar_init(bar(FIN + s), 1);
       mbar_init(bar(TURN + s), 1);
+      mbar_init(bar(JOINT + s), 4);
+      mbar_init(bar(READ + s), 4);
     }
     for (int i = 0; i < kSpItems; ++i) {
       mbar_init(bar(IFULL + i), 1);
@@ -459,7 +475,6 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
               j.first = s;
               j.step = 2;
               j.n = (it.n + 1 - s) >> 1;
-              j.slot += s * rows0;
             } else {  // one key tile: the streams in turn
               j.n = turn == s;
             }
@@ -710,13 +725,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const bool w = mbar_wait_or_abort(b, parity, s_abort);
       return __all_sync(0xffffffffu, w);
     };
-    uint32_t base = 0, tiles = 0, jobs = 0;
+    uint32_t base = 0, tiles = 0, jobs = 0, joints = 0;
     bool ok = true;
     while (ok) {
       const SpItem *item = next_item();
       if (!item) break;
       const int n = item->s[s].n, step = item->s[s].step, rows = item->s[s].rows, keys = item->keys;
       const uint32_t slot0 = item->s[s].slot;
+      const bool joint = !item->dual && item->n > 1;  // the other stream has a part of the same row tile
       bool two = item->two && item->s[s].first == 0;
       uint32_t ring_tile = base + item->s[s].first;
       int tile_pos = (item->t0 + item->s[s].first) * kSpTile;  // position of the tile's first key
@@ -866,19 +882,58 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       ++jobs;
       tc_fence_after_sync();
       float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
+      if (!joint) {
 #pragma unroll 1
-      for (int ch = 0; ch < D / 32; ++ch) {
-        uint32_t ov[32];
-        tmem_ld_32x32b_x32(to + ch * 32, ov);
-        if (valid) {
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t ov[32];
+          tmem_ld_32x32b_x32(to + ch * 32, ov);
+          if (valid) {
 #pragma unroll
-          for (int q4 = 0; q4 < 8; ++q4)
-            dst[static_cast<size_t>(ch * 8 + q4) * rows] =
-                make_float4(__uint_as_float(ov[4 * q4]), __uint_as_float(ov[4 * q4 + 1]),
-                            __uint_as_float(ov[4 * q4 + 2]), __uint_as_float(ov[4 * q4 + 3]));
+            for (int q4 = 0; q4 < 8; ++q4)
+              dst[static_cast<size_t>(ch * 8 + q4) * rows] =
+                  make_float4(__uint_as_float(ov[4 * q4]), __uint_as_float(ov[4 * q4 + 1]),
+                              __uint_as_float(ov[4 * q4 + 2]), __uint_as_float(ov[4 * q4 + 3]));
+          }
         }
+        if (valid) p.part_ml[slot0 + r] = make_float2(ref, l_run);
+      } else {
+        // Both streams' accumulators of a row are in this thread's lane, and its
+        // maximum and sum come through shared memory: each stream joins and writes
+        // half of the columns, when both are done, and goes on when both have read.
+        float2 *s_ml = reinterpret_cast<float2 *>(smem + L::kMlOffset);
+        s_ml[s * kSpTile + r] = make_float2(ref, l_run);
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(JOINT + s));
+        if (!(ok = wwait(bar(JOINT + 1 - s), joints & 1u))) break;
+        tc_fence_after_sync();
+        const float2 ml = s_ml[(1 - s) * kSpTile + r];
+        const float top = fmaxf(ref, ml.x);
+        const float w = ref == -INFINITY ? 0.f : fast_exp2(ref - top), wo = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
+        const uint32_t half = s * (D / 2), other = to + 128 - 256 * s;  // (O_0, O_1 are 128 columns apart)
+#pragma unroll 1
+        for (int ch = 0; ch < D / 32; ++ch) {
+          uint32_t a[16], b[16];
+          tmem_ld_32x32b_x16(to + half + ch * 16, a);
+          tmem_ld_32x32b_x16(other + half + ch * 16, b);
+          if (valid) {
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              float v[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                v[i] = __uint_as_float(a[4 * q4 + i]) * w + __uint_as_float(b[4 * q4 + i]) * wo;
+              dst[static_cast<size_t>(half / 4 + ch * 4 + q4) * rows] = make_float4(v[0], v[1], v[2], v[3]);
+            }
+          }
+        }
+        if (valid && s == 0) p.part_ml[slot0 + r] = make_float2(top, l_run * w + ml.y * wo);
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(READ + s));
+        if (!(ok = wwait(bar(READ + 1 - s), joints & 1u))) break;
+        ++joints;
       }
-      if (valid) p.part_ml[slot0 + r] = make_float2(ref, l_run);
       tc_fence_before_sync();
     }
     tc_fence_before_sync();
@@ -904,7 +959,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 // --------------------------------------------------------------------------
 constexpr int kSpJoinBatch = 8;
 constexpr int kSpMaxSms = 512;                // CTAs of the split kernel at most
-constexpr int kSpListMax = 4 * kSpMaxSms;     // two partials per CTA from the prefix, two from the own segment
+constexpr int kSpListMax = 2 * kSpMaxSms;     // a partial per CTA from the prefix, one from the own segment
 
 struct SpJoin {
   float M, L;
@@ -936,21 +991,15 @@ __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32
   const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
   const uint32_t base = cost + h * x.head_cost + pair * x.pair_cost();
   slot += (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
-  const int rows = sp_rows(p, x, tile);
   const int last = static_cast<int>(sp_div(base + sp_cost(dual, x.key_tiles) - 1, chunk));
   for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
-    int k = 0;
-    if (c <= last) {
-      // (a range's end may lie past the axis' end: no tile does)
-      k = sp_tile_at((c + 1) * chunk, base, dual, x.key_tiles) - sp_tile_at(c * chunk, base, dual, x.key_tiles);
-      k = dual ? min(k, 1) : min(k, 2);  // partials of this piece
-    }
-    const unsigned one = __ballot_sync(0xffffffffu, k > 0), two = __ballot_sync(0xffffffffu, k > 1);
-    const unsigned below = (1u << lane) - 1u;
-    const int at = n + __popc(one & below) + __popc(two & below);
-    for (int u = 0; u < k; ++u) list[at + u] = slot + 2u * kSpTile * c + u * rows;
-    n += __popc(one) + __popc(two);
+    // (a range's end may lie past the axis' end: no tile does)
+    const bool piece = c <= last && sp_tile_at((c + 1) * chunk, base, dual, x.key_tiles) >
+                                        sp_tile_at(c * chunk, base, dual, x.key_tiles);
+    const unsigned in = __ballot_sync(0xffffffffu, piece);
+    if (piece) list[n + __popc(in & ((1u << lane) - 1u))] = slot + 2u * kSpTile * c;
+    n += __popc(in);
   }
   return n;
 }
@@ -1065,7 +1114,7 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
   const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
   SpBounds b;
   b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostOne + B * (kSpCostSeg + own_tiles * kSpCostOne));
-  b.rows = H_kv * (pairs * 2 * kSpTile + 2 * tokens * group) + 2LL * kSpTile * G;
+  b.rows = H_kv * (pairs * 2 * kSpTile + tokens * group) + 2LL * kSpTile * G;
   return b;
 }
 
