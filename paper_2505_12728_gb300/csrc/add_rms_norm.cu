@@ -10,7 +10,12 @@
 // maximum of |h * weight| along with the sum of squares (y is that times one
 // positive factor), so that the scales need no pass of their own; a group of 128
 // columns is 16 neighbouring threads.  CTAs stay for several rows, with the next
-// row's loads in flight during the reduction of the present one.
+// row's loads in flight during the reduction of the present one.  Rows that start off
+// 16-byte boundaries, but all tensors' alike (d odd, say), are cut at those
+// boundaries instead of at the row's start, so that only a row's first and last chunk
+// go element by element.  With a grid of a multiple of 8 CTAs, a CTA's rows all lie
+// alike, and it keeps its weights in registers as it does for aligned rows.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -33,9 +38,14 @@ struct NormParams {
   long long x_stride, residual_stride, residual_out_stride, out_stride;
   int T, d, groups;
   int weight_wide;
+  int shift;  // kNormShifted: elements from x's last 16-byte boundary (of 8 elements) to x
   float eps;
 };
 
+// How a thread's elements lie in a row: 8 neighbours, with every row on a 16-byte
+// boundary; 8 neighbours between boundaries that are the same in all tensors; or a
+// block's width apart, one element at a time.
+constexpr int kNormVec = 0, kNormShifted = 1, kNormSingle = 2;
 // 8 elements as they lie in memory
 template <bool kWide>
 struct NormChunk {
@@ -52,34 +62,41 @@ __device__ __forceinline__ float norm_elem(const NormChunk<true> &c, int i) {
   return __uint_as_float(k == 0 ? q.x : k == 1 ? q.y : k == 2 ? q.z : q.w);
 }
 
-// Where element (k, i) of a thread lies in its row: chunks of 8 neighbours, or,
-// where 16-byte accesses are not possible, a block's width apart.
-template <bool kVec>
-__device__ __forceinline__ int norm_column(int k, int i, int nt) {
-  return kVec ? (k * nt + static_cast<int>(threadIdx.x)) * 8 + i : (k * 8 + i) * nt + static_cast<int>(threadIdx.x);
+// Column of element (k, i) of a thread; `o`: elements from a 16-byte boundary to
+// the row's start.
+template <int kMode>
+__device__ __forceinline__ int norm_column(int k, int i, int nt, int o) {
+  if constexpr (kMode == kNormSingle) return (k * 8 + i) * nt + static_cast<int>(threadIdx.x);
+  else return (k * nt + static_cast<int>(threadIdx.x)) * 8 + i - (kMode == kNormShifted ? o : 0);
 }
 
-template <bool kWide, bool kVec>
-__device__ __forceinline__ void norm_load(const void *base, long long row, int k, int nt, int d, NormChunk<kWide> &c) {
-  if constexpr (kVec) {
-    const int col = norm_column<true>(k, 0, nt);
-    if (col < d) {
+// `last`: no row follows in the tensor.  A row's first and last chunk between
+// boundaries hold elements of the neighbouring rows, or of the space between, which
+// are read and dropped; before the first row and behind the last is nothing to read.
+template <bool kWide, int kMode>
+__device__ __forceinline__ void norm_load(const void *base, long long row, bool first, bool last, int k, int nt, int d, int o, NormChunk<kWide> &c) {
+  const int col = norm_column<kMode>(k, 0, nt, o);
+  if constexpr (kMode != kNormSingle) {
+    c.v[0] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (kWide) c.v[1] = make_uint4(0u, 0u, 0u, 0u);
+    if (col >= d) return;
+    const bool whole = kMode == kNormVec || ((col >= 0 || !first) && (col + 8 <= d || !last));
+    if (whole) {
       const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + (row + col) * (kWide ? 4 : 2));
       c.v[0] = src[0];
       if constexpr (kWide) c.v[1] = src[1];
       return;
     }
-    c.v[0] = make_uint4(0u, 0u, 0u, 0u);
-    if constexpr (kWide) c.v[1] = make_uint4(0u, 0u, 0u, 0u);
-  } else {
+  }
+  if constexpr (kMode != kNormVec) {
     uint32_t e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int col = norm_column<false>(k, i, nt);
+      const int at = norm_column<kMode>(k, i, nt, o);
       e[i] = 0u;
-      if (col < d)
-        e[i] = kWide ? static_cast<const uint32_t *>(base)[row + col]
-                     : static_cast<uint32_t>(static_cast<const uint16_t *>(base)[row + col]);
+      if (at >= 0 && at < d)
+        e[i] = kWide ? static_cast<const uint32_t *>(base)[row + at]
+                     : static_cast<uint32_t>(static_cast<const uint16_t *>(base)[row + at]);
     }
     if constexpr (kWide) {
       c.v[0] = make_uint4(e[0], e[1], e[2], e[3]);
@@ -90,25 +107,37 @@ __device__ __forceinline__ void norm_load(const void *base, long long row, int k
   }
 }
 
-template <bool kWide, bool kVec>
-__device__ __forceinline__ void norm_store(void *base, long long row, int k, int nt, int d, const float (&v)[8]) {
-  if constexpr (kVec) {
-    const int col = norm_column<true>(k, 0, nt);
+template <bool kWide, int kMode>
+__device__ __forceinline__ void norm_store(void *base, long long row, int k, int nt, int d, int o, const float (&v)[8]) {
+  if constexpr (kMode != kNormSingle) {
+    const int col = norm_column<kMode>(k, 0, nt, o);
     if (col >= d) return;
-    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<char *>(base) + (row + col) * (kWide ? 4 : 2));
-    if constexpr (kWide) {
-      dst[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-      dst[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
-    } else {
-      dst[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    if (kMode == kNormVec || (col >= 0 && col + 8 <= d)) {
+      uint4 *dst = reinterpret_cast<uint4 *>(static_cast<char *>(base) + (row + col) * (kWide ? 4 : 2));
+      if constexpr (kWide) {
+        dst[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        dst[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+      } else {
+        dst[0] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+      }
+      return;
     }
-  } else {
+  }
+  if constexpr (kMode != kNormVec) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int col = norm_column<false>(k, i, nt);
-      if (col >= d) continue;
-      if constexpr (kWide) static_cast<float *>(base)[row + col] = v[i];
-      else static_cast<__nv_bfloat16 *>(base)[row + col] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 8; i += 2) {
+      const int col = norm_column<kMode>(k, i, nt, o), next = norm_column<kMode>(k, i + 1, nt, o);
+      if (kMode == kNormShifted && !kWide && col >= 0 && next < d) {
+        *reinterpret_cast<uint32_t *>(static_cast<__nv_bfloat16 *>(base) + row + col) = pack_bf16x2(v[i], v[i + 1]);
+        continue;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int at = j ? next : col;
+        if (at < 0 || at >= d) continue;
+        if constexpr (kWide) static_cast<float *>(base)[row + at] = v[i + j];
+        else static_cast<__nv_bfloat16 *>(base)[row + at] = __float2bfloat16_rn(v[i + j]);
+      }
     }
   }
 }
@@ -123,21 +152,26 @@ __device__ __forceinline__ float norm_scale(unsigned top, float inv) {
 
 // kAhead: the weights stay in registers and the next row is loaded ahead (blocks of
 // at most 512 threads: the registers of 1024 do not hold that).
-template <bool kWide, bool kE4m3, bool kVec, int kChunks, bool kAhead>
+template <bool kWide, bool kE4m3, int kMode, int kChunks, bool kAhead>
 __global__ void __launch_bounds__(kAhead ? kNormMaxThreads / 2 : kNormMaxThreads)
 add_rms_norm_kernel(const __grid_constant__ NormParams p) {
   __shared__ float s_sum[2][kNormMaxThreads / 32];
   __shared__ unsigned s_top[2][kNormMaxThreads / 32];
-  __shared__ unsigned s_group[kE4m3 && !kVec ? SF_MAX_NORM_DIM / kNormGroup : 1];
+  __shared__ unsigned s_group[kE4m3 && kMode != kNormVec ? SF_MAX_NORM_DIM / kNormGroup : 1];
+  constexpr bool kVec = kMode == kNormVec;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
   const bool grouped = kE4m3 && p.groups > 1;
   grid_dependency_wait();
   grid_launch_dependents();
-  auto weight = [&](int k, int i) -> float {
-    const int col = norm_column<kVec>(k, i, nt);
-    if (col >= p.d) return 0.f;
+  auto global_weight = [&](int col) -> float {
     return p.weight_wide ? static_cast<const float *>(p.weight)[col]
                          : __bfloat162float(static_cast<const __nv_bfloat16 *>(p.weight)[col]);
+  };
+  // elements from a 16-byte boundary to a row's start (the same for all rows of a CTA)
+  const int o = kMode == kNormShifted ? static_cast<int>((p.shift + blockIdx.x * p.x_stride) & 7) : 0;
+  auto weight = [&](int k, int i) -> float {
+    const int col = norm_column<kMode>(k, i, nt, o);
+    return col >= 0 && col < p.d ? global_weight(col) : 0.f;
   };
   float w[kChunks][8];
   if constexpr (kAhead) {
@@ -146,12 +180,42 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[k][i] = weight(k, i);
   }
+  // 8 values of a chunk as e4m3, of element `line` on with the next group's scale
+  auto store_e4m3 = [&](int row, int col, const float (&v)[8], float inv, float rs, float rs_next, int line) {
+    uint32_t q[2];
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      float e[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[j] = v[i + j] * inv * (kVec || i + j < line ? rs : rs_next);
+      q[i >> 2] = __nv_cvt_float2_to_fp8x2(make_float2(e[0], e[1]), __NV_SATFINITE, __NV_E4M3) |
+                  static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(e[2], e[3]), __NV_SATFINITE, __NV_E4M3)) << 16;
+    }
+    uint8_t *dst = static_cast<uint8_t *>(p.out) + row * p.out_stride + col;
+    if (kVec || (col >= 0 && col + 8 <= p.d)) {
+      *reinterpret_cast<uint2 *>(dst) = make_uint2(q[0], q[1]);
+      return;
+    }
+    if constexpr (!kVec) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        if (col + i >= 0 && col + i + 4 <= p.d) {
+          *reinterpret_cast<uint32_t *>(dst + i) = q[i >> 2];
+          continue;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + i + j >= 0 && col + i + j < p.d) dst[i + j] = static_cast<uint8_t>(q[i >> 2] >> (8 * j));
+      }
+    }
+  };
   NormChunk<kWide> x[kChunks], r[kChunks];
   auto load_row = [&](int row) {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      norm_load<kWide, kVec>(p.x, row * p.x_stride, k, nt, p.d, x[k]);
-      if (p.residual) norm_load<kWide, kVec>(p.residual, row * p.residual_stride, k, nt, p.d, r[k]);
+      const bool first = row == 0, last = row == p.T - 1;
+      norm_load<kWide, kMode>(p.x, row * p.x_stride, first, last, k, nt, p.d, o, x[k]);
+      if (p.residual) norm_load<kWide, kMode>(p.residual, row * p.residual_stride, first, last, k, nt, p.d, o, r[k]);
     }
   };
   int buf = 0;
@@ -168,10 +232,20 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
         h[k][i] = norm_elem(x[k], i);
         if (p.residual) h[k][i] += norm_elem(r[k], i);
       }
+    if constexpr (kMode == kNormShifted) {
+#pragma unroll
+      for (int k = 0; k < kChunks; ++k) {
+        const int col = norm_column<kMode>(k, 0, nt, o);
+        if (col >= 0 && col + 8 <= p.d) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (col + i < 0 || col + i >= p.d) h[k][i] = 0.f;
+      }
+    }
     if (kAhead && row + static_cast<int>(gridDim.x) < p.T) load_row(row + gridDim.x);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      if (p.residual) norm_store<kWide, kVec>(p.residual_out, row * p.residual_out_stride, k, nt, p.d, h[k]);
+      if (p.residual) norm_store<kWide, kMode>(p.residual_out, row * p.residual_out_stride, k, nt, p.d, o, h[k]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sum = fmaf(h[k][i], h[k][i], sum);
@@ -180,7 +254,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
       }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
     if (lane == 0) s_sum[buf][warp] = sum;
     if constexpr (kE4m3) {
       if (!grouped) {
@@ -193,30 +267,49 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
     __syncthreads();
     sum = lane < nw ? s_sum[buf][lane] : 0.f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
     const float inv = 1.f / sqrtf(sum / static_cast<float>(p.d) + p.eps);
     if constexpr (!kE4m3) {
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[k][i] *= inv;
-        norm_store<false, kVec>(p.out, row * p.out_stride, k, nt, p.d, h[k]);
+        norm_store<false, kMode>(p.out, row * p.out_stride, k, nt, p.d, o, h[k]);
       }
     } else {
       float scale = 0.f;
       if (!grouped) {
         scale = norm_scale(__reduce_max_sync(0xffffffffu, lane < nw ? s_top[buf][lane] : 0u), inv);
         if (tid == 0) p.scales[row] = scale;
-      } else if constexpr (!kVec) {
+      } else if constexpr (kMode == kNormSingle) {
         // (a warp's 32 columns belong to one group: nt is a multiple of 32)
 #pragma unroll
         for (int k = 0; k < kChunks; ++k)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int col = norm_column<false>(k, i, nt);
+            const int col = norm_column<kMode>(k, i, nt, o);
             const unsigned m = __reduce_max_sync(0xffffffffu, magnitude_bits(h[k][i]));
             if (lane == 0 && col < p.d) atomicMax(&s_group[col / kNormGroup], m);
           }
+      } else if constexpr (kMode == kNormShifted) {
+        // 16 threads hold a group, but its last elements are in the next one's first chunk
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) {
+          const int g = (k * nt + tid) >> 4;
+          const bool leader = (lane & 15) == 0;
+          unsigned m = 0u, before = 0u;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (leader && i < o) before = max(before, magnitude_bits(h[k][i]));
+            else m = max(m, magnitude_bits(h[k][i]));
+          }
+#pragma unroll
+          for (int x = 8; x > 0; x >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, x));
+          if (leader && g < p.groups && m) atomicMax(&s_group[g], m);
+          if (leader && g > 0 && before) atomicMax(&s_group[g - 1], before);
+        }
+      }
+      if (grouped && !kVec) {
         __syncthreads();
         for (int g = tid; g < p.groups; g += nt)
           p.scales[static_cast<size_t>(row) * p.groups + g] = norm_scale(s_group[g], inv);
@@ -224,32 +317,34 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
         if constexpr (kVec) {
-          const int col = norm_column<true>(k, 0, nt);
+          const int col = norm_column<kMode>(k, 0, nt, o);
           if (grouped) {
             unsigned m = 0u;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(h[k][i]));
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+            for (int x = 8; x > 0; x >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, x));
             scale = norm_scale(m, inv);
             if ((lane & 15) == 0 && col < p.d) p.scales[static_cast<size_t>(row) * p.groups + col / kNormGroup] = scale;
           }
           const float rs = 1.f / scale;
+          if (col < p.d) store_e4m3(row, col, h[k], inv, rs, rs, 8);
+        } else if constexpr (kMode == kNormShifted) {
+          const int col = norm_column<kMode>(k, 0, nt, o);
           if (col < p.d) {
-            uint32_t q[2];
-#pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-              const float a = h[k][i] * inv * rs, b = h[k][i + 1] * inv * rs, c = h[k][i + 2] * inv * rs,
-                          e = h[k][i + 3] * inv * rs;
-              q[i >> 2] = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3) |
-                          static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(c, e), __NV_SATFINITE, __NV_E4M3)) << 16;
+            // the chunk's group, the next one, and where that begins
+            const int g = max(col, 0) / kNormGroup, line = (g + 1) * kNormGroup - col;
+            float rs = 1.f / scale, rs_next = rs;
+            if (grouped) {
+              rs = 1.f / norm_scale(s_group[g], inv);
+              rs_next = line < 8 && g + 1 < p.groups ? 1.f / norm_scale(s_group[g + 1], inv) : rs;
             }
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.out) + row * p.out_stride + col) = make_uint2(q[0], q[1]);
+            store_e4m3(row, col, h[k], inv, rs, rs_next, line);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int col = norm_column<false>(k, i, nt);
+            const int col = norm_column<kMode>(k, i, nt, o);
             if (col >= p.d) continue;
             if (grouped) scale = norm_scale(s_group[col / kNormGroup], inv);
             static_cast<__nv_fp8_storage_t *>(p.out)[row * p.out_stride + col] =
@@ -265,20 +360,27 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
 
 using NormKernel = void (*)(const NormParams);
 
-template <bool kWide, bool kE4m3, bool kVec>
-static NormKernel norm_kernel(int chunks, bool ahead) {
-  if (chunks == 1) return add_rms_norm_kernel<kWide, kE4m3, kVec, 1, true>;
-  if constexpr (kVec && !kWide) {
-    if (ahead) return add_rms_norm_kernel<kWide, kE4m3, true, 2, true>;
+template <bool kWide, bool kE4m3, int kMode>
+static NormKernel norm_variant(int chunks, bool ahead) {
+  if (chunks == 1) return add_rms_norm_kernel<kWide, kE4m3, kMode, 1, true>;
+  if constexpr (!kWide && (kMode == kNormVec || (kMode == kNormShifted && !kE4m3))) {
+    if (ahead) return add_rms_norm_kernel<kWide, kE4m3, kMode, 2, true>;
   }
-  if (chunks == 2) return add_rms_norm_kernel<kWide, kE4m3, kVec, 2, false>;
-  return add_rms_norm_kernel<kWide, kE4m3, kVec, 4, false>;
+  if (chunks == 2) return add_rms_norm_kernel<kWide, kE4m3, kMode, 2, false>;
+  return add_rms_norm_kernel<kWide, kE4m3, kMode, 4, false>;
 }
 
-// Registers per thread of a variant (0 .. 31), looked up once per device.
+template <bool kWide, bool kE4m3>
+static NormKernel norm_kernel(int mode, int chunks, bool ahead) {
+  if (mode == kNormVec) return norm_variant<kWide, kE4m3, kNormVec>(chunks, ahead);
+  if (mode == kNormShifted) return norm_variant<kWide, kE4m3, kNormShifted>(chunks, ahead);
+  return norm_variant<kWide, kE4m3, kNormSingle>(chunks, ahead);
+}
+
+// Registers per thread of a variant (0 .. 63), looked up once per device.
 static int norm_registers(NormKernel fn, int device, int variant, int *regs) {
   static std::mutex mu;
-  static int known[64][32] = {};
+  static int known[64][64] = {};
   if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
   std::lock_guard<std::mutex> lock(mu);
   if (known[device][variant] == 0) {
@@ -342,41 +444,48 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
   const int st = current_device(&dev);
   if (st != SF_OK) return st;
   const bool wide = dtype == SF_F32;
-  // 16-byte accesses need 8 neighbouring elements in every tensor
+  // 16-byte accesses: where in its 8 elements every row of every tensor starts
   const size_t out_bytes = e4m3 ? 1 : 2;
-  const bool vec = d % 8 == 0 && x_stride % 8 == 0 && out_stride % 8 == 0 && aligned(x, 16) &&
-                   aligned(out, 8 * out_bytes) &&
-                   (!residual || (residual_stride % 8 == 0 && residual_out_stride % 8 == 0 && aligned(residual, 16) &&
-                                  aligned(residual_out, 16)));
-  const int items = (d + 7) / 8;
+  auto start = [](const void *q, size_t bytes) { return static_cast<int>(reinterpret_cast<uintptr_t>(q) / bytes % 8); };
+  p.shift = start(x, e);
+  const bool alike = start(out, out_bytes) == p.shift && (out_stride - x_stride) % 8 == 0 &&
+                     (!residual || (start(residual, e) == p.shift && start(residual_out, e) == p.shift &&
+                                    (residual_stride - x_stride) % 8 == 0 && (residual_out_stride - x_stride) % 8 == 0));
+  const bool vec = alike && p.shift == 0 && x_stride % 8 == 0 && d % 8 == 0;
+  const int mode = vec ? kNormVec : alike && d <= SF_MAX_NORM_DIM - 14 ? kNormShifted : kNormSingle;
+  const int items = (d + 7 + (mode == kNormShifted ? 7 : 0)) / 8;
   // One chunk a thread for rows of up to 4096, and two chunks, still with the next
   // row loaded ahead, for long bf16 rows in number: half the threads wait at a row's
   // barrier, and four CTAs of an SM are at different points of theirs (32768 x 3584
-  // to e4m3 143 -> 131 us, 4096 x 8192 50 -> 39, 2048 x 3584 to bf16 13.2 -> 11.6; but
-  // 16384 x 4096 to bf16 84 -> 88,
-  // and 128 x 3584, one row a CTA, 2.8 -> 3.2).
-  const bool two = vec && !wide && items > 256 && items <= kNormMaxThreads && T > 4 * dev.sm_count;
+  // to e4m3 143 -> 131 us, 4096 x 8192 50 -> 39, 20000 x 3589 to bf16 108 -> 92; but
+  // 16384 x 4096 to bf16 84 -> 88, 128 x 3584, one row a CTA, 2.8 -> 3.2, and
+  // 12000 x 5001 to e4m3, with 111 registers, 119 -> 140).
+  const bool two = (vec || (mode == kNormShifted && !e4m3)) && !wide && items > 256 && items <= kNormMaxThreads &&
+                   T > 4 * dev.sm_count;
   const int chunks = two ? 2 : items <= 512 ? 1 : items <= 2 * kNormMaxThreads ? 2 : 4;
   const int threads = ((items + chunks - 1) / chunks + 31) / 32 * 32;
-  NormKernel fn;
-  if (wide)
-    fn = e4m3 ? (vec ? norm_kernel<true, true, true>(chunks, two) : norm_kernel<true, true, false>(chunks, two))
-              : (vec ? norm_kernel<true, false, true>(chunks, two) : norm_kernel<true, false, false>(chunks, two));
-  else
-    fn = e4m3 ? (vec ? norm_kernel<false, true, true>(chunks, two) : norm_kernel<false, true, false>(chunks, two))
-              : (vec ? norm_kernel<false, false, true>(chunks, two) : norm_kernel<false, false, false>(chunks, two));
+  const NormKernel fn = wide ? (e4m3 ? norm_kernel<true, true>(mode, chunks, two) : norm_kernel<true, false>(mode, chunks, two))
+                             : (e4m3 ? norm_kernel<false, true>(mode, chunks, two) : norm_kernel<false, false>(mode, chunks, two));
   int regs = 0;
-  const int rst = norm_registers(fn, dev.ordinal, (wide ? 1 : 0) | (e4m3 ? 2 : 0) | (vec ? 4 : 0) | (two ? 3 : chunks / 2) << 3, &regs);
+  const int rst = norm_registers(fn, dev.ordinal, (wide ? 1 : 0) | (e4m3 ? 2 : 0) | mode << 2 | (two ? 3 : chunks / 2) << 4, &regs);
   if (rst != SF_OK) return rst;
   // CTAs that are resident together, each for several rows where there are more
   long long per_sm = 65536 / (static_cast<long long>(threads) * ((regs + 7) / 8 * 8));
   if (per_sm > 2048 / threads) per_sm = 2048 / threads;
   if (per_sm < 1) per_sm = 1;
+  // ... but no more than 104 KB of an SM's rows on their way in or out, where every
+  // CTA has several: HBM takes fewer streams of loads and stores better (16000 x 2184
+  // from fp32 86 -> 79 us, 32768 x 3584 to bf16 151 -> 142; to e4m3 100 KB are best).
+  if ((two || chunks == 1) && T >= 4 * per_sm * dev.sm_count) {
+    const long long row_bytes = static_cast<long long>(d) * (e * (residual ? 3 : 1) + out_bytes);
+    per_sm = std::min(per_sm, std::max(2LL, 104 * 1024 / row_bytes));
+  }
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(T < per_sm * dev.sm_count ? T : per_sm * dev.sm_count));
+  const long long resident = std::max(per_sm * dev.sm_count / 8 * 8, 8LL);
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(T, resident)));
   cfg.blockDim = dim3(threads);
   cfg.stream = stream;
   cfg.attrs = attr;

@@ -164,3 +164,35 @@ def test_on_another_stream():
     got = sfv.add_rms_norm(xs, ws, rs, eps=1e-6, out_dtype=torch.float8_e4m3fn, stream=side)
     side.synchronize()
     check(got, x, r, w, 1e-6, 0)
+
+
+# rows that start anywhere between 16-byte boundaries, in all tensors alike or not;
+# one row a CTA, several, and two chunks a thread
+@pytest.mark.parametrize("T, d, stride, offset, apart", [
+    (2600, 1, 1, 0, 0), (2600, 9, 11, 3, 0), (3000, 129, 129, 0, 0), (1300, 777, 777, 5, 0), (5, 5001, 5002, 7, 0),
+    (700, 3589, 3589, 1, 0), (1300, 640, 643, 5, 0), (700, 333, 333, 2, 1), (40, 4097, 4097, 0, 3), (3, 20001, 20001, 6, 0)])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("out_dtype, group", [(torch.bfloat16, 0), (torch.float8_e4m3fn, 0), (torch.float8_e4m3fn, 128)])
+def test_rows_between_boundaries(T, d, stride, offset, apart, kind, out_dtype, group):
+    require_gpu()
+
+    def rows(t, at):
+        big = torch.full((at + T * stride + 16,), 7.0, device="cuda").to(t.dtype)
+        view = big.as_strided((T, d), (stride, 1), at)
+        view.copy_(t)
+        return big, view
+
+    x, r, w = make(T, d, kind, seed=T + d)
+    bad = T // 2  # its neighbours share 16 bytes with it and keep their values
+    x[bad] = float("nan")
+    (_, xs), (_, rs) = rows(x, offset), rows(r, offset + apart)
+    ob, o = rows(torch.zeros(T, d, dtype=out_dtype), offset)
+    rb, ro = rows(torch.zeros(T, d, dtype=kind), offset)
+    out, r_out, sc = sfv.add_rms_norm(xs, w.cuda(), rs, eps=1e-6, group=group, out=o, residual_out=ro)
+    good = torch.arange(T) != bad
+    check((out[good.cuda()], r_out[good.cuda()], None if sc is None else sc[good.cuda()]), x[good], r[good], w, 1e-6, group)
+    assert out[bad].float().isnan().all() and r_out[bad].isnan().all()
+    inside = torch.zeros(ob.numel(), dtype=torch.bool, device="cuda")
+    inside.as_strided((T, d), (stride, 1), offset).fill_(True)
+    for big in (ob, rb):
+        assert (big.float()[~inside] == 7.0).all()
