@@ -39,6 +39,7 @@ struct NormParams {
   int T, d, groups;
   int weight_wide;
   int shift;  // kNormShifted: elements from x's last 16-byte boundary (of 8 elements) to x
+  int margin;  // kNormShifted: rows that hold 7 elements
   float eps;
 };
 
@@ -70,11 +71,12 @@ __device__ __forceinline__ int norm_column(int k, int i, int nt, int o) {
   else return (k * nt + static_cast<int>(threadIdx.x)) * 8 + i - (kMode == kNormShifted ? o : 0);
 }
 
-// `last`: no row follows in the tensor.  A row's first and last chunk between
-// boundaries hold elements of the neighbouring rows, or of the space between, which
-// are read and dropped; before the first row and behind the last is nothing to read.
+// A row's first and last chunk between boundaries hold elements of the neighbouring
+// rows, or of the space between, which are read and dropped.  `first`, `last`: rows
+// before or behind which the tensor may have fewer than the 7 elements of a chunk.
 template <bool kWide, int kMode>
-__device__ __forceinline__ void norm_load(const void *base, long long row, bool first, bool last, int k, int nt, int d, int o, NormChunk<kWide> &c) {
+__device__ __forceinline__ void norm_load(const void *base, long long row, bool first, bool last, int k, int nt, int d, int o,
+                                          NormChunk<kWide> &c) {
   const int col = norm_column<kMode>(k, 0, nt, o);
   if constexpr (kMode != kNormSingle) {
     c.v[0] = make_uint4(0u, 0u, 0u, 0u);
@@ -211,9 +213,9 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
   };
   NormChunk<kWide> x[kChunks], r[kChunks];
   auto load_row = [&](int row) {
+    const bool first = row < p.margin, last = row >= p.T - p.margin;
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const bool first = row == 0, last = row == p.T - 1;
       norm_load<kWide, kMode>(p.x, row * p.x_stride, first, last, k, nt, p.d, o, x[k]);
       if (p.residual) norm_load<kWide, kMode>(p.residual, row * p.residual_stride, first, last, k, nt, p.d, o, r[k]);
     }
@@ -448,6 +450,7 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
   const size_t out_bytes = e4m3 ? 1 : 2;
   auto start = [](const void *q, size_t bytes) { return static_cast<int>(reinterpret_cast<uintptr_t>(q) / bytes % 8); };
   p.shift = start(x, e);
+  p.margin = x_stride >= 7 && (!residual || residual_stride >= 7) ? 1 : 7;
   const bool alike = start(out, out_bytes) == p.shift && (out_stride - x_stride) % 8 == 0 &&
                      (!residual || (start(residual, e) == p.shift && start(residual_out, e) == p.shift &&
                                     (residual_stride - x_stride) % 8 == 0 && (residual_out_stride - x_stride) % 8 == 0));
