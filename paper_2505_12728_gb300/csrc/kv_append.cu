@@ -295,32 +295,34 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_any_kernel(const __g
   }
   __syncthreads();
   const long long place = s_place;
-  const int per = p.D - p.pairs;  // items of a rotated head: its pairs, then the single elements
-  const int heads = p.H_q + (place >= 0 ? p.H_kv : 0);
-  for (int x = tid; x < heads * per; x += kAppendThreads) {
-    const int h = x / per, e = x - h * per;
+  // A thread keeps its item of a head (a pair, or an element that is not turned) over
+  // the heads: one division for all of them.
+  const int per = p.D - p.pairs, at_once = kAppendThreads / per, e = tid % per;
+  const bool turn = e < p.pairs;
+  const int i0 = !turn ? e + p.pairs : p.interleaved ? 2 * e : e, i1 = p.interleaved ? 2 * e + 1 : e + p.pairs;
+  const float2 w = turn ? s_turn[e] : make_float2(1.f, 0.f);
+  const int heads = tid < at_once * per ? p.H_q + (place >= 0 ? p.H_kv : 0) : 0;
+#pragma unroll 2
+  for (int h = tid / per; h < heads; h += at_once) {
     const bool is_q = h < p.H_q;
     const void *src = is_q ? p.q : p.k;
     const long long so = is_q ? t * p.q_row + h * p.q_head : t * p.k_row + (h - p.H_q) * p.k_head;
     __nv_bfloat16 *dst = is_q ? p.q_out + (static_cast<size_t>(t) * p.H_q + h) * p.D
                               : p.k_cache + static_cast<size_t>(place + (h - p.H_q) * SF_PAGE_SIZE) * p.D;
-    if (e < p.pairs) {
-      const int i0 = p.interleaved ? 2 * e : e, i1 = p.interleaved ? 2 * e + 1 : e + p.pairs;
-      const float a = load_as_float(src, so + i0, p.wide), b = load_as_float(src, so + i1, p.wide);
-      const float2 w = s_turn[e];
+    const float a = load_as_float(src, so + i0, p.wide);
+    if (turn) {
+      const float b = load_as_float(src, so + i1, p.wide);
       dst[i0] = __float2bfloat16_rn(a * w.x - b * w.y);
       dst[i1] = __float2bfloat16_rn(a * w.y + b * w.x);
     } else {
-      const int i = e + p.pairs;
-      dst[i] = __float2bfloat16_rn(load_as_float(src, so + i, p.wide));
+      dst[i0] = __float2bfloat16_rn(a);
     }
   }
-  if (place < 0) return;
-  for (int x = tid; x < p.H_kv * p.D; x += kAppendThreads) {
-    const int h = x / p.D, e = x - h * p.D;
-    p.v_cache[static_cast<size_t>(place + h * SF_PAGE_SIZE) * p.D + e] =
-        __float2bfloat16_rn(load_as_float(p.v, t * p.v_row + h * p.v_head + e, p.wide));
-  }
+  const int v_at_once = kAppendThreads / p.D, i = tid % p.D;
+  if (place < 0 || tid >= v_at_once * p.D) return;
+  for (int h = tid / p.D; h < p.H_kv; h += v_at_once)
+    p.v_cache[static_cast<size_t>(place + h * SF_PAGE_SIZE) * p.D + i] =
+        __float2bfloat16_rn(load_as_float(p.v, t * p.v_row + h * p.v_head + i, p.wide));
 }
 
 }  // namespace sf
