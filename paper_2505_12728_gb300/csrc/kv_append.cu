@@ -153,7 +153,9 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *dst, const float (&v)[8]) 
 // the heads.
 template <bool kWide, bool kInterleaved>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendParams p, int rows) {
-  __shared__ float2 s_turn[kAppendRows][kMaxHeadDim / 2];
+  // a row's cosines and sines, two pairs of every chunk in turn: the chunks' threads
+  // read 16 neighbouring bytes each
+  __shared__ float4 s_turn[kAppendRows][kMaxHeadDim / 4];
   __shared__ long long s_place[kAppendRows];
   const int tid = threadIdx.x, warp = tid >> 5;
   const int t0 = blockIdx.x * rows, nr = min(rows, p.T - t0);
@@ -203,7 +205,11 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
   }
 #pragma unroll
   for (int i = 0; i < kTurns; ++i)
-    if (r_first + i * each < nr) s_turn[r_first + i * each][j] = pair_turn(p, step_j, position[i]);
+    if (r_first + i * each < nr) {
+      constexpr int kPairs = kInterleaved ? 4 : 8;  // of a chunk
+      reinterpret_cast<float2 *>(s_turn[r_first + i * each])[(j % kPairs / 2 * turned + j / kPairs) * 2 + j % 2] =
+          pair_turn(p, step_j, position[i]);
+    }
   __syncthreads();
   for (; h < p.H_q + p.H_kv; h += heads_at_once * gridDim.y) {
     const bool is_q = h < p.H_q;
@@ -221,23 +227,27 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
         float x[8], y[8];
         a[i].floats(x);
         if (turn) {
-          const float2 *w = s_turn[r] + (kInterleaved ? 4 : 8) * u;
+          const float4 *w = s_turn[r] + u;
           if constexpr (kInterleaved) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 c = w[e];
-              const float m = x[2 * e], n = x[2 * e + 1];
-              x[2 * e] = m * c.x - n * c.y;
-              x[2 * e + 1] = m * c.y + n * c.x;
+            for (int e = 0; e < 8; e += 4) {
+              const float4 c = w[e / 4 * turned];
+              const float x0 = x[e], x1 = x[e + 1], x2 = x[e + 2], x3 = x[e + 3];
+              x[e] = x0 * c.x - x1 * c.y;
+              x[e + 1] = x0 * c.y + x1 * c.x;
+              x[e + 2] = x2 * c.z - x3 * c.w;
+              x[e + 3] = x2 * c.w + x3 * c.z;
             }
           } else {
             b[i].floats(y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 c = w[e];
-              const float m = x[e], n = y[e];
-              x[e] = m * c.x - n * c.y;
-              y[e] = m * c.y + n * c.x;
+            for (int e = 0; e < 8; e += 2) {
+              const float4 c = w[e / 2 * turned];
+              const float x0 = x[e], y0 = y[e], x1 = x[e + 1], y1 = y[e + 1];
+              x[e] = x0 * c.x - y0 * c.y;
+              y[e] = x0 * c.y + y0 * c.x;
+              x[e + 1] = x1 * c.z - y1 * c.w;
+              y[e + 1] = x1 * c.w + y1 * c.z;
             }
             store8(dst + at + p.pairs, y);
           }
