@@ -14,11 +14,12 @@
 // row: a 32-ary search in row_starts), then its threads walk the heads, each with
 // one 16-byte chunk of a head (and, for pairs (j, j + n), the chunk of the partners)
 // in kBatch rows at a time.  A row's place is three loads that wait for each other:
-// the first rows' elements and the positions are loaded in front of them.  38k rows
-// of 28 + 8 bf16 heads of 128: 117 us, 5.6 TB/s (135 us with everything behind the
-// places, 148 with four rows at a time and three CTAs an SM).  Few rows are spread
-// over more CTAs by heads.  Tensors that 16-byte accesses cannot reach take
-// kv_append_any_kernel, one pair of elements at a time.
+// the first rows' elements and the positions are loaded in front of them.  35k rows
+// of 28 + 8 bf16 heads of 128: 105 us, 6.2 TB/s (117 us with the sines in the order of
+// the pairs, four-way bank conflicts; 148 with four rows at a time and three CTAs an
+// SM).  Few rows are spread over more CTAs by heads.  Tensors that 16-byte accesses
+// cannot reach take kv_append_any_kernel, one pair of elements at a time (16000 rows
+// of 28 + 8 heads of 128, 2 bytes off: 168 us, 51 on the boundary).
 #include <cmath>
 
 #include "sf_device.cuh"
@@ -28,6 +29,7 @@ namespace sf {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 8;      // rows of a CTA at most, one per warp for their places
+constexpr int kAppendResident = 4; // CTAs of an SM
 constexpr int kMaxHeadDim = 256;
 constexpr int kMaxHeads = 1024;
 
@@ -152,7 +154,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *dst, const float (&v)[8]) 
 // `rows` rows per CTA; blockIdx.y of gridDim.y takes every gridDim.y-th pass over
 // the heads.
 template <bool kWide, bool kInterleaved>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendParams p, int rows) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendResident) kv_append_kernel(const __grid_constant__ AppendParams p, int rows) {
   // a row's cosines and sines, two pairs of every chunk in turn: the chunks' threads
   // read 16 neighbouring bytes each
   __shared__ float4 s_turn[kAppendRows][kMaxHeadDim / 4];
@@ -163,8 +165,8 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
   grid_launch_dependents();
   // units of a head: its rotated chunks (or pairs of chunks), then the others.  A
   // thread has one unit of a head and takes the CTA's rows kBatch at a time, all their
-  // loads in flight.
-  constexpr int kBatch = kWide ? 1 : 2;
+  // loads in flight: 64 bytes (16000 rows of 36 interleaved bf16 heads: 60 us with 32).
+  constexpr int kBatch = (kWide ? 1 : 2) * (kInterleaved ? 2 : 1);
   const int turned = kInterleaved ? p.pairs / 4 : p.pairs / 8, rest = (p.D - 2 * p.pairs) / 8, units = turned + rest;
   const int u = tid % units, lane_head = tid / units, heads_at_once = kAppendThreads / units;
   const bool turn = u < turned, both = turn && !kInterleaved;
@@ -434,9 +436,12 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
   cfg.numAttrs = 1;
   cudaError_t err;
   if (vec) {
-    // as many rows a CTA as leave every SM several CTAs; few rows are cut by heads
-    int rows = static_cast<int>(T / (8LL * dev.sm_count));
-    rows = rows < 1 ? 1 : rows > kAppendRows ? kAppendRows : rows;
+    // Full waves of CTAs, with the fewest that kAppendRows allows (3250 rows of 16 + 4
+    // fp32 heads of 64: 7.2 us with one wave of 6 rows, 9.7 with 2.7 waves of 2); few
+    // rows are cut by heads.
+    const long long wave = static_cast<long long>(kAppendResident) * dev.sm_count;
+    const long long ctas = wave * ((T + wave * kAppendRows - 1) / (wave * kAppendRows));
+    const int rows = static_cast<int>((T + ctas - 1) / ctas);
     const int grid = (T + rows - 1) / rows;
     const int passes = ((H_q + H_kv) * (head_dim / 8) + kAppendThreads - 1) / kAppendThreads;
     int parts = dev.sm_count / grid;
