@@ -33,9 +33,9 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 195 us, 1.26 PFLOP/s): the MMAs.  A key tile of two row tiles is 32 of
-// them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K, V
-// and the copies together read and write shared memory at its full 128 bytes a
+// 32768 tokens: 194 to 204 us, 1.2 PFLOP/s): the MMAs.  A key tile of two row tiles is
+// 32 of them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K,
+// V and the copies together read and write shared memory at its full 128 bytes a
 // cycle; a tile takes 2,800 cycles with what the turns leave idle.  One row tile (8
 // sequences of 5 rows, 32 / 32 heads, 3008 tokens: 26 us for 62.5 MB, 2.4 TB/s) and
 // few keys: the start (the cut of the axis takes 3 us from cold instructions, the
