@@ -473,7 +473,8 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
   const int rst = norm_registers(fn, dev.ordinal, (wide ? 1 : 0) | (e4m3 ? 2 : 0) | mode << 2 | (two ? 3 : chunks / 2) << 4, &regs);
   if (rst != SF_OK) return rst;
   // CTAs that are resident together, each for several rows where there are more
-  long long per_sm = 65536 / (static_cast<long long>(threads) * ((regs + 7) / 8 * 8));
+  // (a sub-partition's 16K registers hold whole warps)
+  long long per_sm = 16384 / (32 * ((regs + 7) / 8 * 8)) * 4 / (threads / 32);
   if (per_sm > 2048 / threads) per_sm = 2048 / threads;
   if (per_sm < 1) per_sm = 1;
   // ... but no more than 104 KB of an SM's rows on their way in or out, where every
