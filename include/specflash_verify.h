@@ -428,7 +428,7 @@ int sf_visual_compress(const void *queries, const void *features, int F, int N, 
 /*               and strides agree.                                          */
 /* scales        fp32 [T][ceil(d / group)], or [T] for group 0; NULL with    */
 /*               SF_BF16.                                                    */
-/* Strides count elements.  0 <= T < 2^31 (0: nothing is done), 1 <= d <=    */
+/* Strides count elements.  0 <= T <= 0x7fff0000 (0: nothing), 1 <= d <=    */
 /* SF_MAX_NORM_DIM; every pointer aligned to its element.  16-byte accesses  */
 /* are used where addresses, strides and d allow them, else one element at a */
 /* time.  One launch; asynchronous on `stream`; deterministic.               */

@@ -27,6 +27,7 @@
 namespace sf {
 
 constexpr int kNormMaxThreads = 1024;
+constexpr int kNormMaxRows = 0x7fff0000;  // a row and a step of the grid fit an int
 constexpr int kNormGroup = 128;       // columns per scale
 constexpr float kE4m3Max = 448.f;     // largest finite e4m3 value
 constexpr float kLeastScale = 1.17549435e-38f;  // 2^-126
@@ -405,6 +406,7 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
   using namespace sf;
   clear_error();
   if (T < 0) return fail(SF_ERR_INVALID_ARG, "T=%d is negative", T);
+  if (T > kNormMaxRows) return fail(SF_ERR_UNSUPPORTED, "T=%d above %d", T, kNormMaxRows);
   if (d < 1 || d > SF_MAX_NORM_DIM) return fail(SF_ERR_INVALID_ARG, "d=%d outside [1, %d]", d, SF_MAX_NORM_DIM);
   if (dtype != SF_BF16 && dtype != SF_F32) return fail(SF_ERR_UNSUPPORTED, "dtype=%d (built: bf16, fp32)", dtype);
   if (weight_dtype != SF_BF16 && weight_dtype != SF_F32)

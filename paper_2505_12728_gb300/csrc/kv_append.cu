@@ -450,7 +450,7 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
     const long long wave = static_cast<long long>(kAppendResident) * dev.sm_count;
     const long long ctas = wave * ((T + wave * kAppendRows - 1) / (wave * kAppendRows));
     const int rows = static_cast<int>((T + ctas - 1) / ctas);
-    const int grid = (T + rows - 1) / rows;
+    const int grid = (T - 1) / rows + 1;
     const int passes = ((H_q + H_kv) * (head_dim / 8) + kAppendThreads - 1) / kAppendThreads;
     const int per_head = head_dim / 8 - (p.interleaved ? 0 : p.pairs / 8), at_once = kAppendThreads / per_head;
     const int row_groups = H_q + H_kv < at_once && rows > 1 ? at_once / (H_q + H_kv) : 1;

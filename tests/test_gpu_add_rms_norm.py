@@ -196,3 +196,16 @@ def test_rows_between_boundaries(T, d, stride, offset, apart, kind, out_dtype, g
     inside.as_strided((T, d), (stride, 1), offset).fill_(True)
     for big in (ob, rb):
         assert (big.float()[~inside] == 7.0).all()
+
+
+# narrow rows in number: a warp each, the last CTA not full
+@pytest.mark.parametrize("T, d", [(1217, 256), (1220, 248), (1301, 249), (4999, 64), (2001, 136), (1999, 255)])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("out_dtype, group", [(torch.bfloat16, 0), (torch.float8_e4m3fn, 0), (torch.float8_e4m3fn, 128)])
+def test_many_narrow_rows(T, d, kind, out_dtype, group):
+    require_gpu()
+    for residual in (True, False):
+        x, r, w = make(T, d, kind, seed=T + d, residual=residual, wkind=torch.float32)
+        got = sfv.add_rms_norm(x.cuda(), w.cuda(), None if r is None else r.cuda(), eps=1e-5, group=group,
+                               out_dtype=out_dtype)
+        check(got, x, r, w, 1e-5, group)

@@ -131,3 +131,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes_before_the_library(monkey
         sfv.shared_prefix_attention(q, cache[..., :32], cache, bt, sl, torch.zeros(2, dtype=i32), bt, sl)
     with pytest.raises(ValueError, match="q must be"):
         sfv.shared_prefix_attention(q[0], cache, cache, bt, sl, torch.zeros(2, dtype=i32), bt, sl)
+
+
+def test_norm_refuses_rows_that_a_step_of_the_grid_would_take_past_an_int(lib):
+    assert lib.sf_add_rms_norm(*norm_args(T=0x7fff0001)) == 2
+    assert b"T=" in lib.sf_last_error()
