@@ -9,8 +9,9 @@
 //    group's sequences for one KV head, packed into tiles of 128 rows (whole
 //    tokens: floor(128 / g) tokens of g query heads), two tiles a segment.  The
 //    prefix's keys and values are copied to shared memory once for 256 rows.
-//  * own segments (sequence, KV head): the sequence's n_q * g rows against its
-//    own tokens, with the causal mask of the draft block.
+//  * own segments (sequence, pair of KV heads): the sequence's n_q * g rows of each
+//    head against its own tokens, with the causal mask of the draft block.  Their key
+//    tiles alternate between the heads.
 // The segments' key tiles (128 keys) lie on one axis, which is cut into one
 // equal range per SM by a cost rule (below); a CTA works through the pieces of
 // its range and leaves one partial result (maximum, sum, O in fp32) per piece
@@ -19,9 +20,11 @@
 // The CTA has two streams, each with 128 softmax threads (one TMEM lane, one
 // query row a thread), a score buffer and an accumulator:
 //     TMEM columns  S_0 [0, 128)  S_1 [128, 256)  O_0 [256, 384)  O_1 [384, 512).
-// A piece with two row tiles gives one to each stream; a piece with one row tile
-// gives its even key tiles to stream 0 and its odd ones to stream 1, whose results
-// are joined in the CTA, or, with one key tile, goes to the streams in turn.  So
+// A piece with two row tiles gives one to each stream, and so does one with two heads
+// (59 sequences of 212 to 916 own tokens, 32 heads: @TWO, against 138 us with a
+// piece per head); a piece with one row tile gives its even key tiles to stream 0 and
+// its odd ones to stream 1, whose results are joined in the CTA, or, with one key
+// tile, goes to the streams in turn.  So
 // while one stream's softmax runs, the tensor cores work for the other.
 // P = exp2(S') goes back over the scores as bf16 (the A operand of O += P V), so
 // a stream's next Q K^T is issued behind its P V; tcgen05 MMAs of one thread
@@ -110,7 +113,9 @@ struct SpParams {
 // tiles, against `keys` keys.
 struct SpEntity {
   int keys, token0, tokens, tiles, pairs, key_tiles;
-  uint32_t head_cost;  // per KV head
+  int units;           // KV heads, or (own) pairs of KV heads, the last perhaps a single one
+  uint32_t head_cost;  // per unit
+  uint32_t cost;       // of all units
   uint32_t slot_rows;  // partial rows of one piece
   __device__ __forceinline__ uint32_t pair_cost() const { return kSpCostSeg + kSpCostTwo * static_cast<uint32_t>(key_tiles); }
 };
@@ -128,11 +133,20 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
   x.tiles = own ? 1 : sp_tiles(p, x.tokens + p.tokens_per_tile - 1);
   x.pairs = (x.tiles + 1) >> 1;
   x.key_tiles = (keys + kSpTile - 1) / kSpTile;
-  x.head_cost = keys > 0 ? static_cast<uint32_t>(x.pairs) * kSpCostSeg +
-                               static_cast<uint32_t>(x.key_tiles) *
-                                   (kSpCostTwo * static_cast<uint32_t>(x.tiles >> 1) + kSpCostOne * (x.tiles & 1))
-                         : 0u;
-  x.slot_rows = x.tiles > 1 ? 2u * kSpTile : static_cast<uint32_t>(x.tokens * p.group);
+  const uint32_t key_tiles = static_cast<uint32_t>(x.key_tiles);
+  if (own) {
+    x.units = (p.H_kv + 1) >> 1;
+    x.head_cost = kSpCostSeg + 2u * kSpCostOne * key_tiles;
+    x.cost = x.units * x.head_cost - (p.H_kv & 1) * kSpCostOne * key_tiles;
+    x.slot_rows = 2u * static_cast<uint32_t>(x.tokens * p.group);
+  } else {
+    x.units = p.H_kv;
+    x.head_cost = static_cast<uint32_t>(x.pairs) * kSpCostSeg +
+                  key_tiles * (kSpCostTwo * static_cast<uint32_t>(x.tiles >> 1) + kSpCostOne * (x.tiles & 1));
+    x.cost = x.units * x.head_cost;
+    x.slot_rows = x.tiles > 1 ? 2u * kSpTile : static_cast<uint32_t>(x.tokens * p.group);
+  }
+  if (keys == 0) x.head_cost = x.cost = 0u;
   return x;
 }
 
@@ -174,9 +188,10 @@ struct SpItem {
   int n, t0, keys;  // key tiles t0 .. t0 + n - 1 of the segment's keys; n = 0: no more pieces
   int own, row, h;  // row of block_table (own) or prefix_table
   int dual, again;  // both streams read every tile; the keys are read again by other pieces
-  int two;          // the first key tile's weights go to P V as two bf16 terms
+  int duo;          // key tiles t of head h + t % 2, a stream a head
   int pad;
   struct {
+    int two;               // the first key tile's weights go to P V as two bf16 terms
     int n, first, step;    // the stream's key tiles within the piece (n = 0: none)
     int token, rows;       // first query token and rows of its row tile
     uint32_t slot;         // first row of its partial
@@ -359,8 +374,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       return lo;
     };
     uint32_t sum = 0;
-    for (int e = lane; e < E; e += 32) sum += entity(e).head_cost;
-    const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum) * p.H_kv, chunk = sp_chunk(p, Tot);
+    for (int e = lane; e < E; e += 32) sum += entity(e).cost;
+    const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum), chunk = sp_chunk(p, Tot);
     const uint32_t c = blockIdx.x;
     const bool writes = c == gridDim.x - 1;  // this CTA (with the least to do) leaves the plan for the merge kernel
     const uint32_t at = min(c * chunk, Tot), end = min(at + chunk, Tot);
@@ -371,7 +386,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const int k = e0 + lane;
       SpEntity x{};
       if (k < E) x = entity(k);
-      uint32_t ci = x.head_cost * p.H_kv, si = x.head_cost ? x.slot_rows * x.pairs * p.H_kv : 0u;
+      uint32_t ci = x.cost, si = x.cost ? x.slot_rows * x.pairs * x.units : 0u;
       const uint32_t mine = ci, rows = si;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -436,25 +451,26 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       SpItem it;
       it.n = 0;
       while (it.n == 0 && e < E && base < end) {
-        const int dual = 2 * pair + 1 < x.tiles;
-        it.t0 = sp_tile_at(at, base, dual, x.key_tiles);
-        it.n = sp_tile_at(end, base, dual, x.key_tiles) - it.t0;
+        const bool own = e >= p.num_groups;
+        const int dual = 2 * pair + 1 < x.tiles, duo = own && 2 * h + 1 < p.H_kv, key_tiles = x.key_tiles << duo;
+        it.t0 = sp_tile_at(at, base, dual, key_tiles);
+        it.n = sp_tile_at(end, base, dual, key_tiles) - it.t0;
         if (it.n > 0) {
-          const bool own = e >= p.num_groups;
           it.keys = x.keys;
           it.own = own;
           it.row = own ? e - p.num_groups : e;
-          it.h = h;
+          it.h = own ? 2 * h : h;
           it.dual = dual;
+          it.duo = duo;
           it.again = x.pairs > 1;
-          // Rows that see few keys besides this segment's need more of its weights
-          // than 8 bits: over many keys the roundings average out.
-          int others = 0;
+          // Rows that see few keys need more of the weights than 8 bits: over many keys
+          // the roundings average out.
+          int least = x.keys;  // keys that every row sees, in all (of a prefix: at least)
           if (own) {
             const int g = group_of(it.row);
-            others = s_start[g + 1] > s_start[g] ? s_len[g] : 0;
+            least += (s_start[g + 1] > s_start[g] ? s_len[g] : 0) + 1 - p.n_q;
           }
-          it.two = it.t0 == 0 && (own ? others : x.keys) < kSpTile;
+          const bool few = least < kSpTile;
           const int rows0 = sp_rows(p, x, 2 * pair), tok0 = x.token0 + 2 * pair * p.tokens_per_tile;
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
@@ -471,6 +487,11 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                 j.rows = sp_rows(p, x, 2 * pair + 1);
                 j.slot += kSpTile;
               }
+            } else if (duo) {  // a head each
+              j.first = (it.t0 ^ s) & 1;
+              j.step = 2;
+              j.n = (it.n + 1 - j.first) >> 1;
+              j.slot += s * rows0;
             } else if (it.n > 1) {  // even and odd key tiles
               j.first = s;
               j.step = 2;
@@ -478,15 +499,16 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             } else {  // one key tile: the streams in turn
               j.n = turn == s;
             }
+            j.two = few && (it.t0 + j.first) >> duo == 0;
           }
-          if (!dual && it.n == 1) turn ^= 1;
+          if (!dual && !duo && it.n == 1) turn ^= 1;
         }
         // the next segment
-        base += sp_cost(dual, x.key_tiles);
+        base += sp_cost(dual, key_tiles);
         slot += x.slot_rows;
         if (++pair == x.pairs) {
           pair = 0;
-          if (++h == p.H_kv) {
+          if (++h == x.units) {
             h = 0;
             do x = ++e < E ? entity(e) : x;
             while (e < E && x.head_cost == 0);  // entities without keys or rows
@@ -510,7 +532,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                                 static_cast<uint32_t>((it.own ? p.n_q : p.tokens_per_tile) * p.group * D * 2));
           for (int hf = 0; hf < HALVES; ++hf)
             tma_load_4d(ring + L::kQOffset + s * L::kTileBytes + hf * kHalfTileBytes, it.own ? &tmap_q_own : &tmap_q_tile,
-                        64 * hf, 0, it.h, it.s[s].token, bar(QFULL + s), again);
+                        64 * hf, 0, it.h + (it.duo & s), it.s[s].token, bar(QFULL + s), again);
         }
         __syncwarp();
         ++jobs[s];
@@ -538,7 +560,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     while (ok) {
       const SpItem *item = next_item();
       if (!item) break;
-      const int n = item->n, t0 = item->t0, keys = item->keys, h = item->h;
+      const int n = item->n, t0 = item->t0, keys = item->keys, h = item->h, duo = item->duo;
       const int32_t *table = item->own ? p.block_table + static_cast<size_t>(item->row) * p.max_pages
                                        : p.prefix_table + static_cast<size_t>(item->row) * p.max_prefix_pages;
       const uint64_t policy = item->again ? again : once;
@@ -546,7 +568,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       int ids = kBeyondEnd;
       for (int it = 0; it < n; ++it) {
         if ((it & 3) == 0) {  // page ids of the next four tiles, one a lane
-          const int lt = it + (lane >> 3), page = (t0 + lt) * kSpTilePages + (lane & 7);
+          const int lt = it + (lane >> 3), page = ((t0 + lt) >> duo) * kSpTilePages + (lane & 7);
           ids = lt < n && page * SF_PAGE_SIZE < keys ? table[page] : kBeyondEnd;
         }
         const int phys = __shfl_sync(0xffffffffu, ids, ((it & 3) << 3) + (lane & 7));
@@ -555,7 +577,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           if (phys < 0 || phys >= p.num_pages) {
             if (lane < kSpTilePages) set_status(p.status, SF_DEVICE_BAD_PAGE);
           } else {
-            row = (phys * p.H_kv + h) * SF_PAGE_SIZE;
+            row = (phys * p.H_kv + h + (duo & (t0 + it))) * SF_PAGE_SIZE;
           }
         }
         int rows[kSpTilePages];  // the same in every lane: the copies' operands are warp-uniform
@@ -639,7 +661,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const int step = __shfl_sync(0xffffffffu, item->s[s].step, 0);
       const bool dual = __shfl_sync(0xffffffffu, item->dual, 0) != 0;
       int mine = n > 0 ? __shfl_sync(0xffffffffu, item->s[s].first, 0) : total;  // the stream's next key tile
-      bool two = __shfl_sync(0xffffffffu, item->two, 0) != 0 && mine == 0;  // P_hi + P_lo on the segment's first key tile
+      bool two = __shfl_sync(0xffffffffu, item->s[s].two, 0) != 0;  // P_hi + P_lo on the segment's first key tile
       int left = n;
       bool ahead = false;  // the tile's Q K^T is issued already
       release_item();
@@ -732,10 +754,11 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       if (!item) break;
       const int n = item->s[s].n, step = item->s[s].step, rows = item->s[s].rows, keys = item->keys;
       const uint32_t slot0 = item->s[s].slot;
-      const bool joint = !item->dual && item->n > 1;  // the other stream has a part of the same row tile
-      bool two = item->two && item->s[s].first == 0;
+      const int duo = item->duo;
+      const bool joint = !item->dual && !duo && item->n > 1;  // the other stream has a part of the same row tile
+      bool two = item->s[s].two != 0;
       uint32_t ring_tile = base + item->s[s].first;
-      int tile_pos = (item->t0 + item->s[s].first) * kSpTile;  // position of the tile's first key
+      int tile_pos = ((item->t0 + item->s[s].first) >> duo) * kSpTile;  // position of the tile's first key
       base += item->n;
       const bool valid = r < rows;
       // last visible key of this row (rows past the tile's end see every key:
@@ -744,7 +767,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       release_item();
       if (n == 0) continue;
       float ref = -INFINITY, l_run = 0.f;
-      for (int k = 0; k < n; ++k, ++tiles, ring_tile += step, tile_pos += step * kSpTile) {
+      for (int k = 0; k < n; ++k, ++tiles, ring_tile += step, tile_pos += (step >> duo) * kSpTile) {
         if (!(ok = wwait(bar(SFULL + s), tiles & 1u))) break;
         tc_fence_after_sync();
         uint32_t sv[128];
@@ -986,17 +1009,19 @@ struct SpJoin {
 // Appends the first partial rows of a row tile's partials of one segment to
 // list[n ..]; returns the new length.  A whole warp calls it.
 __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32_t cost, uint32_t slot, const SpEntity &x,
-                                       int h, int tile, uint32_t *list, int n) {
+                                       bool own, int h, int tile, uint32_t *list, int n) {
   if (x.head_cost == 0) return n;
   const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
-  const uint32_t base = cost + h * x.head_cost + pair * x.pair_cost();
-  slot += (h * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : 0);
-  const int last = static_cast<int>(sp_div(base + sp_cost(dual, x.key_tiles) - 1, chunk));
+  const int duo = own && (h | 1) < p.H_kv, second = h & 1, unit = own ? h >> 1 : h, key_tiles = x.key_tiles << duo;
+  const uint32_t base = cost + unit * x.head_cost + pair * x.pair_cost();
+  slot += (unit * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : duo ? second * x.tokens * p.group : 0);
+  const int last = static_cast<int>(sp_div(base + sp_cost(dual, key_tiles) - 1, chunk));
   for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
     // (a range's end may lie past the axis' end: no tile does)
-    const bool piece = c <= last && sp_tile_at((c + 1) * chunk, base, dual, x.key_tiles) >
-                                        sp_tile_at(c * chunk, base, dual, x.key_tiles);
+    const int t0 = sp_tile_at(c * chunk, base, dual, key_tiles);
+    // (of a pair of heads: a tile of this one)
+    const bool piece = c <= last && sp_tile_at((c + 1) * chunk, base, dual, key_tiles) > t0 + (duo ? (t0 ^ second) & 1 : 0);
     const unsigned in = __ballot_sync(0xffffffffu, piece);
     if (piece) list[n + __popc(in & ((1u << lane) - 1u))] = slot + 2u * kSpTile * c;
     n += __popc(in);
@@ -1026,11 +1051,11 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
       if (rec.pre_keys > 0) {
         const SpEntity px = sp_entity(p, false, rec.first, rec.sequences, rec.pre_keys);
         if (tile < px.tiles) {
-          n = sp_list(rec.chunk, p, rec.pre_cost, rec.pre_slot, px, h, tile, s_list[warp], 0);
+          n = sp_list(rec.chunk, p, rec.pre_cost, rec.pre_slot, px, false, h, tile, s_list[warp], 0);
           rows = sp_rows(p, px, tile);
         }
       }
-      const int all = sp_list(rec.chunk, p, rec.cost, rec.slot, sp_entity(p, true, b, 1, rec.keys), h, 0, s_list[warp], n);
+      const int all = sp_list(rec.chunk, p, rec.cost, rec.slot, sp_entity(p, true, b, 1, rec.keys), true, h, 0, s_list[warp], n);
       s_pre[warp] = n;
       s_all[warp] = all;
       s_rows[warp] = rows;
@@ -1114,7 +1139,7 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
   const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
   SpBounds b;
   b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostOne + B * (kSpCostSeg + own_tiles * kSpCostOne));
-  b.rows = H_kv * (pairs * 2 * kSpTile + tokens * group) + 2LL * kSpTile * G;
+  b.rows = H_kv * pairs * 2 * kSpTile + (H_kv + 1) * tokens * group + 2LL * kSpTile * G;
   return b;
 }
 
