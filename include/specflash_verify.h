@@ -539,8 +539,8 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
 /* Accuracy: scores and softmax statistics in fp32, the softmax weights in   */
 /* bf16 for the product with V (each rounded by at most 2^-8 of itself; over */
 /* many keys that averages out below the rounding of the bf16 output, and    */
-/* where a row may see fewer than 128 keys besides a segment's, that          */
-/* segment's first 128 weights are carried in two bf16 terms).  A NaN or an  */
+/* where a row sees fewer than 128 keys in all, and on prefixes of fewer     */
+/* than 128 keys, the weights are carried in two bf16 terms).  A NaN or an   */
 /* infinity in V reaches every row of the sequence's draft block, later       */
 /* draft positions included: a weight of 0 times NaN is NaN.  Deterministic. */
 /* ------------------------------------------------------------------------ */

@@ -21,7 +21,7 @@
 // query row a thread), a score buffer and an accumulator:
 //     TMEM columns  S_0 [0, 128)  S_1 [128, 256)  O_0 [256, 384)  O_1 [384, 512).
 // A piece with two row tiles gives one to each stream, and so does one with two heads
-// (59 sequences of 212 to 916 own tokens, 32 heads: @TWO, against 138 us with a
+// (59 sequences of 212 to 916 own tokens, 32 heads, a prefix of 128: 110 us, 138 with a
 // piece per head); a piece with one row tile gives its even key tiles to stream 0 and
 // its odd ones to stream 1, whose results are joined in the CTA, or, with one key
 // tile, goes to the streams in turn.  So
@@ -36,11 +36,11 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 194 to 204 us, 1.2 PFLOP/s): the MMAs.  A key tile of two row tiles is
+// 32768 tokens: 190 us, 1.3 PFLOP/s): the MMAs.  A key tile of two row tiles is
 // 32 of them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K,
 // V and the copies together read and write shared memory at its full 128 bytes a
 // cycle; a tile takes 2,800 cycles with what the turns leave idle.  One row tile (8
-// sequences of 5 rows, 32 / 32 heads, 3008 tokens: 26 us for 62.5 MB, 2.4 TB/s) and
+// sequences of 5 rows, 32 / 32 heads, 3008 tokens: 25 us for 62.5 MB, 2.5 TB/s) and
 // few keys: the start (the cut of the axis takes 3 us from cold instructions, the
 // first keys 2), the partials' way through L2 and the merge kernel (5 us behind the
 // last piece).
@@ -49,8 +49,8 @@
 // exceeds it by more than kSpRescaleLog2, so rescaling O is rare.  The row sums
 // are sums of the fp32 weights.  P V takes the weights rounded to bf16 (up to 2^-8
 // of a weight, which averages out over many keys), and where rows may see fewer
-// than 128 keys outside a segment, on the segment's first key tile also what that
-// rounding left, as a second bf16 term.
+// than 128 keys in all, on a segment's first key tile also what that rounding left, as
+// a second bf16 term.
 // Every wait is bounded; a timeout sets SF_DEVICE_TIMEOUT and stops every role.
 #include <cmath>
 #include <mutex>
@@ -70,12 +70,15 @@ constexpr float kSpRescaleLog2 = 8.f;
 constexpr int kSpMergeThreads = 256;
 constexpr int kSpSmemMax = 227 * 1024;
 // Cost of a segment on the partition's axis: kSpCostOne or kSpCostTwo for each of its
-// key tiles (one row tile, or two), and kSpCostSeg for itself (its Q copy, pipeline
-// start and epilogue).  Measured, least squares over the CTAs of three workloads: 1.3
-// to 1.5 us for a key tile of two row tiles, 0.9 to 1.8 of one, 2 to 4 for a piece.
-// With one unit for every row tile's key tile and two a segment the longest CTA of
-// the workload of 64 sequences took 18 % more than the mean (225 us, now 195).
-constexpr uint32_t kSpCostSeg = 5, kSpCostOne = 3, kSpCostTwo = 4;
+// key tiles (one row tile, or two), and kSpCostSegOne or kSpCostSegTwo for itself (its Q
+// copy, pipeline start and epilogue; two row tiles leave 128 KB of partial results),
+// with kSpCostFew more for weights in two terms.  Measured, least squares over the CTAs
+// of three workloads: 1.3 to 1.5 us for a key tile of two row tiles, 0.9 to 1.8 of one,
+// 2 to 4 for a piece.  With one unit for every row tile's key tile and two a segment the
+// longest CTA of the workload of 64 sequences took 18 % more than the mean (225 us, now
+// 190); with 5 for either kind of segment, 59 sequences of some 560 tokens with a prefix
+// of 8 took 174 us (now 119): a few CTAs had all the prefix's segments.
+constexpr uint32_t kSpCostSegOne = 5, kSpCostSegTwo = 10, kSpCostFew = 4, kSpCostOne = 3, kSpCostTwo = 4;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
 constexpr int kSpItems = 4;      // pieces published ahead
 
@@ -117,7 +120,19 @@ struct SpEntity {
   uint32_t head_cost;  // per unit
   uint32_t cost;       // of all units
   uint32_t slot_rows;  // partial rows of one piece
-  __device__ __forceinline__ uint32_t pair_cost() const { return kSpCostSeg + kSpCostTwo * static_cast<uint32_t>(key_tiles); }
+  uint32_t few;        // a first key tile with two terms
+  // of a segment: its start, and its length for key tiles of which some may be other heads'
+  __device__ __forceinline__ uint32_t start(int dual) const { return (dual ? kSpCostSegTwo : kSpCostSegOne) + few; }
+  __device__ __forceinline__ uint32_t length(int dual, int tiles_) const {
+    return start(dual) + (dual ? kSpCostTwo : kSpCostOne) * static_cast<uint32_t>(tiles_);
+  }
+  // its first key tile at or behind position at of the axis
+  __device__ __forceinline__ int tile_at(uint32_t at, uint32_t base, int dual, int tiles_) const {
+    const uint32_t b = base + start(dual);
+    if (at <= b) return 0;
+    const uint32_t t = dual ? (at - b + kSpCostTwo - 1) / kSpCostTwo : (at - b + kSpCostOne - 1) / kSpCostOne;
+    return t < static_cast<uint32_t>(tiles_) ? static_cast<int>(t) : tiles_;
+  }
 };
 
 // n / tokens_per_tile for n < 2^25 (tile_magic = ceil(2^32 / tokens_per_tile))
@@ -133,16 +148,15 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
   x.tiles = own ? 1 : sp_tiles(p, x.tokens + p.tokens_per_tile - 1);
   x.pairs = (x.tiles + 1) >> 1;
   x.key_tiles = (keys + kSpTile - 1) / kSpTile;
-  const uint32_t key_tiles = static_cast<uint32_t>(x.key_tiles);
+  x.few = !own && keys < kSpTile ? kSpCostFew : 0u;
   if (own) {
     x.units = (p.H_kv + 1) >> 1;
-    x.head_cost = kSpCostSeg + 2u * kSpCostOne * key_tiles;
-    x.cost = x.units * x.head_cost - (p.H_kv & 1) * kSpCostOne * key_tiles;
+    x.head_cost = x.length(0, 2 * x.key_tiles);
+    x.cost = x.units * x.head_cost - (p.H_kv & 1) * kSpCostOne * static_cast<uint32_t>(x.key_tiles);
     x.slot_rows = 2u * static_cast<uint32_t>(x.tokens * p.group);
   } else {
     x.units = p.H_kv;
-    x.head_cost = static_cast<uint32_t>(x.pairs) * kSpCostSeg +
-                  key_tiles * (kSpCostTwo * static_cast<uint32_t>(x.tiles >> 1) + kSpCostOne * (x.tiles & 1));
+    x.head_cost = static_cast<uint32_t>(x.tiles >> 1) * x.length(1, x.key_tiles) + (x.tiles & 1) * x.length(0, x.key_tiles);
     x.cost = x.units * x.head_cost;
     x.slot_rows = x.tiles > 1 ? 2u * kSpTile : static_cast<uint32_t>(x.tokens * p.group);
   }
@@ -163,19 +177,6 @@ __device__ __forceinline__ uint32_t sp_div(uint32_t a, uint32_t b) {
   if (q * b > a) --q;
   if ((q + 1u) * b <= a) ++q;
   return q;
-}
-
-// First key tile of a segment at or behind position x of the axis.
-__device__ __forceinline__ int sp_tile_at(uint32_t x, uint32_t base, int dual, int key_tiles) {
-  const uint32_t b = base + kSpCostSeg;
-  if (x <= b) return 0;
-  const uint32_t t = dual ? (x - b + kSpCostTwo - 1) / kSpCostTwo : (x - b + kSpCostOne - 1) / kSpCostOne;
-  return t < static_cast<uint32_t>(key_tiles) ? static_cast<int>(t) : key_tiles;
-}
-
-// Length of a segment on the axis.
-__device__ __forceinline__ uint32_t sp_cost(int dual, int key_tiles) {
-  return kSpCostSeg + (dual ? kSpCostTwo : kSpCostOne) * static_cast<uint32_t>(key_tiles);
 }
 
 __device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int tile) {
@@ -434,8 +435,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       x = entity(e);
       const uint32_t in = at - e_cost;
       h = static_cast<int>(sp_div(in, x.head_cost));
-      pair = x.pairs > 1 ? static_cast<int>(sp_div(in - h * x.head_cost, x.pair_cost())) : 0;
-      base = e_cost + h * x.head_cost + pair * x.pair_cost();
+      pair = x.pairs > 1 ? static_cast<int>(sp_div(in - h * x.head_cost, x.length(1, x.key_tiles))) : 0;
+      base = e_cost + h * x.head_cost + pair * x.length(1, x.key_tiles);
       slot = e_slot + (h * x.pairs + pair) * x.slot_rows + 2u * kSpTile * c;
     }
     const uint64_t again = l2_policy_evict_last();
@@ -453,8 +454,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       while (it.n == 0 && e < E && base < end) {
         const bool own = e >= p.num_groups;
         const int dual = 2 * pair + 1 < x.tiles, duo = own && 2 * h + 1 < p.H_kv, key_tiles = x.key_tiles << duo;
-        it.t0 = sp_tile_at(at, base, dual, key_tiles);
-        it.n = sp_tile_at(end, base, dual, key_tiles) - it.t0;
+        it.t0 = x.tile_at(at, base, dual, key_tiles);
+        it.n = x.tile_at(end, base, dual, key_tiles) - it.t0;
         if (it.n > 0) {
           it.keys = x.keys;
           it.own = own;
@@ -504,7 +505,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           if (!dual && !duo && it.n == 1) turn ^= 1;
         }
         // the next segment
-        base += sp_cost(dual, key_tiles);
+        base += x.length(dual, key_tiles);
         slot += x.slot_rows;
         if (++pair == x.pairs) {
           pair = 0;
@@ -1013,15 +1014,15 @@ __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32
   if (x.head_cost == 0) return n;
   const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
   const int duo = own && (h | 1) < p.H_kv, second = h & 1, unit = own ? h >> 1 : h, key_tiles = x.key_tiles << duo;
-  const uint32_t base = cost + unit * x.head_cost + pair * x.pair_cost();
+  const uint32_t base = cost + unit * x.head_cost + pair * x.length(1, x.key_tiles);
   slot += (unit * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : duo ? second * x.tokens * p.group : 0);
-  const int last = static_cast<int>(sp_div(base + sp_cost(dual, key_tiles) - 1, chunk));
+  const int last = static_cast<int>(sp_div(base + x.length(dual, key_tiles) - 1, chunk));
   for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
     // (a range's end may lie past the axis' end: no tile does)
-    const int t0 = sp_tile_at(c * chunk, base, dual, key_tiles);
+    const int t0 = x.tile_at(c * chunk, base, dual, key_tiles);
     // (of a pair of heads: a tile of this one)
-    const bool piece = c <= last && sp_tile_at((c + 1) * chunk, base, dual, key_tiles) > t0 + (duo ? (t0 ^ second) & 1 : 0);
+    const bool piece = c <= last && x.tile_at((c + 1) * chunk, base, dual, key_tiles) > t0 + (duo ? (t0 ^ second) & 1 : 0);
     const unsigned in = __ballot_sync(0xffffffffu, piece);
     if (piece) list[n + __popc(in & ((1u << lane) - 1u))] = slot + 2u * kSpTile * c;
     n += __popc(in);
@@ -1138,7 +1139,7 @@ static SpBounds sp_bounds(int B, int n_q, int H_q, int H_kv, int num_groups, int
   // at most half of that plus one pairs, of at most 2 * kSpTile partial rows each
   const long long tiles = tokens / per_tile + num_groups, pairs = tokens / (2 * per_tile) + num_groups;
   SpBounds b;
-  b.cost = H_kv * (pairs * kSpCostSeg + tiles * prefix_tiles * kSpCostOne + B * (kSpCostSeg + own_tiles * kSpCostOne));
+  b.cost = H_kv * (pairs * (kSpCostSegTwo + kSpCostFew) + tiles * prefix_tiles * kSpCostOne + B * (kSpCostSegOne + own_tiles * kSpCostOne));
   b.rows = H_kv * pairs * 2 * kSpTile + (H_kv + 1) * tokens * group + 2LL * kSpTile * G;
   return b;
 }
