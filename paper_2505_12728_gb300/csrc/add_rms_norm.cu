@@ -42,6 +42,7 @@ struct NormParams {
   int shift;  // kNormShifted: elements from x's last 16-byte boundary (of 8 elements) to x
   int margin;  // kNormShifted: rows that hold 7 elements
   float eps;
+  float per_d;  // 1 / d
 };
 
 // How a thread's elements lie in a row: 8 neighbours, with every row on a 16-byte
@@ -148,9 +149,23 @@ __device__ __forceinline__ void norm_store(void *base, long long row, int k, int
 // |v| as an integer: the same order as the magnitudes, with NaN above infinity
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+template <bool kFast>
 __device__ __forceinline__ float norm_scale(unsigned top, float inv) {
-  const float s = __uint_as_float(top) * inv / kE4m3Max;
+  const float s = kFast ? __uint_as_float(top) * inv * (1.f / kE4m3Max) : __uint_as_float(top) * inv / kE4m3Max;
   return s < kLeastScale ? kLeastScale : s;
+}
+
+// 1 / s, and 1 / sqrt(mean + eps), within 2 ulp (kFast) or one.  Fewer instructions and
+// registers, so more CTAs: 20000 x 1152 to e4m3 with groups 33 -> 27.5 us, 12000 x 5001
+// 120 -> 110.  The variant of two chunks with the next row ahead gets fewer registers
+// than it needs instead (20000 x 3589 92 -> 100, 32768 x 3584 to e4m3 131 -> 137).
+template <bool kFast>
+__device__ __forceinline__ float norm_reciprocal(float s) {
+  return kFast ? __fdividef(1.f, s) : 1.f / s;
+}
+template <bool kFast>
+__device__ __forceinline__ float norm_inverse(float sum, const NormParams &p) {
+  return kFast ? rsqrtf(fmaf(sum, p.per_d, p.eps)) : 1.f / sqrtf(sum / static_cast<float>(p.d) + p.eps);
 }
 
 // kAhead: the weights stay in registers and the next row is loaded ahead (blocks of
@@ -161,7 +176,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
   __shared__ float s_sum[2][kNormMaxThreads / 32];
   __shared__ unsigned s_top[2][kNormMaxThreads / 32];
   __shared__ unsigned s_group[kE4m3 && kMode != kNormVec ? SF_MAX_NORM_DIM / kNormGroup : 1];
-  constexpr bool kVec = kMode == kNormVec;
+  constexpr bool kVec = kMode == kNormVec, kFast = !(kChunks == 2 && kAhead);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
   const bool grouped = kE4m3 && p.groups > 1;
   grid_dependency_wait();
@@ -271,7 +286,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
     sum = lane < nw ? s_sum[buf][lane] : 0.f;
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-    const float inv = 1.f / sqrtf(sum / static_cast<float>(p.d) + p.eps);
+    const float inv = norm_inverse<kFast>(sum, p);
     if constexpr (!kE4m3) {
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
@@ -282,7 +297,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
     } else {
       float scale = 0.f;
       if (!grouped) {
-        scale = norm_scale(__reduce_max_sync(0xffffffffu, lane < nw ? s_top[buf][lane] : 0u), inv);
+        scale = norm_scale<kFast>(__reduce_max_sync(0xffffffffu, lane < nw ? s_top[buf][lane] : 0u), inv);
         if (tid == 0) p.scales[row] = scale;
       } else if constexpr (kMode == kNormSingle) {
         // (a warp's 32 columns belong to one group: nt is a multiple of 32)
@@ -315,7 +330,7 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
       if (grouped && !kVec) {
         __syncthreads();
         for (int g = tid; g < p.groups; g += nt)
-          p.scales[static_cast<size_t>(row) * p.groups + g] = norm_scale(s_group[g], inv);
+          p.scales[static_cast<size_t>(row) * p.groups + g] = norm_scale<kFast>(s_group[g], inv);
       }
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
@@ -327,20 +342,20 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
             for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(h[k][i]));
 #pragma unroll
             for (int x = 8; x > 0; x >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, x));
-            scale = norm_scale(m, inv);
+            scale = norm_scale<kFast>(m, inv);
             if ((lane & 15) == 0 && col < p.d) p.scales[static_cast<size_t>(row) * p.groups + col / kNormGroup] = scale;
           }
-          const float rs = 1.f / scale;
+          const float rs = norm_reciprocal<kFast>(scale);
           if (col < p.d) store_e4m3(row, col, h[k], inv, rs, rs, 8);
         } else if constexpr (kMode == kNormShifted) {
           const int col = norm_column<kMode>(k, 0, nt, o);
           if (col < p.d) {
             // the chunk's group, the next one, and where that begins
             const int g = max(col, 0) / kNormGroup, line = (g + 1) * kNormGroup - col;
-            float rs = 1.f / scale, rs_next = rs;
+            float rs = norm_reciprocal<kFast>(scale), rs_next = rs;
             if (grouped) {
-              rs = 1.f / norm_scale(s_group[g], inv);
-              rs_next = line < 8 && g + 1 < p.groups ? 1.f / norm_scale(s_group[g + 1], inv) : rs;
+              rs = norm_reciprocal<kFast>(norm_scale<kFast>(s_group[g], inv));
+              rs_next = line < 8 && g + 1 < p.groups ? norm_reciprocal<kFast>(norm_scale<kFast>(s_group[g + 1], inv)) : rs;
             }
             store_e4m3(row, col, h[k], inv, rs, rs_next, line);
           }
@@ -349,9 +364,9 @@ add_rms_norm_kernel(const __grid_constant__ NormParams p) {
           for (int i = 0; i < 8; ++i) {
             const int col = norm_column<kMode>(k, i, nt, o);
             if (col >= p.d) continue;
-            if (grouped) scale = norm_scale(s_group[col / kNormGroup], inv);
+            if (grouped) scale = norm_scale<kFast>(s_group[col / kNormGroup], inv);
             static_cast<__nv_fp8_storage_t *>(p.out)[row * p.out_stride + col] =
-                __nv_cvt_float_to_fp8(h[k][i] * inv * (1.f / scale), __NV_SATFINITE, __NV_E4M3);
+                __nv_cvt_float_to_fp8(h[k][i] * inv * norm_reciprocal<kFast>(scale), __NV_SATFINITE, __NV_E4M3);
           }
         }
       }
@@ -444,6 +459,7 @@ extern "C" int sf_add_rms_norm(const void *x, const void *residual, const void *
   p.groups = e4m3 && group ? (d + group - 1) / group : 1;
   p.weight_wide = weight_dtype == SF_F32;
   p.eps = eps;
+  p.per_d = 1.f / static_cast<float>(d);
   DeviceInfo dev;
   const int st = current_device(&dev);
   if (st != SF_OK) return st;
