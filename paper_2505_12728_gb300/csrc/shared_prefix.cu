@@ -24,8 +24,8 @@
 // (59 sequences of 212 to 916 own tokens, 32 heads, a prefix of 128: 110 us, 138 with a
 // piece per head); a piece with one row tile gives its even key tiles to stream 0 and
 // its odd ones to stream 1, whose results are joined in the CTA, or, with one key
-// tile, goes to the streams in turn.  So
-// while one stream's softmax runs, the tensor cores work for the other.
+// tile, goes to the streams in turn.  So while one stream's softmax runs, the tensor
+// cores work for the other.
 // P = exp2(S') goes back over the scores as bf16 (the A operand of O += P V), so
 // a stream's next Q K^T is issued behind its P V; tcgen05 MMAs of one thread
 // execute in issue order.  Each stream has a warp that issues its MMAs (one warp
@@ -36,7 +36,7 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 190 us, 1.3 PFLOP/s): the MMAs.  A key tile of two row tiles is
+// 32768 tokens: 190 to 201 us, 1.2 to 1.3 PFLOP/s): the MMAs.  A key tile of two row tiles is
 // 32 of them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K,
 // V and the copies together read and write shared memory at its full 128 bytes a
 // cycle; a tile takes 2,800 cycles with what the turns leave idle.  One row tile (8
