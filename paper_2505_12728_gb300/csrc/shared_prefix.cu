@@ -52,6 +52,7 @@
 // than 128 keys in all, on a segment's first key tile also what that rounding left, as
 // a second bf16 term.
 // Every wait is bounded; a timeout sets SF_DEVICE_TIMEOUT and stops every role.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -332,12 +333,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     // ------------------------------------------------------------------
     // The CTA's pieces, published one after the other, each followed by the
     // copies of its Q tiles as soon as the streams' last Q K^T have read theirs.
+    // Loops up to the first piece stay loops: their instructions come from L2, and
+    // unrolled they cost a call of few keys 0.3 to 0.6 us of some 14.
     // ------------------------------------------------------------------
     const int E = p.num_groups + p.B;
     int *s_len = reinterpret_cast<int *>(smem + L::kPlanOffset), *s_start = s_len + E;
     uint32_t *s_cost = reinterpret_cast<uint32_t *>(s_start + p.num_groups + 1), *s_slot = s_cost + p.num_groups;
     bool bad = false;
-#pragma unroll 4
+#pragma unroll 1
     for (int e = lane; e <= E; e += 32) {
       const bool own = e >= p.num_groups;
       int n = 0, s = 0;
@@ -355,6 +358,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       }
     }
     __syncwarp();
+#pragma unroll 1
     for (int g = lane; g < p.num_groups; g += 32) bad |= s_start[g + 1] < s_start[g];
     if (__any_sync(0xffffffffu, bad)) {  // malformed groups: no sequence has a prefix
       for (int g = lane; g <= p.num_groups; g += 32) s_start[g] = 0;
@@ -368,6 +372,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     };
     auto group_of = [&](int b) -> int {  // the last group that starts at or before sequence b
       int lo = 0, hi = p.num_groups;
+#pragma unroll 1
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (s_start[mid] <= b) lo = mid; else hi = mid;
@@ -375,6 +380,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       return lo;
     };
     uint32_t sum = 0;
+#pragma unroll 1
     for (int e = lane; e < E; e += 32) sum += entity(e).cost;
     const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum), chunk = sp_chunk(p, Tot);
     const uint32_t c = blockIdx.x;
@@ -383,6 +389,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     // the entity that position `at` lies in, with the costs and partial rows before it
     int e = E;
     uint32_t e_cost = 0, e_slot = 0, cost = 0, slot = 0;
+#pragma unroll 1
     for (int e0 = 0; e0 < E && (e == E || writes); e0 += 32) {
       const int k = e0 + lane;
       SpEntity x{};
@@ -511,6 +518,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           pair = 0;
           if (++h == x.units) {
             h = 0;
+#pragma unroll 1
             do x = ++e < E ? entity(e) : x;
             while (e < E && x.head_cost == 0);  // entities without keys or rows
           }
@@ -1005,6 +1013,21 @@ struct SpJoin {
     }
     M = top;
   }
+  // what the lanes at distance `lanes` have joined, too (both sides alike)
+  __device__ __forceinline__ void add_lanes(int lanes) {
+    const float m = __shfl_xor_sync(0xffffffffu, M, lanes), l = __shfl_xor_sync(0xffffffffu, L, lanes);
+    const float x = __shfl_xor_sync(0xffffffffu, acc.x, lanes), y = __shfl_xor_sync(0xffffffffu, acc.y, lanes);
+    const float z = __shfl_xor_sync(0xffffffffu, acc.z, lanes), w = __shfl_xor_sync(0xffffffffu, acc.w, lanes);
+    const float top = fmaxf(M, m);
+    if (top == -INFINITY) return;
+    const float a = fast_exp2(M - top), b = fast_exp2(m - top);
+    L = L * a + l * b;
+    acc.x = acc.x * a + x * b;
+    acc.y = acc.y * a + y * b;
+    acc.z = acc.z * a + z * b;
+    acc.w = acc.w * a + w * b;
+    M = top;
+  }
 };
 
 // Appends the first partial rows of a row tile's partials of one segment to
@@ -1030,7 +1053,8 @@ __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32
   return n;
 }
 
-template <int D>
+// kWays threads an output quad, every kWays-th batch of its partials each.
+template <int D, int kWays>
 __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(const __grid_constant__ SpParams p) {
   constexpr float kLn2 = 0.6931471805599453f;
   constexpr int C4 = D / 4;
@@ -1063,7 +1087,12 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     }
     __syncthreads();
   }
-  for (int item = blockIdx.y * kSpMergeThreads + tid; item < per; item += gridDim.y * kSpMergeThreads) {
+  constexpr int kItems = kSpMergeThreads / kWays, kLanes = 32 / kWays;  // quads of a block, and of a warp, at a time
+  const int way = (tid & 31) / kLanes;
+  for (int first = blockIdx.y * kItems; first < per; first += gridDim.y * kItems) {
+    const int item = first + warp * kLanes + (tid & (kLanes - 1));
+    const bool live = item < per;
+    if (kWays == 1 && !live) break;
     const int c4 = item / R, r = item - c4 * R, i = r / p.group, j = r - i * p.group;
     const size_t row = (static_cast<size_t>(b) * p.n_q + i) * p.H_q + static_cast<size_t>(h) * p.group + j;
     SpJoin jn;
@@ -1074,8 +1103,8 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     if (rec.keys > 0) {
       const int sel = (tok0 + i >= (tile0 + 1) * p.tokens_per_tile);
       const int row_pre = (tok0 + i - (tile0 + sel) * p.tokens_per_tile) * p.group + j;
-      const int pre = s_pre[sel], all = s_all[sel], rows_pre = s_rows[sel];
-      for (int k0 = 0; k0 < all; k0 += kSpJoinBatch) {
+      const int pre = s_pre[sel], all = live ? s_all[sel] : 0, rows_pre = s_rows[sel];
+      for (int k0 = way * kSpJoinBatch; k0 < all; k0 += kWays * kSpJoinBatch) {
         float2 ml[kSpJoinBatch];
         float4 o[kSpJoinBatch];
 #pragma unroll
@@ -1092,8 +1121,11 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
         }
         jn.add(ml, o);
       }
+#pragma unroll
+      for (int lanes = kLanes; lanes < 32; lanes *= 2) jn.add_lanes(lanes);
       inv = 1.f / jn.L;
     }
+    if (kWays > 1 && (!live || way > 0)) continue;
     uint2 packed;
     packed.x = pack_bf16x2(jn.acc.x * inv, jn.acc.y * inv);
     packed.y = pack_bf16x2(jn.acc.z * inv, jn.acc.w * inv);
@@ -1331,14 +1363,26 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix attention launch: %s", cudaGetErrorString(e));
   // one block per sequence and KV head, its rows over several where that leaves
   // SMs without one
-  const int per = (n_q * p.group * (head_dim / 4) + kSpMergeThreads - 1) / kSpMergeThreads;
+  // and, where its rows may have more than two batches of partials and four threads an
+  // output quad still leave SMs without a second block, each list over four threads
+  // (one sequence of 6 rows, 4 KV heads of 64, 14000 tokens, 38 partials a row: 18.7 ->
+  // 15.5 us; with at most 8 partials 10.9 -> 11.9, with more blocks, as for 8 sequences of
+  // 5 rows and 32 heads, 24.8 -> 27.7).
+  const int quads = n_q * p.group * (head_dim / 4);
+  auto partials = [&](int pages, int segments) { return std::min((pages + kSpTilePages - 1) / kSpTilePages, G / segments + 1); };
+  const bool wide = std::max(partials(max_prefix_pages, num_groups * H_kv), partials(max_pages_per_seq, B * H_kv)) >
+                        2 * kSpJoinBatch &&
+                    static_cast<long long>(B) * H_kv * ((quads * 4 + kSpMergeThreads - 1) / kSpMergeThreads) <= 2 * G;
+  const int per = ((wide ? 4 : 1) * quads + kSpMergeThreads - 1) / kSpMergeThreads;
   int parts = (4 * G + B * H_kv - 1) / (B * H_kv);
   if (parts > per) parts = per;
   cfg.gridDim = dim3(static_cast<unsigned>(B * H_kv), static_cast<unsigned>(parts));
   cfg.blockDim = dim3(kSpMergeThreads);
   cfg.dynamicSmemBytes = 0;
-  e = head_dim == 128 ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128>, p)
-                      : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64>, p);
+  e = head_dim == 128 ? (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 4>, p)
+                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 1>, p))
+                      : (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 4>, p)
+                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 1>, p));
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix merge launch: %s", cudaGetErrorString(e));
   return SF_OK;
 }

@@ -287,3 +287,21 @@ def test_refusals():
     assert e.value.status == 4
     with pytest.raises(sfv.SFError, match="softmax_scale"):
         sfv.shared_prefix_attention(*args, softmax_scale=-1.0)
+
+
+# few rows, long parts: many partials a row (lists over several threads), an odd and a
+# single KV head among them, the long part shared or a sequence's own
+@pytest.mark.parametrize("prefix, own, n, H_q, H_kv, d", [
+    (9000, 15, 6, 16, 4, 64), (6100, 9, 1, 3, 3, 128), (5003, 20, 3, 8, 1, 128), (70, 6007, 4, 6, 2, 64), (0, 7011, 16, 5, 5, 128)])
+def test_many_partials_a_row(prefix, own, n, H_q, H_kv, d):
+    check([1], [prefix], [own], n, H_q, H_kv, d, seed=prefix + own)
+    check([2], [prefix], [own, 0], n, H_q, H_kv, d, seed=prefix + own + 1)
+
+
+# own tokens of two KV heads side by side: one, two and many key tiles, with an odd
+# number of heads, cut between and inside the pairs
+@pytest.mark.parametrize("H_q, H_kv, d", [(3, 3, 128), (2, 2, 64), (10, 5, 64), (7, 1, 128), (32, 32, 64)])
+@pytest.mark.parametrize("lens", [[128, 140], [129, 1, 300], [127, 640, 16, 255, 1000, 17]])
+def test_own_tokens_of_pairs_of_heads(H_q, H_kv, d, lens):
+    check([len(lens)], [0], lens, 1, H_q, H_kv, d, seed=sum(lens))
+    check([1, len(lens) - 1], [40, 260], [x + 3 for x in lens], 4, H_q, H_kv, d, seed=sum(lens) + 1)
