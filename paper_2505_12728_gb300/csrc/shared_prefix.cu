@@ -787,13 +787,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll
           for (int i = 0; i < 64; ++i) sv[64 * q + i] = part[i];
         }
+        // V rows of the last page past the end hold whatever the page holds: zeros
+        // there, so that 0 * v stays 0 (whole pages past the end are zeros already).
+        // In front of the weights' release, as V may come behind the scores.
         const int valid_keys = keys - tile_pos;
-        if (valid_keys < kSpTile && (valid_keys & (SF_PAGE_SIZE - 1)) != 0) {
-          // V rows of the last page past the end hold whatever the page holds:
-          // zeros there, so that 0 * v stays 0 (whole pages past the end are
-          // zeros already)
+        auto zero_tail = [&]() -> bool {
+          if (valid_keys >= kSpTile || (valid_keys & (SF_PAGE_SIZE - 1)) == 0) return true;
           const uint32_t pos = 2u * ring_tile + 1u, slot = pos % STAGES;
-          if (!(ok = wwait(bar(FULL + slot), (pos / STAGES) & 1u))) break;
+          if (!wwait(bar(FULL + slot), (pos / STAGES) & 1u)) return false;
           uint8_t *vt = smem + slot * L::kTileBytes + (valid_keys / SF_PAGE_SIZE) * kPageBytes;
           const int tok0 = valid_keys & (SF_PAGE_SIZE - 1);
           for (int idx = r; idx < (SF_PAGE_SIZE - tok0) * HALVES * 8; idx += 128) {
@@ -802,7 +803,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                 make_uint4(0u, 0u, 0u, 0u);
           }
           fence_proxy_async_smem();
-        }
+          return true;
+        };
         if (tile_pos + kSpTile - 1 > lim) {
 #pragma unroll
           for (int i = 0; i < 128; ++i)
@@ -856,6 +858,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             }
             tmem_st_32x32b_x16(ts + 16 * ch, w);
             if (ch == 1) {  // P V of the first 64 keys may begin
+              if (!(ok = zero_tail())) break;
               tmem_wait_st();
               tc_fence_before_sync();
               __syncwarp();
@@ -864,6 +867,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
           sp_unpair(sum, sum0, sum1);
         } else {
+          if (!(ok = zero_tail())) break;
           // A first key tile with two terms: what P's rounding to bf16 left goes to
           // columns [64, 128) as a second term.  The scores are read again, 64 at a
           // time, so that the two terms need no more registers than the scores do
@@ -899,6 +903,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             tmem_st_32x32b_x16(ts + x, w);
           }
         }
+        if (!ok) break;
         l_run = l_run * alpha + (sum0 + sum1);
         tmem_wait_st();
         tc_fence_before_sync();
