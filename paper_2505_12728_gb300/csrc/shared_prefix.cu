@@ -36,14 +36,14 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 190 to 201 us, 1.2 to 1.3 PFLOP/s): the MMAs.  A key tile of two row tiles is
-// 32 of them; they take 74 cycles each, not the 64 of the tensor cores' rate, as Q, K,
-// V and the copies together read and write shared memory at its full 128 bytes a
-// cycle; a tile takes 2,800 cycles with what the turns leave idle.  One row tile (8
-// sequences of 5 rows, 32 / 32 heads, 3008 tokens: 25 us for 62.5 MB, 2.5 TB/s) and
-// few keys: the start (the cut of the axis takes 3 us from cold instructions, the
-// first keys 2), the partials' way through L2 and the merge kernel (5 us behind the
-// last piece).
+// 32768 tokens: 177 to 190 us, 1.3 to 1.4 PFLOP/s, 13 of them the merge): the MMAs.  A
+// key tile of two row tiles is 32 of them; they take 74 cycles each, not the 64 of the
+// tensor cores' rate, as Q, K, V and the copies together read and write shared memory
+// at its full 128 bytes a cycle; a tile takes 2,550 cycles with what the turns leave
+// idle.  One row tile (8 sequences of 5 rows, 32 / 32 heads, 3008 tokens: 24 us for 62.5
+// MB, 2.6 TB/s) and few keys: the start (the cut of the axis takes 3 us from cold
+// instructions, the first keys 2), the partials' way through L2 and the merge kernel
+// (5 us behind the last piece).
 //
 // The running maximum is a reference that moves when a row's new maximum
 // exceeds it by more than kSpRescaleLog2, so rescaling O is rare.  The row sums
@@ -76,8 +76,8 @@ constexpr int kSpSmemMax = 227 * 1024;
 // with kSpCostFew more for weights in two terms.  Measured, least squares over the CTAs
 // of three workloads: 1.3 to 1.5 us for a key tile of two row tiles, 0.9 to 1.8 of one,
 // 2 to 4 for a piece.  With one unit for every row tile's key tile and two a segment the
-// longest CTA of the workload of 64 sequences took 18 % more than the mean (225 us, now
-// 190); with 5 for either kind of segment, 59 sequences of some 560 tokens with a prefix
+// longest CTA of the workload of 64 sequences took 18 % more than the mean (225 us, with
+// the costs 195); with 5 for either kind of segment, 59 sequences of some 560 tokens with a prefix
 // of 8 took 174 us (now 119): a few CTAs had all the prefix's segments.
 constexpr uint32_t kSpCostSegOne = 5, kSpCostSegTwo = 10, kSpCostFew = 4, kSpCostOne = 3, kSpCostTwo = 4;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
