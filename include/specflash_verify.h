@@ -540,9 +540,9 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
 /* bf16 for the product with V (each rounded by at most 2^-8 of itself; over */
 /* many keys that averages out below the rounding of the bf16 output, and    */
 /* where a row sees fewer than 128 keys in all, and on prefixes of fewer     */
-/* than 128 keys, the weights are carried in two bf16 terms).  A NaN or an   */
-/* infinity in V reaches every row of the sequence's draft block, later       */
-/* draft positions included: a weight of 0 times NaN is NaN.  Deterministic. */
+/* than 128 keys, the weights are carried in two bf16 terms).  Infinities    */
+/* and NaN in K and V reach the rows that see them, and no others.           */
+/* Deterministic.                                                            */
 /* ------------------------------------------------------------------------ */
 size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_kv, int head_dim,
                                                  int num_groups, int max_prefix_pages,

@@ -97,6 +97,7 @@ struct __align__(16) SpRecord {
 
 struct SpParams {
   const int32_t *prefix_table, *prefix_lens, *group_starts, *block_table, *seq_lens;
+  const __nv_bfloat16 *v_cache;
   __nv_bfloat16 *out;
   float *lse;
   uint32_t *status;
@@ -215,7 +216,8 @@ struct SpSmem {
   static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word
   static constexpr int kItemOffset = kMiscOffset + 16;
   static constexpr int kMlOffset = kItemOffset + kSpItems * static_cast<int>(sizeof(SpItem));  // float2 [2][128]
-  static constexpr int kPlanOffset = kMlOffset + 2 * 8 * kSpTile;
+  static constexpr int kInfoOffset = kMlOffset + 2 * 8 * kSpTile;  // int [8 warps][8], int [2][2]
+  static constexpr int kPlanOffset = kInfoOffset + 8 * 32 + 16;
 };
 
 // max of three in one instruction (a NaN is ignored, as by fmaxf)
@@ -268,6 +270,10 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   auto bar = [&](int i) -> uint32_t { return ring + L::kBarOffset + 8u * static_cast<uint32_t>(i); };
   int *s_misc = reinterpret_cast<int *>(smem + L::kMiscOffset);
   volatile int *s_abort = s_misc + 1;
+  int *s_info = reinterpret_cast<int *>(smem + L::kInfoOffset);
+  // per stream and parity of its job (a warp may be a job ahead of another): the last
+  // piece with infinities or NaN among the draft's V
+  volatile int *s_bad = s_info + 64;
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
 
   if (tid == 0) {
@@ -297,6 +303,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     prefetch_tensormap(&tmap_q_tile);
     prefetch_tensormap(&tmap_q_own);
     s_misc[1] = 0;
+    for (int i = 0; i < 4; ++i) s_bad[i] = 0;
   }
   __syncthreads();
   grid_dependency_wait();
@@ -770,6 +777,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       int tile_pos = ((item->t0 + item->s[s].first) >> duo) * kSpTile;  // position of the tile's first key
       base += item->n;
       const bool valid = r < rows;
+      int *info = s_info + 8 * warp;
+      if (lane == 0) {
+        info[0] = item->own ? p.n_q - 1 : 0;  // draft rows that are masked for some rows
+        info[1] = item->row;
+        info[2] = item->h + (duo & s);
+        info[3] = tile_pos - (joint ? s * kSpTile : 0);  // the piece's first key, and the one behind its last
+        info[4] = joint ? (item->t0 + item->n) * kSpTile : tile_pos + n * kSpTile;
+      }
       // last visible key of this row (rows past the tile's end see every key:
       // their scores are not used)
       const int lim = !valid ? 0x7fffff00 : item->own ? keys - p.n_q + r / p.group : keys - 1;
@@ -787,20 +802,44 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll
           for (int i = 0; i < 64; ++i) sv[64 * q + i] = part[i];
         }
-        // V rows of the last page past the end hold whatever the page holds: zeros
-        // there, so that 0 * v stays 0 (whole pages past the end are zeros already).
-        // In front of the weights' release, as V may come behind the scores.
+        // What must not meet a weight of 0 (0 * NaN) is taken out of V: the rows of the
+        // last page past the end, which hold whatever the page holds (whole pages past
+        // the end are zeros already), and infinities and NaN of draft rows that are
+        // masked for the rows before them (spread_bad gives them to those that see
+        // them).  In front of the weights' release, as V may come behind the scores.
         const int valid_keys = keys - tile_pos;
-        auto zero_tail = [&]() -> bool {
-          if (valid_keys >= kSpTile || (valid_keys & (SF_PAGE_SIZE - 1)) == 0) return true;
+        auto clean_v = [&]() -> bool {
+          if (valid_keys >= kSpTile + SF_MAX_QUERY_ROWS - 1) return true;
+          const int tok0 = valid_keys & (SF_PAGE_SIZE - 1), from = max(valid_keys - info[0], 0), to_ = min(valid_keys, kSpTile);
+          const bool cut = valid_keys < kSpTile && tok0 != 0;
+          if (!cut && from >= to_) return true;
           const uint32_t pos = 2u * ring_tile + 1u, slot = pos % STAGES;
           if (!wwait(bar(FULL + slot), (pos / STAGES) & 1u)) return false;
-          uint8_t *vt = smem + slot * L::kTileBytes + (valid_keys / SF_PAGE_SIZE) * kPageBytes;
-          const int tok0 = valid_keys & (SF_PAGE_SIZE - 1);
-          for (int idx = r; idx < (SF_PAGE_SIZE - tok0) * HALVES * 8; idx += 128) {
-            const int tok = tok0 + idx / (HALVES * 8), rem = idx % (HALVES * 8);
-            *reinterpret_cast<uint4 *>(vt + (rem >> 3) * kPageHalfBytes + tok * kRowBytes + (rem & 7) * 16) =
-                make_uint4(0u, 0u, 0u, 0u);
+          uint8_t *vt = smem + slot * L::kTileBytes;
+          auto chunk = [&](int tok, int rem) -> uint4 * {  // 16 bytes of a row (in the order that the copy's swizzle leaves)
+            return reinterpret_cast<uint4 *>(vt + (tok / SF_PAGE_SIZE) * kPageBytes + (rem >> 3) * kPageHalfBytes +
+                                             (tok % SF_PAGE_SIZE) * kRowBytes + (rem & 7) * 16);
+          };
+          if (cut) {
+#pragma unroll 1
+            for (int idx = r; idx < (SF_PAGE_SIZE - tok0) * HALVES * 8; idx += 128)
+              *chunk(valid_keys + idx / (HALVES * 8), idx % (HALVES * 8)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll 1
+          for (int idx = r; idx < (to_ - from) * HALVES * 8; idx += 128) {
+            uint4 *at = chunk(from + idx / (HALVES * 8), idx % (HALVES * 8));
+            uint4 v = *at;
+            uint32_t kept = 0xffffffffu;
+            auto finite = [&](uint32_t w) -> uint32_t {
+              const uint32_t m = ((w & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+              kept &= m;
+              return w & m;
+            };
+            v = make_uint4(finite(v.x), finite(v.y), finite(v.z), finite(v.w));
+            if (kept != 0xffffffffu) {
+              *at = v;
+              s_bad[2 * s + (jobs & 1u)] = static_cast<int>(seen);
+            }
           }
           fence_proxy_async_smem();
           return true;
@@ -858,7 +897,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             }
             tmem_st_32x32b_x16(ts + 16 * ch, w);
             if (ch == 1) {  // P V of the first 64 keys may begin
-              if (!(ok = zero_tail())) break;
+              if (!(ok = clean_v())) break;
               tmem_wait_st();
               tc_fence_before_sync();
               __syncwarp();
@@ -867,7 +906,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
           sp_unpair(sum, sum0, sum1);
         } else {
-          if (!(ok = zero_tail())) break;
+          if (!(ok = clean_v())) break;
           // A first key tile with two terms: what P's rounding to bf16 left goes to
           // columns [64, 128) as a second term.  The scores are read again, 64 at a
           // time, so that the two terms need no more registers than the scores do
@@ -919,6 +958,28 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       ++jobs;
       tc_fence_after_sync();
       float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
+      // spread_bad: the infinities and NaN that this row sees among the piece's draft
+      // rows of V, added to its results of `columns` columns from `first` on.
+      auto is_bad = [&](int stream) {
+        return s_bad[2 * stream] == static_cast<int>(seen) || s_bad[2 * stream + 1] == static_cast<int>(seen);
+      };
+      auto spread_bad = [&](int first, int columns) {
+        if (!valid) return;
+        const int32_t *table = p.block_table + static_cast<size_t>(info[1]) * p.max_pages;
+#pragma unroll 1
+        for (int col = first; col < first + columns; ++col) {
+          float f = 0.f;
+#pragma unroll 1
+          for (int pos = max(keys - info[0], info[3]); pos < min(keys, info[4]) && pos <= lim; ++pos) {
+            const int page = table[pos / SF_PAGE_SIZE];
+            if (page < 0 || page >= p.num_pages) continue;  // (zeros)
+            const float v = __bfloat162float(
+                p.v_cache[((static_cast<size_t>(page) * p.H_kv + info[2]) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE) * D + col]);
+            if (!isfinite(v)) f += v;
+          }
+          if (f != 0.f) reinterpret_cast<float *>(dst + static_cast<size_t>(col / 4) * rows)[col % 4] += f;
+        }
+      };
       if (!joint) {
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
@@ -933,6 +994,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
         }
         if (valid) p.part_ml[slot0 + r] = make_float2(ref, l_run);
+        if (is_bad(s)) spread_bad(0, D);
       } else {
         // Both streams' accumulators of a row are in this thread's lane, and its
         // maximum and sum come through shared memory: each stream joins and writes
@@ -965,6 +1027,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
         }
         if (valid && s == 0) p.part_ml[slot0 + r] = make_float2(top, l_run * w + ml.y * wo);
+        if (is_bad(0) || is_bad(1)) spread_bad(s * (D / 2), D / 2);
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(READ + s));
@@ -1326,6 +1389,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   p.group_starts = group_starts;
   p.block_table = block_table;
   p.seq_lens = seq_lens;
+  p.v_cache = static_cast<const __nv_bfloat16 *>(v_cache);
   p.out = static_cast<__nv_bfloat16 *>(out);
   p.lse = lse;
   p.status = reinterpret_cast<uint32_t *>(ws);

@@ -305,3 +305,39 @@ def test_many_partials_a_row(prefix, own, n, H_q, H_kv, d):
 def test_own_tokens_of_pairs_of_heads(H_q, H_kv, d, lens):
     check([len(lens)], [0], lens, 1, H_q, H_kv, d, seed=sum(lens))
     check([1, len(lens) - 1], [40, 260], [x + 3 for x in lens], 4, H_q, H_kv, d, seed=sum(lens) + 1)
+
+
+# NaN and infinities in V of a draft token reach its own row and the later ones, in
+# their columns: one key tile and several, drafts across the line between two tiles, an
+# odd head, two-term weights, pieces of one and of two heads
+@pytest.mark.parametrize("H_q, H_kv, d", [(3, 3, 128), (8, 2, 64), (7, 1, 128), (16, 8, 64)])
+@pytest.mark.parametrize("prefix, lens, n", [
+    (0, [9, 40], 8), (300, [130, 128, 131], 8), (40, [1000, 16, 257], 16), (500, [263, 640], 4), (0, [2000], 3)])
+def test_draft_values_reach_the_rows_that_see_them(prefix, lens, n, H_q, H_kv, d):
+    require_gpu()
+    args = make([len(lens)], [prefix], lens, n, H_q, H_kv, d, seed=prefix + sum(lens) + d)
+    vc, bt = args[2], args[6]
+    bad = vc.clone()
+    nan = torch.zeros(len(lens), n, H_q, d, dtype=torch.bool)
+    up, down = nan.clone(), nan.clone()
+    g = H_q // H_kv
+    for b, size in enumerate(lens):
+        for j, marks in ((1, [(nan, 3, math.nan), (up, 5, math.inf)]), (n - 1, [(down, d - 1, -math.inf), (down, 5, -math.inf)])):
+            pos = size - n + j
+            for h in range(b % 2, H_kv, 2):  # every other head
+                for mask, col, value in marks:
+                    bad[bt[b, pos // 16], h, pos % 16, col] = value
+                    vc[bt[b, pos // 16], h, pos % 16, col] = 0.0
+                    mask[b, j:, h * g:(h + 1) * g, col] = True
+    want = ref.shared_prefix(*args)  # what the rows before see, and the other columns
+    args[2] = bad
+    out, lse, status = run(args)
+    assert status == 0
+    out = out.cpu()
+    nan |= up & down  # inf - inf
+    assert out[nan].isnan().all()
+    assert (out[up & ~nan] == math.inf).all() and (out[down & ~nan] == -math.inf).all()
+    seen = nan | up | down
+    o, l, spread = want
+    out = torch.where(seen, o, out.double())
+    close(out, lse, want)
