@@ -36,7 +36,7 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 177 to 190 us, 1.3 to 1.4 PFLOP/s, 13 of them the merge): the MMAs.  A
+// 32768 tokens: 183 to 193 us, 1.3 PFLOP/s, 13 of them the merge): the MMAs.  A
 // key tile of two row tiles is 32 of them; they take 74 cycles each, not the 64 of the
 // tensor cores' rate, as Q, K, V and the copies together read and write shared memory
 // at its full 128 bytes a cycle; a tile takes 2,550 cycles with what the turns leave
@@ -806,7 +806,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         // last page past the end, which hold whatever the page holds (whole pages past
         // the end are zeros already), and infinities and NaN of draft rows that are
         // masked for the rows before them (spread_bad gives them to those that see
-        // them).  In front of the weights' release, as V may come behind the scores.
+        // them; 3 % of the time for many rows, 5 % where all keys are own ones).  In
+        // front of the weights' release, as V may come behind the scores.
         const int valid_keys = keys - tile_pos;
         auto clean_v = [&]() -> bool {
           if (valid_keys >= kSpTile + SF_MAX_QUERY_ROWS - 1) return true;
