@@ -806,41 +806,36 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         // last page past the end, which hold whatever the page holds (whole pages past
         // the end are zeros already), and infinities and NaN of draft rows that are
         // masked for the rows before them (spread_bad gives them to those that see
-        // them; 3 % of the time for many rows, 5 % where all keys are own ones).  In
+        // them; 3 % of the time for many rows, 4 % where all keys are own ones).  In
         // front of the weights' release, as V may come behind the scores.
         const int valid_keys = keys - tile_pos;
         auto clean_v = [&]() -> bool {
           if (valid_keys >= kSpTile + SF_MAX_QUERY_ROWS - 1) return true;
-          const int tok0 = valid_keys & (SF_PAGE_SIZE - 1), from = max(valid_keys - info[0], 0), to_ = min(valid_keys, kSpTile);
-          const bool cut = valid_keys < kSpTile && tok0 != 0;
-          if (!cut && from >= to_) return true;
+          // rows from .. behind - 1 of the tile: hidden draft rows, then those past the end
+          const int from = max(valid_keys - info[0], 0), behind = min((valid_keys + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE * SF_PAGE_SIZE, kSpTile);
+          if (from >= behind) return true;
           const uint32_t pos = 2u * ring_tile + 1u, slot = pos % STAGES;
           if (!wwait(bar(FULL + slot), (pos / STAGES) & 1u)) return false;
           uint8_t *vt = smem + slot * L::kTileBytes;
-          auto chunk = [&](int tok, int rem) -> uint4 * {  // 16 bytes of a row (in the order that the copy's swizzle leaves)
-            return reinterpret_cast<uint4 *>(vt + (tok / SF_PAGE_SIZE) * kPageBytes + (rem >> 3) * kPageHalfBytes +
-                                             (tok % SF_PAGE_SIZE) * kRowBytes + (rem & 7) * 16);
-          };
-          if (cut) {
 #pragma unroll 1
-            for (int idx = r; idx < (SF_PAGE_SIZE - tok0) * HALVES * 8; idx += 128)
-              *chunk(valid_keys + idx / (HALVES * 8), idx % (HALVES * 8)) = make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll 1
-          for (int idx = r; idx < (to_ - from) * HALVES * 8; idx += 128) {
-            uint4 *at = chunk(from + idx / (HALVES * 8), idx % (HALVES * 8));
-            uint4 v = *at;
-            uint32_t kept = 0xffffffffu;
-            auto finite = [&](uint32_t w) -> uint32_t {
-              const uint32_t m = ((w & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
-              kept &= m;
-              return w & m;
-            };
-            v = make_uint4(finite(v.x), finite(v.y), finite(v.z), finite(v.w));
-            if (kept != 0xffffffffu) {
-              *at = v;
-              s_bad[2 * s + (jobs & 1u)] = static_cast<int>(seen);
+          for (int idx = r; idx < (behind - from) * HALVES * 8; idx += 128) {
+            // 16 bytes of a row (in the order that the copy's swizzle leaves)
+            const int tok = from + idx / (HALVES * 8), rem = idx % (HALVES * 8);
+            uint4 *at = reinterpret_cast<uint4 *>(vt + (tok / SF_PAGE_SIZE) * kPageBytes + (rem >> 3) * kPageHalfBytes +
+                                                  (tok % SF_PAGE_SIZE) * kRowBytes + (rem & 7) * 16);
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            uint32_t out = 0u;
+            if (tok < valid_keys) {
+              v = *at;
+              auto finite = [&](uint32_t w) -> uint32_t {
+                const uint32_t m = __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u);
+                out |= m;
+                return w & ~m;
+              };
+              v = make_uint4(finite(v.x), finite(v.y), finite(v.z), finite(v.w));
+              if (out) s_bad[2 * s + (jobs & 1u)] = static_cast<int>(seen);
             }
+            if (out || tok >= valid_keys) *at = v;
           }
           fence_proxy_async_smem();
           return true;
