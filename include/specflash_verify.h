@@ -428,10 +428,11 @@ int sf_visual_compress(const void *queries, const void *features, int F, int N, 
 /*               and strides agree.                                          */
 /* scales        fp32 [T][ceil(d / group)], or [T] for group 0; NULL with    */
 /*               SF_BF16.                                                    */
-/* Strides count elements.  0 <= T <= 0x7fff0000 (0: nothing), 1 <= d <=    */
+/* Strides count elements.  0 <= T <= 0x7fff0000 (0: nothing), 1 <= d <=     */
 /* SF_MAX_NORM_DIM; every pointer aligned to its element.  16-byte accesses  */
-/* are used where addresses, strides and d allow them, else one element at a */
-/* time.  One launch; asynchronous on `stream`; deterministic.               */
+/* are used where the rows of all tensors lie alike between 16-byte (8       */
+/* elements') boundaries, else one element at a time.  One launch;           */
+/* asynchronous on `stream`; deterministic.                                  */
 /* ------------------------------------------------------------------------ */
 int sf_add_rms_norm(const void *x, const void *residual, const void *weight, int dtype,
                     int weight_dtype, int T, int d, long long x_stride,
