@@ -953,6 +953,9 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       if (!ok) break;
       ++jobs;
       tc_fence_after_sync();
+      // Where every visible score is NaN the sum is NaN and no maximum was found; -inf
+      // would tell the joins that the row saw no key.
+      if (ref == -INFINITY && l_run != 0.f) ref = 0.f;
       float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
       // spread_bad: the infinities and NaN that this row sees among the piece's draft
       // rows of V, added to its results of `columns` columns from `first` on.
