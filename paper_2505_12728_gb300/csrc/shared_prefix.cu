@@ -58,10 +58,10 @@
 
 #include "attn_common.cuh"
 #include "sf_host.h"
+#include "shared_prefix_layout.h"
 
 namespace sf {
 
-constexpr int kSpTile = 128;     // keys per tile, query rows per row tile
 constexpr int kSpTilePages = kSpTile / SF_PAGE_SIZE;
 constexpr int kSpThreads = 384;  // two softmax warpgroups, two MMA warps, two copy warps
 constexpr int kSpMmaWarp = 8, kSpCopyWarp = 10, kSpQueryWarp = 11;
@@ -69,7 +69,6 @@ constexpr int kSpMaxRegs = 168;  // three warps share a sub-partition's 16K regi
 constexpr uint32_t kSpTmemCols = 512;
 constexpr float kSpRescaleLog2 = 8.f;
 constexpr int kSpMergeThreads = 256;
-constexpr int kSpSmemMax = 227 * 1024;
 // Cost of a segment on the partition's axis: kSpCostOne or kSpCostTwo for each of its
 // key tiles (one row tile, or two), and kSpCostSegOne or kSpCostSegTwo for itself (its Q
 // copy, pipeline start and epilogue; two row tiles leave 128 KB of partial results),
@@ -81,7 +80,6 @@ constexpr int kSpSmemMax = 227 * 1024;
 // of 8 took 174 us (now 119): a few CTAs had all the prefix's segments.
 constexpr uint32_t kSpCostSegOne = 5, kSpCostSegTwo = 10, kSpCostFew = 4, kSpCostOne = 3, kSpCostTwo = 4;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
-constexpr int kSpItems = 4;      // pieces published ahead
 
 // What the merge kernel has to know about a sequence: where its own segments and
 // its group's lie on the partition's axis.
@@ -186,40 +184,6 @@ __device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int
   return (left < p.tokens_per_tile ? left : p.tokens_per_tile) * p.group;
 }
 
-// A piece, as its CTA's warps read it from shared memory.
-struct SpItem {
-  int n, t0, keys;  // key tiles t0 .. t0 + n - 1 of the segment's keys; n = 0: no more pieces
-  int own, row, h;  // row of block_table (own) or prefix_table
-  int dual, again;  // both streams read every tile; the keys are read again by other pieces
-  int duo;          // key tiles t of head h + t % 2, a stream a head
-  int pad;
-  struct {
-    int two;               // the first key tile's weights go to P V as two bf16 terms
-    int n, first, step;    // the stream's key tiles within the piece (n = 0: none)
-    int token, rows;       // first query token and rows of its row tile
-    uint32_t slot;         // first row of its partial
-  } s[2];
-};
-
-// Bytes of shared memory behind the barriers: lengths of all entities, the groups'
-// first sequences, costs and partial rows.
-__host__ __device__ constexpr int sp_plan_bytes(int B, int num_groups) { return 4 * (B + 4 * num_groups + 1); }
-
-template <int D, int STAGES>
-struct SpSmem {
-  static constexpr int kTileBytes = kSpTile * D * 2;  // a K, V or Q tile
-  static constexpr int kQOffset = STAGES * kTileBytes;
-  static constexpr int kBarOffset = kQOffset + 2 * kTileBytes;
-  // full[S], empty[S], then per stream q_full, q_empty, s_full, p_full[2], o_done, fin, turn;
-  // item_full, item_empty per published piece; joint, read per stream
-  static constexpr int kNumBars = 2 * STAGES + 16 + 2 * kSpItems + 4;
-  static constexpr int kMiscOffset = kBarOffset + 8 * kNumBars;  // TMEM base, abort word
-  static constexpr int kItemOffset = kMiscOffset + 16;
-  static constexpr int kMlOffset = kItemOffset + kSpItems * static_cast<int>(sizeof(SpItem));  // float2 [2][128]
-  static constexpr int kInfoOffset = kMlOffset + 2 * 8 * kSpTile;  // int [8 warps][8], int [2][2]
-  static constexpr int kPlanOffset = kInfoOffset + 8 * 32 + 16;
-};
-
 // max of three in one instruction (a NaN is ignored, as by fmaxf)
 __device__ __forceinline__ float sp_max3(float a, float b, float c) {
   float d;
@@ -273,7 +237,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
   int *s_info = reinterpret_cast<int *>(smem + L::kInfoOffset);
   // per stream and parity of its job (a warp may be a job ahead of another): the last
   // piece with infinities or NaN among the draft's V
-  volatile int *s_bad = s_info + 64;
+  volatile int *s_bad = s_info + 8 * kSpInfo;
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
 
   if (tid == 0) {
@@ -777,7 +741,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       int tile_pos = ((item->t0 + item->s[s].first) >> duo) * kSpTile;  // position of the tile's first key
       base += item->n;
       const bool valid = r < rows;
-      int *info = s_info + 8 * warp;
+      int *info = s_info + kSpInfo * warp;
       if (lane == 0) {
         info[0] = item->own ? p.n_q - 1 : 0;  // draft rows that are masked for some rows
         info[1] = item->row;
@@ -1268,20 +1232,15 @@ static int sp_grid(int *G) {
 
 using SpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const SpParams);
 
-template <int D, int STAGES>
-static bool sp_variant(int plan_bytes, SpKernel *fn, int *smem) {
-  *fn = shared_prefix_split_kernel<D, STAGES>;
-  *smem = SpSmem<D, STAGES>::kPlanOffset + plan_bytes;
-  return *smem <= kSpSmemMax;
-}
-
-// The deepest ring that leaves room for the plan of B sequences.
+// The kernel with the deepest ring that leaves room for the plan of B sequences.
 static void sp_select(int D, int B, int num_groups, SpKernel *fn, int *smem) {
-  const int plan = sp_plan_bytes(B, num_groups);
+  const int stages = sp_stages(D, B, num_groups);
   if (D == 128) {
-    if (!sp_variant<128, 5>(plan, fn, smem)) sp_variant<128, 4>(plan, fn, smem);
+    *fn = stages == 5 ? shared_prefix_split_kernel<128, 5> : shared_prefix_split_kernel<128, 4>;
+    *smem = stages == 5 ? sp_smem_bytes<128, 5>(B, num_groups) : sp_smem_bytes<128, 4>(B, num_groups);
   } else {
-    if (!sp_variant<64, 10>(plan, fn, smem)) sp_variant<64, 8>(plan, fn, smem);
+    *fn = stages == 10 ? shared_prefix_split_kernel<64, 10> : shared_prefix_split_kernel<64, 8>;
+    *smem = stages == 10 ? sp_smem_bytes<64, 10>(B, num_groups) : sp_smem_bytes<64, 8>(B, num_groups);
   }
 }
 
