@@ -538,11 +538,12 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
 /* workspace    >= sf_shared_prefix_attention_workspace_size(...) bytes,     */
 /*              256-byte aligned, zero-filled before first use.              */
 /* Accuracy: scores and softmax statistics in fp32, the softmax weights in   */
-/* bf16 for the product with V (each rounded by at most 2^-8 of itself; over */
-/* many keys that averages out below the rounding of the bf16 output, and    */
-/* where a row sees fewer than 128 keys in all, and on prefixes of fewer     */
-/* than 128 keys, the weights are carried in two bf16 terms).  Infinities    */
-/* and NaN in K and V reach the rows that see them, and no others.           */
+/* bf16 for the product with V, each rounded by at most 2^-8 of itself,      */
+/* which averages out over many keys; the weights of each sequence's first   */
+/* 128 keys (prefix and own tokens together) are carried in two bf16 terms.  */
+/* Infinities and NaN in K and V reach the rows that see them, and no others */
+/* (an infinite score, or an infinity in V under a weight of two terms, as   */
+/* NaN).                                                                     */
 /* Deterministic.                                                            */
 /* ------------------------------------------------------------------------ */
 size_t sf_shared_prefix_attention_workspace_size(int B, int n_q, int H_q, int H_kv, int head_dim,

@@ -82,3 +82,69 @@ def test_nan_in_keys_reaches_the_rows_that_see_it(prefix, lens, H_q, H_kv, d):
             kc[pt[0, 8:16].long(), h] = math.nan  # the prefix's second key tile
             nan[:2, :, heads] = True
         check_nan(args, nan)
+
+
+def weights(args):
+    """Softmax weights in fp64: one [n][H_q][prefix + own keys] per sequence, over its prefix
+    and own tokens, and their values [H_kv][keys][d]."""
+    q, kc, vc, pt, pl, gs, bt, sl = args
+    n, H, d = q.shape[1:]
+    kv = kc.shape[1]
+    for b, L in enumerate(sl.tolist()):
+        g = max(i for i in range(len(gs) - 1) if int(gs[i]) <= b < int(gs[i + 1]))
+        P = int(pl[g])
+        k, v = (torch.cat([ref.tokens(c, pt[g], P), ref.tokens(c, bt[b], L)], 1) for c in (kc, vc))
+        s = torch.einsum("nhd,hkd->nhk", q[b].double(), k.repeat_interleave(H // kv, 0)) / math.sqrt(d)
+        hidden = torch.arange(P + L) > (P + L - n + torch.arange(n))[:, None]
+        yield torch.softmax(s.masked_fill(hidden[:, None], -math.inf), 2), v
+
+
+def attract(args, tokens, score):
+    """Keys `tokens` (table row, position, whether of the prefix) get `score` more from every
+    q, in natural units: q has 4 in its first column, a key what that takes."""
+    q, kc, pt, bt = args[0], args[1], args[3], args[6]
+    d = q.shape[3]
+    q[..., 0] = 4.0
+    kc[..., 0] = torch.where(kc[..., 0].isnan(), kc[..., 0], torch.zeros_like(kc[..., 0]))
+    for i, (row, at, prefix) in enumerate(tokens):
+        page = (pt if prefix else bt)[row, at // 16]
+        kc[page, :, at % 16, 0] = (score if isinstance(score, float) else score[i]) * math.sqrt(d) / 4
+
+
+# A few first keys that carry nearly all of the weight, as attention sinks do: in the
+# prefix, in the own tokens where there is no prefix, and in both where it is short.
+# The first 128 keys' weights come with 16 bits, so of the error only the output's own
+# rounding, that of the scores (|q| . |k| below 250 products' size 1 here and the sinks'
+# 20 units: 3e-4 of a weight and as much of their sum), and 2^-8 of the later keys' part
+# remain.
+@pytest.mark.parametrize("prefix, own, at", [(700, 40, [(0, 0, 1), (0, 1, 1), (0, 2, 1), (0, 5, 1)]),
+                                             (3000, 300, [(0, 3, 1), (0, 90, 1), (0, 127, 1)]),
+                                             (0, 900, [(0, 0, 0), (0, 1, 0), (0, 3, 0), (0, 100, 0)]),
+                                             (50, 700, [(0, 0, 0), (0, 7, 0), (0, 20, 1), (0, 77, 0)])])
+@pytest.mark.parametrize("H_q, H_kv, d", [(8, 8, 64), (28, 4, 128), (3, 3, 128)])
+def test_first_keys_that_carry_the_weight(prefix, own, at, H_q, H_kv, d):
+    require_gpu()
+    args = make([1], [prefix], [own], 8, H_q, H_kv, d, seed=prefix + own + d)
+    attract(args, at, 14.0)
+    out, lse, status = run(args)
+    assert status == 0
+    o, l, _ = ref.shared_prefix(*args)
+    (w, v), = weights(args)
+    size = v.abs().repeat_interleave(H_q // H_kv, 0)
+    first, later = (torch.einsum("nhk,hkd->nhd", w[..., part], size[:, part]) for part in (slice(0, 128), slice(128, None)))
+    tol = ref.bf16_half_ulp(o[0]) * (1 + 2.0 ** -6) + 2 * 3e-4 * (first + later) + 2.0 ** -8 * later
+    err = (out[0].double().cpu() - o[0]).abs()
+    assert (err <= tol).all(), ((err > tol).sum(), (err - tol).max())
+    assert (lse.double().cpu() - l).abs().max() <= 3e-3  # (scores of 14 and more: their fp32 error grows with them)
+
+
+@pytest.mark.parametrize("prefix, lens", [(0, [9, 40]), (900, [130, 20])])
+def test_an_infinite_score_makes_its_rows_nan(prefix, lens):
+    require_gpu()
+    args = make([2], [prefix], lens, 4, 4, 2, 64, seed=prefix + 3)
+    args[0][..., 0] = 1.0
+    args[1][args[6][0, 0], 1, 2, 0] = math.inf  # own token 2 of sequence 0: all of its rows see it
+    out, lse, status = run(args)
+    assert status == 0
+    assert out[0, :, 2:].isnan().all() and lse[0, :, 2:].isnan().all()
+    assert out[0, :, :2].isfinite().all() and out[1].isfinite().all() and lse[1].isfinite().all()
