@@ -538,9 +538,12 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
 /* workspace    >= sf_shared_prefix_attention_workspace_size(...) bytes,     */
 /*              256-byte aligned, zero-filled before first use.              */
 /* Accuracy: scores and softmax statistics in fp32, the softmax weights in   */
-/* bf16 for the product with V, each rounded by at most 2^-8 of itself,      */
-/* which averages out over many keys; the weights of each sequence's first   */
-/* 128 keys (prefix and own tokens together) are carried in two bf16 terms.  */
+/* bf16 for the product with V, each rounded by at most 2^-8 of itself.  The */
+/* weights of each sequence's first 128 keys (prefix and own tokens          */
+/* together) are carried in two bf16 terms, and the rounding of the largest  */
+/* weight of every 128 later keys is in the sum that divides as well, so     */
+/* that it cancels where one key outweighs the others; what is left is at    */
+/* most 2^-8 of the other weights' part, and averages out over many keys.    */
 /* Infinities and NaN in K and V reach the rows that see them, and no others */
 /* (an infinite score, or an infinity in V under a weight of two terms, as   */
 /* NaN).                                                                     */

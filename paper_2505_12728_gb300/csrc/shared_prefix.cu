@@ -52,7 +52,10 @@
 // sequence's first 128 keys also what that rounding left, as a second bf16 term: rows
 // that see few keys, and rows whose weight lies on their first keys, as with attention
 // sinks, have no others to average with (8 sequences of 5 rows over 3008 tokens: 24.4 ->
-// 24.9 us, 64 over 32768 183 -> 184).
+// 24.9 us, 64 over 32768 183 -> 184).  On the other tiles the sum that O is divided by
+// takes each tile's largest weight as it was rounded (the LSE's does not): a later key
+// that outweighs all others may be up to 2^kSpRescaleLog2 in units of the reference, and
+// its rounding would be the row's (1 %: 24.9 -> 25.2 us, 34.0 -> 34.3 for 4 videos).
 // Every wait is bounded; a timeout sets SF_DEVICE_TIMEOUT and stops every role.
 #include <algorithm>
 #include <cmath>
@@ -757,7 +760,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       const int lim = !valid ? 0x7fffff00 : item->own ? keys - p.n_q + r / p.group : keys - 1;
       release_item();
       if (n == 0) continue;
-      float ref = -INFINITY, l_run = 0.f;
+      float ref = -INFINITY, l_run = 0.f, off = 0.f;
       for (int k = 0; k < n; ++k, ++tiles, ring_tile += step, tile_pos += (step >> duo) * kSpTile) {
         if (!(ok = wwait(bar(SFULL + s), tiles & 1u))) break;
         tc_fence_after_sync();
@@ -824,7 +827,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         }
         a0 = sp_max3(a0, __uint_as_float(sv[124]), __uint_as_float(sv[125]));
         a1 = sp_max3(a1, __uint_as_float(sv[126]), __uint_as_float(sv[127]));
-        const float mx = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * p.scale_log2;
+        const float raw = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)), mx = raw * p.scale_log2;
         float alpha = 1.f;
         if (mx > ref + kSpRescaleLog2) {
           if (ref != -INFINITY) alpha = exp2f(ref - mx);
@@ -893,6 +896,9 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PFULL + 2 * s + 1));
+        // what rounding made of the tile's largest weight, for the same score in the same steps
+        const float most = fast_exp2(fmaf(raw, p.scale_log2, -mu));
+        off = off * alpha + (two ? 0.f : __bfloat162float(__float2bfloat16_rn(most)) - most);
         two = false;
       }
       if (ok) ok = wwait(bar(ODONE + s), jobs & 1u);
@@ -902,6 +908,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       // Where every visible score is NaN the sum is NaN and no maximum was found; -inf
       // would tell the joins that the row saw no key.
       if (ref == -INFINITY && l_run != 0.f) ref = 0.f;
+      // One weight may be nearly all of the sum, and O has it as it was rounded.  So O is
+      // divided by the sum with that rounding in it, l_run + off, and the unit of both is
+      // moved so that the part counts with its unrounded sum, l_run 2^ref, as before.
+      if (l_run > fabsf(off)) {
+        const float rounded = l_run + off;
+        ref += __log2f(__fdividef(l_run, rounded));  // (near 1: within 2^-21)
+        l_run = rounded;
+      }
       float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
       // spread_bad: the infinities and NaN that this row sees among the piece's draft
       // rows of V, added to its results of `columns` columns from `first` on.

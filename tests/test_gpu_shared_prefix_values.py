@@ -148,3 +148,41 @@ def test_an_infinite_score_makes_its_rows_nan(prefix, lens):
     assert status == 0
     assert out[0, :, 2:].isnan().all() and lse[0, :, 2:].isnan().all()
     assert out[0, :, :2].isfinite().all() and out[1].isfinite().all() and lse[1].isfinite().all()
+
+
+# One key of a later tile that outweighs all others, 3 to 8 base-2 units above the first
+# tile's largest score, so that its weight is no power of two and its rounding (2^-8 of it)
+# would be the row's.  With p_t the weights, * that key and |delta_t| <= 2^-8 the weights'
+# roundings, a result that is divided by a sum with the rounding of each tile's largest
+# weight in it is off by at most 2^-8 (1 + 2^-7) times
+#     p_* |v_* - out| + sum over the other keys of p_t (|v_t| + |out|),
+# beside the scores' 3e-4 and the output's own rounding.
+@pytest.mark.parametrize("groups, prefix, own, n, H_q, H_kv, d", [
+    ([1] * 16, 1024, 3, 2, 8, 8, 128), ([1] * 16, 0, 1024, 2, 8, 8, 64), ([20], 2048, 9, 8, 32, 32, 64),
+    ([9, 12], 1500, 300, 4, 28, 4, 128)])
+@pytest.mark.parametrize("excess", [3.4, 5.3, 7.3])
+def test_one_key_that_outweighs_all_others(groups, prefix, own, n, H_q, H_kv, d, excess):
+    require_gpu()
+    B = sum(groups)
+    args = make(groups, [prefix] * len(groups), [own] * B, n, H_q, H_kv, d, seed=int(10 * excess) + d, q_scale=0.1)
+    at, score = [], []
+    for i in range(len(groups) if prefix else B):
+        later = 130 + (i * 97) % ((prefix or own) - 140)
+        at += [(i, 5, prefix > 0), (i, later, prefix > 0)]
+        score += [12.0, 12.0 + excess * math.log(2)]
+    attract(args, at, score)
+    out, lse, status = run(args)
+    assert status == 0
+    out, lse = out.double().cpu(), lse.double().cpu()
+    for b, (w, v) in enumerate(weights(args)):
+        v = v.repeat_interleave(H_q // H_kv, 0)
+        o = torch.einsum("nhk,hkd->nhd", w, v)
+        size = torch.einsum("nhk,hkd->nhd", w, v.abs())
+        top, key = w.max(2)
+        assert (top > 0.85).all()
+        mine = v.gather(1, key.t()[..., None].expand(-1, -1, d)).transpose(0, 1)
+        p = top[..., None]
+        rest = p * (mine - o).abs() + (size - p * mine.abs()) + (1 - p) * o.abs()
+        tol = ref.bf16_half_ulp(o) * (1 + 2.0 ** -6) + 2 * 3e-4 * size + 2.0 ** -8 * (1 + 2.0 ** -7) * rest
+        err = (out[b] - o).abs()
+        assert (err <= tol).all(), ((err > tol).sum(), (err - tol).max())
