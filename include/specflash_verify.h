@@ -40,9 +40,11 @@
  *     seq_lens[b] - n_q), and the LM-head projections read the weights;
  *     these, and the workspace, must already be in place when the previous
  *     kernel on the stream starts (so neither it nor a kernel it may overlap
- *     writes them).  Everything else (q, hidden states, the draft rows' K/V,
- *     logits, probabilities, tokens, uniforms, temperatures) may come from
- *     the previous kernel: every kernel waits for it before reading them.
+ *     writes them; sf_kv_append says which of its calls may come in front of
+ *     sf_verify_attention all the same).  Everything else (q, hidden states,
+ *     the draft rows' K/V, logits, probabilities, tokens, uniforms,
+ *     temperatures) may come from the previous kernel: every kernel waits for
+ *     it before reading them.
  */
 #ifndef SPECFLASH_VERIFY_H
 #define SPECFLASH_VERIFY_H
@@ -486,9 +488,14 @@ int sf_add_rms_norm(const void *x, const void *residual, const void *weight, int
 /* workspace     >= sf_kv_append_workspace_size() bytes, 256-byte aligned,   */
 /*               zero-filled before first use (status word).                 */
 /* sf_verify_attention reads the prefix before it waits for the kernel in    */
-/* front of it: it may follow the append of its own n_q draft rows directly, */
-/* but not the append of a prompt (another kernel must come between).        */
-/* sf_shared_prefix_attention may follow either.                             */
+/* front of it.  So an append with row_starts, or of more than 16 rows a     */
+/* sequence, lets no kernel start before its stores can be read, and         */
+/* sf_verify_attention may follow it directly.  The append of up to 16 rows  */
+/* a sequence without row_starts lets it start early, so its n_q must then   */
+/* be no less than those rows (its draft rows), unless a kernel that waits   */
+/* before it lets its own successor start (the three of this section do,     */
+/* sf_verify_attention and the LM-head projections do not) comes between.    */
+/* sf_shared_prefix_attention may follow any append.                         */
 /* ------------------------------------------------------------------------ */
 size_t sf_kv_append_workspace_size(void);
 

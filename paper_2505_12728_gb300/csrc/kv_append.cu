@@ -15,11 +15,12 @@
 // one 16-byte chunk of a head (and, for pairs (j, j + n), the chunk of the partners)
 // in kBatch rows at a time.  A row's place is three loads that wait for each other:
 // the first rows' elements and the positions are loaded in front of them.  35k rows
-// of 28 + 8 bf16 heads of 128: 105 us, 6.2 TB/s (117 us with the sines in the order of
-// the pairs, four-way bank conflicts; 148 with four rows at a time and three CTAs an
-// SM).  Few rows are spread over more CTAs by heads.  Tensors that 16-byte accesses
+// of 28 + 8 bf16 heads of 128: 110 us, 5.9 TB/s (6 of them for the order of the stores
+// and the next kernel; without that 117 us with the sines in the order of the pairs,
+// four-way bank conflicts, and 148 with four rows at a time and three CTAs an SM).
+// Few rows are spread over more CTAs by heads.  Tensors that 16-byte accesses
 // cannot reach take kv_append_any_kernel, one pair of elements at a time (16000 rows
-// of 28 + 8 heads of 128, 2 bytes off: 168 us, 51 on the boundary).
+// of 28 + 8 heads of 128, 2 bytes off: 174 us, 52 on the boundary).
 #include <cmath>
 
 #include "sf_device.cuh"
@@ -45,6 +46,7 @@ struct AppendParams {
   __nv_bfloat16 *q_out, *k_cache, *v_cache;
   uint32_t *status;
   int T, B, H_q, H_kv, D, num_pages, max_pages, axes, pairs, interleaved, wide, rows;
+  int late;  // the next kernel on the stream starts behind the stores, not beside them
   float amplitude;
 };
 
@@ -66,6 +68,19 @@ __device__ __forceinline__ float2 pair_turn(const AppendParams &p, unsigned long
   float s, c;
   sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &s, &c);  // 2^-31: half turns
   return make_float2(c * p.amplitude, s * p.amplitude);
+}
+
+// Lets the next kernel on the stream start once all stores of the grid can be read by
+// it, also by bulk copies that it issues before it waits for this one.  All threads of
+// the block call it, behind their stores.  (A block stays until its stores have arrived:
+// 35k rows 104 -> 110 us.)
+__device__ __forceinline__ void launch_dependents_after_stores() {
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    grid_launch_dependents();
+  }
 }
 
 // The cache row (page * H_kv * 16 + slot; head h adds h * 16) of row t, or -1
@@ -163,7 +178,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendResident) kv_append_ker
   const int tid = threadIdx.x, warp = tid >> 5;
   const int t0 = blockIdx.x * rows, nr = min(rows, p.T - t0);
   grid_dependency_wait();
-  grid_launch_dependents();
+  if (!p.late) grid_launch_dependents();
   // units of a head: its rotated chunks (or pairs of chunks), then the others.  A
   // thread has one unit of a head and takes the CTA's rows kBatch at a time, all their
   // loads in flight: 64 bytes (16000 rows of 36 interleaved bf16 heads: 60 us with 32).
@@ -294,6 +309,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendResident) kv_append_ker
       }
     }
   }
+  if (p.late) launch_dependents_after_stores();
 }
 
 // The same for any alignment, strides and number of pairs: one row per CTA, one
@@ -303,7 +319,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_any_kernel(const __g
   __shared__ long long s_place;
   const int tid = threadIdx.x, t = blockIdx.x;
   grid_dependency_wait();
-  grid_launch_dependents();
+  if (!p.late) grid_launch_dependents();
   for (int j = tid; j < p.pairs; j += kAppendThreads) {
     int axis;
     const unsigned long long step = pair_step(p, j, axis);
@@ -339,10 +355,11 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_any_kernel(const __g
     }
   }
   const int v_at_once = kAppendThreads / p.D, i = tid % p.D;
-  if (place < 0 || tid >= v_at_once * p.D) return;
-  for (int h = tid / p.D; h < p.H_kv; h += v_at_once)
+  const int v_heads = place >= 0 && tid < v_at_once * p.D ? p.H_kv : 0;
+  for (int h = tid / p.D; h < v_heads; h += v_at_once)
     p.v_cache[static_cast<size_t>(place + h * SF_PAGE_SIZE) * p.D + i] =
         __float2bfloat16_rn(load_as_float(p.v, t * p.v_row + h * p.v_head + i, p.wide));
+  if (p.late) launch_dependents_after_stores();
 }
 
 }  // namespace sf
@@ -426,6 +443,11 @@ int sf_kv_append(const void *q, const void *k, const void *v, int dtype, long lo
   p.interleaved = interleaved != 0;
   p.wide = dtype == SF_F32;
   p.rows = T / B;
+  // sf_verify_attention copies the keys in front of its n_q draft rows before it waits for
+  // this kernel, so it starts beside it only where all rows are such draft rows (late
+  // always: append and attention 17.6 us a layer, 15.7 so, for 5 rows, 32 heads, 3008
+  // tokens).
+  p.late = row_starts != nullptr || p.rows > SF_MAX_QUERY_ROWS;
   p.amplitude = amplitude;
   DeviceInfo dev;
   const int st = current_device(&dev);

@@ -278,7 +278,12 @@ def verify_attention(q, k_cache, v_cache, block_table, seq_lens, *, out=None, ls
     """sf_verify_attention: q bf16 [B][n_q][H_q][d]; k/v_cache bf16
     [pages][H_kv][16][d]; block_table int32 [B][max_pages]; seq_lens int32 [B]
     (prefix + n_q).  Returns (out bf16 [B][n_q][H_q][d], lse fp32 [B][n_q][H_q]
-    or None)."""
+    or None).
+
+    The keys and values in front of the n_q draft rows, the block table and the
+    lengths are read before the kernel waits for the previous one on the stream: a
+    kernel that lets its successor start early must not write them (kv_append says
+    which of its calls may precede this one)."""
     B, n_q, H_q, d = q.shape
     num_pages, H_kv, page, d2 = k_cache.shape
     if block_table.dim() != 2 or block_table.shape[0] != B:
@@ -702,7 +707,12 @@ def kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_l
     positions); axis int32 [rotary_dim / 2] (None: axis 0); caches, block_table
     and seq_lens (counting the new rows) as for verify_attention; row_starts
     int32 [B + 1] for sequences of different numbers of new rows (None: T / B
-    each).  Returns q_out bf16 [T][H_q][d] or None."""
+    each).  Returns q_out bf16 [T][H_q][d] or None.
+
+    verify_attention copies the keys in front of its n_q draft rows before it waits
+    for the previous kernel.  It may follow this call directly if row_starts is given,
+    if a sequence has more than 16 new rows, or if they are no more than its n_q;
+    shared_prefix_attention always may."""
     if _calls is not None and workspace is not None and stream is None and (q is None) == (q_out is None):
         status = _calls.kv_append(q, k, v, positions, inv_freq, k_cache, v_cache, block_table, seq_lens, axis,
                                   row_starts, interleaved, amplitude, q_out, workspace)
