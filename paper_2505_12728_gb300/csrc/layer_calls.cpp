@@ -60,6 +60,10 @@ long long stride(const at::Tensor &t, int i) {
   return t.stride(i);
 }
 
+// Elements between the rows of a tensor [T][d].  A contiguous one's are d apart, also
+// where it has a single row whose stride says something else.
+long long row_stride(const at::Tensor &t) { return t.is_contiguous() ? t.size(1) : stride(t, 0); }
+
 at::ScalarType rows_type(PyObject *o) {
   if (!THPVariable_Check(o)) throw Unusual();
   const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
@@ -106,8 +110,8 @@ PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
       need(t.sizes() == x.sizes() && u.sizes() == x.sizes());
       r = t.data_ptr();
       ro = u.data_ptr();
-      r_row = stride(t, 0);
-      ro_row = stride(u, 0);
+      r_row = row_stride(t);
+      ro_row = row_stride(u);
     } else {
       need(a[6] == Py_None);
     }
@@ -124,8 +128,8 @@ PyObject *add_rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
       need(a[7] == Py_None && group == 0);
     }
     return g_add_rms_norm(x.data_ptr(), r, w.data_ptr(), type == at::kFloat ? SF_F32 : SF_BF16,
-                          wtype == at::kFloat ? SF_F32 : SF_BF16, T, d, stride(x, 0), r_row, number(a[3]), ro, ro_row,
-                          out.data_ptr(), e4m3 ? SF_E4M3 : SF_BF16, stride(out, 0), static_cast<int>(group), scales,
+                          wtype == at::kFloat ? SF_F32 : SF_BF16, T, d, row_stride(x), r_row, number(a[3]), ro, ro_row,
+                          out.data_ptr(), e4m3 ? SF_E4M3 : SF_BF16, row_stride(out), static_cast<int>(group), scales,
                           stream());
   });
 }
