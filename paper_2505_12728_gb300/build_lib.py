@@ -8,12 +8,13 @@ source or header is newer than the library.
 
 csrc/layer_calls.cpp (the decoder-layer operators' calls from Python without the
 detour through ctypes) is compiled beside it with g++ and torch's headers into
-``_build/_layer_calls.so``; where that fails, the binding does without.
+``_build/_layer_calls.<Python>.<torch>.so``; where that fails, the binding does without.
 """
 from __future__ import annotations
 
 import glob
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -27,7 +28,6 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libspecflash_verify.so")
 CALLS_SOURCE = os.path.join(CSRC, "layer_calls.cpp")
-CALLS = os.path.join(BUILD, "_layer_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2",
               "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]
@@ -56,20 +56,39 @@ def up_to_date() -> bool:
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
+def calls_path() -> str:
+    """Where _layer_calls is for the Python and the torch that run: torch's inline
+    accessors are compiled into it, so one that was built for another torch may load
+    and look at tensors through the wrong offsets."""
+    import torch
+    key = f"{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+    return os.path.join(BUILD, f"_layer_calls.{re.sub('[^A-Za-z0-9.+-]', '_', key)}.so")
+
+
 def build_calls(force: bool = False) -> str | None:
-    """Compile _layer_calls.so against the installed torch; its path, or None where
-    that is not possible (the reason goes to stderr)."""
+    """Compile _layer_calls against the installed torch; its path, or None where that
+    is not possible (the reason goes to stderr, and to a file beside it, so that the
+    same source is not tried again)."""
     header = os.path.join(INCLUDE, "specflash_verify.h")
-    if not force and os.path.exists(CALLS) and \
-            os.path.getmtime(CALLS) >= max(os.path.getmtime(CALLS_SOURCE), os.path.getmtime(header)):
-        return CALLS
+    newest = max(os.path.getmtime(CALLS_SOURCE), os.path.getmtime(header))
+    try:
+        path = calls_path()
+    except (ImportError, AttributeError) as e:
+        print(f"_layer_calls is not built: {e}", file=sys.stderr)
+        return None
+    failed = path + ".failed"
+    if not force:
+        if os.path.exists(path) and os.path.getmtime(path) >= newest:
+            return path
+        if os.path.exists(failed) and os.path.getmtime(failed) >= newest:
+            return None
     try:
         import torch
         root = os.path.join(os.path.dirname(torch.__file__))
         inc = os.path.join(root, "include")
         lib = os.path.join(root, "lib")
         cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
-        tmp = CALLS + f".{os.getpid()}.tmp"
+        tmp = path + f".{os.getpid()}.tmp"
         cmd = ["g++", "-O2", "-shared", "-fPIC", "-std=c++17", "-fvisibility=hidden",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
                "-I", sysconfig.get_paths()["include"], "-isystem", cuda, "-isystem", inc,
@@ -81,9 +100,11 @@ def build_calls(force: bool = False) -> str | None:
         return None
     if r.returncode != 0:
         print(f"_layer_calls is not built:\n{r.stderr[-2000:]}", file=sys.stderr)
+        with open(failed, "w") as f:
+            f.write(r.stderr)
         return None
-    os.replace(tmp, CALLS)
-    return CALLS
+    os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:

@@ -139,16 +139,17 @@ def load_library(path: str | None = None):
 
 
 def _load_calls(lib):
-    """The decoder-layer operators' direct calls, where they were built for this
-    torch."""
+    """The decoder-layer operators' direct calls, where they were built for the
+    Python and the torch that run."""
     global _calls
-    if not os.path.exists(build_lib.CALLS):
+    path = build_lib.calls_path()
+    if not os.path.exists(path):
         return
-    spec = importlib.util.spec_from_file_location("_layer_calls", build_lib.CALLS)
+    spec = importlib.util.spec_from_file_location("_layer_calls", path)
     try:
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-    except ImportError:  # built for another torch: build() has not run since
+    except ImportError:  # a library that it was linked with is gone
         return
     module.set_entries(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.sf_add_rms_norm, lib.sf_kv_append, lib.sf_shared_prefix_attention)))
