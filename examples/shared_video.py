@@ -115,13 +115,15 @@ def block(model, cache, tokens, frames, unshared=False):
     text = frames + cache.lens[:, None] - n + torch.arange(n, device="cuda")  # one time step a text token
     pos = text.to(I32).flatten().expand(3, -1).contiguous()
     prefix = cache.prefix_table.shape[1]
+    if unshared:  # (here: verify_attention reads both before it waits for the kernel in front of it)
+        table = torch.cat([cache.prefix_table.expand(questions, prefix), cache.table], 1)
+        lens = cache.lens + prefix * PAGE
 
     def attend(layer, q, k, v):
         q = sfv.kv_append(q, k, v, pos, model.inv_freq, cache.k[layer], cache.v[layer], cache.table, cache.lens,
                           axis=model.axis).view(questions, n, model.heads, model.d)
         if unshared:
-            table = torch.cat([cache.prefix_table.expand(questions, prefix), cache.table], 1)
-            out = sfv.verify_attention(q, cache.k[layer], cache.v[layer], table, cache.lens + prefix * PAGE)[0]
+            out = sfv.verify_attention(q, cache.k[layer], cache.v[layer], table, lens)[0]
         else:
             out = sfv.shared_prefix_attention(q, cache.k[layer], cache.v[layer], cache.prefix_table, cache.prefix_lens,
                                               cache.group_starts, cache.table, cache.lens)[0]
