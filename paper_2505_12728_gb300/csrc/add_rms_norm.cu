@@ -15,6 +15,12 @@
 // boundaries instead of at the row's start, so that only a row's first and last chunk
 // go element by element.  With a grid of a multiple of 8 CTAs, a CTA's rows all lie
 // alike, and it keeps its weights in registers as it does for aligned rows.
+//
+// Slower: tensors whose rows do not lie alike go one element at a time (kNormSingle;
+// 16384 x 3584 to bf16 183 us, 74 alike; to e4m3 with groups 311, 69), and rows of more
+// chunks than registers hold with the next row load one row at a time, and the weights
+// again for each (8192 x 8192 from fp32 139 us, 2 % above the copy rate; 4096 x 16384 from
+// bf16 97, 22 % above).
 #include <algorithm>
 #include <cmath>
 #include <mutex>

@@ -21,8 +21,8 @@
 // query row a thread), a score buffer and an accumulator:
 //     TMEM columns  S_0 [0, 128)  S_1 [128, 256)  O_0 [256, 384)  O_1 [384, 512).
 // A piece with two row tiles gives one to each stream, and so does one with two heads
-// (59 sequences of 212 to 916 own tokens, 32 heads, a prefix of 128: 110 us, 138 with a
-// piece per head); a piece with one row tile gives its even key tiles to stream 0 and
+// (59 sequences of 212 to 916 own tokens, 32 heads, a prefix of 140: 122 us; a piece per
+// head took a quarter more); a piece with one row tile gives its even key tiles to stream 0 and
 // its odd ones to stream 1, whose results are joined in the CTA, or, with one key
 // tile, goes to the streams in turn.  So while one stream's softmax runs, the tensor
 // cores work for the other.
@@ -36,12 +36,12 @@
 // KB with 64-wide heads), which both streams pass in order.
 //
 // What bounds it.  Many rows (64 sequences of 8 rows, 28 / 4 heads of 128, a prefix of
-// 32768 tokens: 183 to 193 us, 1.3 PFLOP/s, 13 of them the merge): the MMAs.  A
+// 32768 tokens: 184 to 199 us by box, 1.2 to 1.3 PFLOP/s, 13 of them the merge): the MMAs.  A
 // key tile of two row tiles is 32 of them; they take 74 cycles each, not the 64 of the
 // tensor cores' rate, as Q, K, V and the copies together read and write shared memory
-// at its full 128 bytes a cycle; a tile takes 2,550 cycles with what the turns leave
-// idle.  One row tile (8 sequences of 5 rows, 32 / 32 heads, 3008 tokens: 24 us for 62.5
-// MB, 2.6 TB/s) and few keys: the start (the cut of the axis takes 3 us from cold
+// at its full 128 bytes a cycle; a tile takes 2,880 cycles with what the turns leave
+// idle.  One row tile (8 sequences of 5 rows, 32 / 32 heads, 3008 tokens: 25 us for 62.5
+// MB, 2.5 TB/s) and few keys: the start (the cut of the axis takes 3 us from cold
 // instructions, the first keys 2), the partials' way through L2 and the merge kernel
 // (5 us behind the last piece).
 //
@@ -78,12 +78,13 @@ constexpr int kSpMergeThreads = 256;
 // Cost of a segment on the partition's axis: kSpCostOne or kSpCostTwo for each of its
 // key tiles (one row tile, or two), and kSpCostSegOne or kSpCostSegTwo for itself (its Q
 // copy, pipeline start and epilogue; two row tiles leave 128 KB of partial results),
-// with kSpCostFew more for weights in two terms.  Measured, least squares over the CTAs
+// with kSpCostFew more for a prefix's first key tile in two terms (with 0, 1 or 2 the same
+// within 3 %).  Measured, least squares over the CTAs
 // of three workloads: 1.3 to 1.5 us for a key tile of two row tiles, 0.9 to 1.8 of one,
 // 2 to 4 for a piece.  With one unit for every row tile's key tile and two a segment the
 // longest CTA of the workload of 64 sequences took 18 % more than the mean (225 us, with
 // the costs 195); with 5 for either kind of segment, 59 sequences of some 560 tokens with a prefix
-// of 8 took 174 us (now 119): a few CTAs had all the prefix's segments.
+// of 8 took 174 us (119 with 10): a few CTAs had all the prefix's segments.
 constexpr uint32_t kSpCostSegOne = 5, kSpCostSegTwo = 10, kSpCostFew = 4, kSpCostOne = 3, kSpCostTwo = 4;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
 
