@@ -6,7 +6,7 @@ import torch
 
 from tests import layer_reference as ref
 from tests.gpu_helpers import require_gpu
-from tests.test_gpu_shared_prefix import close, make, run
+from tests.test_gpu_shared_prefix import check, close, make, run
 
 pytestmark = pytest.mark.gpu
 
@@ -186,3 +186,11 @@ def test_one_key_that_outweighs_all_others(groups, prefix, own, n, H_q, H_kv, d,
         tol = ref.bf16_half_ulp(o) * (1 + 2.0 ** -6) + 2 * 3e-4 * size + 2.0 ** -8 * (1 + 2.0 ** -7) * rest
         err = (out[b] - o).abs()
         assert (err <= tol).all(), ((err > tol).sum(), (err - tol).max())
+
+
+# 128-wide heads with batches whose plan leaves four ring slots (88 sequences of one
+# group and more), beside the largest that leave five
+@pytest.mark.parametrize("groups", [[87], [88], [40, 60], [1] * 19, [1] * 18, [3, 297]])
+def test_batches_on_both_sides_of_the_ring(groups):
+    check(groups, [(171 * (g + 2)) % 700 for g in range(len(groups))], [3 + (53 * b) % 290 for b in range(sum(groups))], 3, 4, 2,
+          128, seed=len(groups) + sum(groups))
