@@ -430,11 +430,11 @@ int sf_visual_compress(const void *queries, const void *features, int F, int N, 
 /*               and strides agree.                                          */
 /* scales        fp32 [T][ceil(d / group)], or [T] for group 0; NULL with    */
 /*               SF_BF16.                                                    */
-/* Strides count elements.  0 <= T <= 0x7fff0000 (0: nothing), 1 <= d <=     */
-/* SF_MAX_NORM_DIM; every pointer aligned to its element.  16-byte accesses  */
-/* are used where the rows of all tensors lie alike between 16-byte (8       */
-/* elements') boundaries, else one element at a time.  One launch;           */
-/* asynchronous on `stream`; deterministic.                                  */
+/* Strides count elements and are at least d.  0 <= T <= 0x7fff0000 (0:      */
+/* nothing), 1 <= d <= SF_MAX_NORM_DIM; every pointer aligned to its         */
+/* element.  16-byte accesses are used where the rows of all tensors lie     */
+/* alike between 16-byte (8 elements') boundaries, else one element at a     */
+/* time.  One launch; asynchronous on `stream`; deterministic.               */
 /* ------------------------------------------------------------------------ */
 int sf_add_rms_norm(const void *x, const void *residual, const void *weight, int dtype,
                     int weight_dtype, int T, int d, long long x_stride,
@@ -469,7 +469,7 @@ int sf_add_rms_norm(const void *x, const void *residual, const void *weight, int
 /*               stride 1, row and head strides in elements (views of one    */
 /*               fused projection).  q NULL with H_q 0: keys and values only.*/
 /* positions     int32 [axes][T], 1 <= axes <= SF_MAX_AXES; may be negative. */
-/* inv_freq      fp64 [n]: radians per position.                             */
+/* inv_freq      fp64 [n], finite: radians per position.                     */
 /* freq_axis     int32 [n], values in [0, axes); NULL: axis 0.  A value      */
 /*               outside sets SF_DEVICE_BAD_INDEX and reads axis 0.          */
 /* rotary_dim    even, in [0, head_dim]; 0: no rotation, and positions,      */
