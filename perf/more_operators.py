@@ -254,8 +254,6 @@ def prepare(case, seed):
         s["lens_out"] = torch.empty_like(s["lens"])
         s["kept"] = torch.empty(case["layers"], B, kv, case["budget"], dtype=torch.int32, device=DEVICE)
         s["budget"], s["first"], s["recent"] = case["budget"], case["first"], case["recent"]
-        s["k_layers"], s["v_layers"] = list(s["k"]), list(s["v"])
-        s["mass_layers"], s["mass_out_layers"], s["kept_layers"] = list(s["mass"]), list(s["mass_out"]), list(s["kept"])
         if own:
             from paper_2505_12728_gb300 import specflash_verify as sfv
             s["workspace"] = sfv.new_workspace(sfv.kv_evict_workspace_size(case["layers"], B, kv, case["budget"]))
@@ -306,7 +304,6 @@ def prepare(case, seed):
     s["table"], pool = _table(rng, totals, [0 if x is None else x // PAGE for x in lens])
     s["k"] = torch.stack([normal(pool, kv, PAGE, d) for _ in range(case["layers"])])
     s["v"] = torch.stack([normal(pool, kv, PAGE, d) for _ in range(case["layers"])])
-    s["k_layers"], s["v_layers"] = list(s["k"]), list(s["v"])
     tokens, sampled = [], []
     for p, want in zip(trees, depths):
         # siblings carry different tokens; the target follows the path to a node
@@ -353,16 +350,16 @@ def _library(s):
         return sfv.tree_attention(s["q"], s["k"], s["v"], s["table"], s["lens"], s["mask"], out=s["out"],
                                   lse=s["lse"], workspace=s["workspace"])
     if s["op"] == "commit":
-        got = sfv.tree_commit(s["tokens"], s["sampled"], s["parents"], s["k_layers"], s["v_layers"], s["table"],
-                              s["lens"], num_accepted=s["accepted"], out_tokens=s["out_tokens"], path=s["path"],
+        # (the layers' caches side by side; a list of them will do as well)
+        got = sfv.tree_commit(s["tokens"], s["sampled"], s["parents"], s["k"], s["v"], s["table"], s["lens"],
+                              num_accepted=s["accepted"], out_tokens=s["out_tokens"], path=s["path"],
                               row_weights=s["weights"], workspace=s["workspace"])
         return tuple(got) + (s["k"], s["v"])
     if s["op"] == "mass":
         return sfv.attention_mass(s["q"], s["lse"], s["k"], s["table"], s["lens"], s["mass"],
                                   row_weights=s["weights"], out=s["mass_out"], workspace=s["workspace"])
-    sfv.kv_evict(s["mass_layers"], s["k_layers"], s["v_layers"], s["table"], s["lens"], s["budget"], first=s["first"],
-                 recent=s["recent"], mass_out=s["mass_out_layers"], seq_lens_out=s["lens_out"], kept=s["kept_layers"],
-                 workspace=s["workspace"])
+    sfv.kv_evict(s["mass"], s["k"], s["v"], s["table"], s["lens"], s["budget"], first=s["first"], recent=s["recent"],
+                 mass_out=s["mass_out"], seq_lens_out=s["lens_out"], kept=s["kept"], workspace=s["workspace"])
     return s["k"], s["v"], s["mass_out"], s["lens_out"], s["kept"]
 
 
