@@ -72,8 +72,8 @@ typedef enum {
 #define SF_DEVICE_BAD_TOKEN 0x2u /* draft token outside [0, V)                */
 #define SF_DEVICE_TIMEOUT 0x4u   /* a bounded wait on a copy gave up (~1 s)   */
 #define SF_DEVICE_BAD_SEQLEN 0x8u /* seq_lens[b] outside [n_q, max_pages*16]   */
-#define SF_DEVICE_OUT_OF_PAGES 0x10u /* sf_kv_commit: free-page stack too small */
-#define SF_DEVICE_BAD_INDEX 0x20u /* group_starts / freq_axis: an entry out of range */
+#define SF_DEVICE_OUT_OF_PAGES 0x10u /* free-page stack too small (commit) or full */
+#define SF_DEVICE_BAD_INDEX 0x20u /* group_starts / freq_axis / parents: an entry out of range */
 
 /* Compile-time limits of the library (calls beyond them return an error). */
 #define SF_PAGE_SIZE 16      /* tokens per KV page                            */
@@ -85,6 +85,8 @@ typedef enum {
 #define SF_MAX_VOCAB 8388608  /* V for sf_lm_head / sf_sample / sf_draft_sample */
 #define SF_MAX_NORM_DIM 32768 /* d of sf_add_rms_norm                         */
 #define SF_MAX_AXES 4         /* position axes of sf_kv_append                */
+#define SF_MAX_TREE_ROWS 64   /* nodes of a tree, the emitted token included  */
+#define SF_MAX_LAYERS 128     /* layers' caches of one call                   */
 
 /* Element types of the operators that take more than one. */
 #define SF_BF16 0
@@ -568,6 +570,201 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
                                int max_prefix_pages, int max_pages_per_seq, float softmax_scale,
                                void *out, float *lse, void *workspace, size_t workspace_bytes,
                                cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Trees of drafted tokens.  Where a draft is a tree instead of a chain (some */
+/* alternatives for the next token, some after each of those, ..), one       */
+/* forward pass of the target scores all its nodes (Sec. 3.1, with n_q nodes  */
+/* for the K candidates): each node sees the context and the nodes above it.  */
+/* One step is sf_tree_mask, in every layer sf_kv_append (with the nodes'     */
+/* positions) and sf_tree_attention, then the target's token after every node */
+/* (sf_sample of the logits, greedy or by its uniforms) and sf_tree_commit.   */
+/*                                                                           */
+/* A tree has n <= SF_MAX_TREE_ROWS nodes; node i hangs below parents[i] < i. */
+/* Node 0 is the root: the token that the previous step emitted, whose key    */
+/* the context does not have yet.  -1 marks a root, anything below that a row */
+/* that is not part of the tree, as are all nodes below it.                   */
+/*                                                                           */
+/* sf_tree_mask: mask[b][i] has bit i and the bits of all nodes above i       */
+/* (0 for rows that are not part of the tree), positions[b][i] = start[b] +   */
+/* the number of nodes above i.                                               */
+/*                                                                           */
+/* parents      int32 [B][n].  An entry not below its row sets                */
+/*              SF_DEVICE_BAD_INDEX, and the row is not part of the tree.     */
+/* start        int32 [B], the roots' positions; NULL: 0.                     */
+/* mask         uint64 [B][n]; positions int32 [B][n], may be NULL.           */
+/* workspace    >= sf_tree_mask_workspace_size() bytes, 256-byte aligned,     */
+/*              zero-filled before first use (status word).                   */
+/* ------------------------------------------------------------------------ */
+size_t sf_tree_mask_workspace_size(void);
+
+int sf_tree_mask(const int32_t *parents, const int32_t *start, int B, int n, uint64_t *mask,
+                 int32_t *positions, void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Verification attention of a tree's nodes.  As sf_verify_attention, but row */
+/* i of sequence b sees, of the n_q new rows at positions L_b .. L_b + n_q - 1*/
+/* (L_b = seq_lens[b] - n_q), those whose bit tree_mask[b][i] has.  The L_b   */
+/* tokens in front are seen by all rows.  The masks need not be a tree's.     */
+/* seq_lens[b] = 0 marks an idle slot.  A row that sees no key (no context    */
+/* and no bit, or an idle slot) gets out = 0 and lse = -inf.                  */
+/*                                                                           */
+/* tree_mask    uint64 [B][n_q], mask_stride elements from one sequence's to  */
+/*              the next (at least n_q; 0: one tree for all).  Bits from n_q  */
+/*              on have no meaning.                                           */
+/* Limits: 1 <= n_q <= SF_MAX_TREE_ROWS, otherwise those of                   */
+/* sf_verify_attention.  seq_lens[b] outside [n_q, 16 * max_pages_per_seq] is */
+/* clamped and flagged with SF_DEVICE_BAD_SEQLEN, a page outside the pool     */
+/* reads as zeros and sets SF_DEVICE_BAD_PAGE.  What rows hold that nothing   */
+/* sees, or pages past a length, has no effect (NaN neither).  Infinities and */
+/* NaN in K and V reach the rows that see them, and no others.                */
+/* softmax_scale  0 selects 1/sqrt(head_dim).                                 */
+/* workspace    >= sf_tree_attention_workspace_size(...) bytes, 256-byte      */
+/*              aligned, zero-filled before first use.                        */
+/* Accuracy: as sf_shared_prefix_attention.  Deterministic.  Waits for the    */
+/* previous kernel on the stream before it reads anything.                    */
+/* ------------------------------------------------------------------------ */
+size_t sf_tree_attention_workspace_size(int B, int n_q, int H_q, int H_kv, int head_dim,
+                                        int max_pages_per_seq, int page_size);
+
+int sf_tree_attention(const void *q, const void *k_cache, const void *v_cache,
+                      const int32_t *block_table, const int32_t *seq_lens,
+                      const uint64_t *tree_mask, long long mask_stride, int B, int n_q, int H_q,
+                      int H_kv, int head_dim, int page_size, int num_pages, int max_pages_per_seq,
+                      float softmax_scale, void *out, float *lse, void *workspace,
+                      size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* The path of the accepted tokens through a tree, and its way into the       */
+/* context.  From the root (node 0): as long as a child of the current node   */
+/* carries the token that the target gives after that node, the lowest such   */
+/* child is next.  With sampled[b][i] drawn from the target's distribution    */
+/* after node i, every token so emitted has the target's distribution         */
+/* whatever the draft proposed (Sec. 1: the output stays the target's); with  */
+/* its argmax this is greedy decoding.                                        */
+/*     num_accepted = nodes of the path - 1                                   */
+/*     path         = its nodes, then -1                                      */
+/*     out_tokens   = sampled[b][path[0 .. num_accepted]], then -1: the       */
+/*                    accepted drafts, and the token after the last of them   */
+/*     row_weights  = 1 for the path's rows, 0 for others (for                */
+/*                    sf_attention_mass)                                      */
+/* The keys and values of the path then follow the context: in each layer's   */
+/* caches row L_b + path[r] is copied to L_b + r, L_b = seq_lens[b] - n_q.    */
+/* With free_pages, the lengths and pages are then prepared for the next tree */
+/* of n_q_next nodes, exactly as by sf_kv_commit (whose arguments these are); */
+/* without, seq_lens and block_table stay as they are.                        */
+/* Slots with seq_lens[b] = 0 are idle: num_accepted 0, path and out_tokens   */
+/* -1, row_weights 0.  A seq_lens[b] outside [n_q, 16 * max_pages_per_seq]    */
+/* sets SF_DEVICE_BAD_SEQLEN and counts as idle (and sf_kv_commit's part      */
+/* changes nothing); a row whose page is outside the pool is not moved and    */
+/* sets SF_DEVICE_BAD_PAGE.                                                   */
+/*                                                                           */
+/* tokens       int32 [B][n_q], the nodes' tokens; sampled int32 [B][n_q];    */
+/* parents      int32 [B][n_q], as for sf_tree_mask.                          */
+/* k_caches, v_caches  HOST arrays of num_layers device pointers, bf16        */
+/*              [num_pages][H_kv][16][head_dim] each, all with the same       */
+/*              block_table; 0 <= num_layers <= SF_MAX_LAYERS.  A page is in  */
+/*              one sequence's table only.                                    */
+/* num_accepted int32 [B]; out_tokens, path int32 [B][n_q] and row_weights    */
+/*              fp32 [B][n_q] may be NULL.                                    */
+/* head_dim a multiple of 8 in [8, 256]; H_kv <= 1024.                        */
+/* workspace    >= sf_tree_commit_workspace_size() bytes, 256-byte aligned,   */
+/*              zero-filled before first use (status word).                   */
+/* Lets no kernel start before its stores can be read: sf_verify_attention    */
+/* may follow (not after the free_pages form: see sf_kv_commit).              */
+/* ------------------------------------------------------------------------ */
+size_t sf_tree_commit_workspace_size(void);
+
+int sf_tree_commit(const int32_t *tokens, const int32_t *sampled, const int32_t *parents,
+                   void *const *k_caches, void *const *v_caches, int num_layers,
+                   int32_t *block_table, int32_t *seq_lens, int B, int n_q, int H_kv, int head_dim,
+                   int page_size, int num_pages, int max_pages_per_seq, int32_t *num_accepted,
+                   int32_t *out_tokens, int32_t *path, float *row_weights, int n_q_next,
+                   int32_t *free_pages, int32_t *free_count, int capacity, void *workspace,
+                   size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* A context held at a budget.  Most keys of a long visual context get next   */
+/* to no attention; the two calls below measure what each key gets, and drop  */
+/* the rest.  The paper compresses visual tokens for the draft model only     */
+/* (Sec. 3.2); this is the target's cache.                                    */
+/*                                                                           */
+/* sf_attention_mass: the attention weight that the rows of one attention     */
+/* call gave each key of the context, per KV head,                            */
+/*     mass_out[b][h][t] = mass[b][h][t]                                      */
+/*         + sum_i row_weights[b][i] sum_j exp(scale * <q_ij, k_t> - lse_ij), */
+/* over the n_q rows i and the query heads j of KV head h, for t < L_b =      */
+/* seq_lens[b] - n_q.  q, lse, k_cache, block_table and seq_lens are those of */
+/* that call (sf_verify_attention, sf_tree_attention; after a prompt, a       */
+/* window of its last rows).  The rows' own keys are too new to be judged and */
+/* get nothing.  Entries from L_b on are not written.                         */
+/*                                                                           */
+/* lse          fp32 [B][n_q][H_q] (natural log); a row of -inf counts 0.     */
+/* mass         fp32 [B][H_kv][mass_width], or NULL for 0; may be mass_out.   */
+/* row_weights  fp32 [B][n_q], finite and >= 0, or NULL for 1.  What a row of */
+/*              weight 0 holds has no effect (NaN neither).                   */
+/* Limits and device flags: those of sf_tree_attention (n_q likewise); L_b    */
+/* above mass_width is clamped and flagged with SF_DEVICE_BAD_SEQLEN.         */
+/* workspace    >= sf_attention_mass_workspace_size() bytes, 256-byte         */
+/*              aligned, zero-filled before first use (status word).          */
+/* Scores and sums in fp32.  Deterministic.                                   */
+/* ------------------------------------------------------------------------ */
+size_t sf_attention_mass_workspace_size(void);
+
+int sf_attention_mass(const void *q, const float *lse, const void *k_cache,
+                      const int32_t *block_table, const int32_t *seq_lens, const float *mass,
+                      const float *row_weights, int B, int n_q, int H_q, int H_kv, int head_dim,
+                      int page_size, int num_pages, int max_pages_per_seq, int mass_width,
+                      float softmax_scale, float *mass_out, void *workspace,
+                      size_t workspace_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* sf_kv_evict: every sequence of more than `budget` tokens is cut to its     */
+/* budget.  L_b = seq_lens[b] - n_q tokens count: the last n_q positions are  */
+/* places for rows that are still to be written (as after sf_tree_commit or   */
+/* sf_kv_commit).  Per layer and KV head these stay: the `first` tokens, the  */
+/* last `recent` ones, and of the others those with the largest mass, the     */
+/* lowest positions among equal ones (NaN counts as -inf).  They keep their   */
+/* order: the kept ones' rows of K, V and mass move to 0 .. budget - 1.       */
+/* Positions are in the keys' rotation already, so attention over what is     */
+/* left needs no change.                                                      */
+/*     seq_lens_out[b] = min(L_b, budget) + n_q     (0 for an idle slot)      */
+/*     mass_out = the kept tokens' mass, then 0     (to mass_width)           */
+/*     kept     = their positions before, then -1                             */
+/* Sequences within the budget keep everything in its place.                  */
+/*                                                                           */
+/* mass, mass_out  HOST arrays of num_layers device pointers, fp32            */
+/*              [B][H_kv][mass_width]; a layer's two may be the same.         */
+/* k_caches, v_caches  HOST arrays of num_layers device pointers, as for      */
+/*              sf_tree_commit.  A sequence that is cut shares no page.       */
+/* seq_lens     int32 [B]; seq_lens_out int32 [B], may be seq_lens.           */
+/* kept         HOST array of num_layers device pointers, int32               */
+/*              [B][H_kv][budget], or NULL.                                   */
+/* free_pages, free_count, capacity  as for sf_kv_commit: pages that are no   */
+/*              longer needed go onto the stack (sequence order, ascending    */
+/*              logical page), their entries in block_table become -1.        */
+/*              Sequences from the first whose pages the stack has no room    */
+/*              for keep theirs, and SF_DEVICE_OUT_OF_PAGES is set.  NULL:    */
+/*              pages stay mapped.                                            */
+/* A sequence with L_b < 0, or longer than its pages or mass_width, sets      */
+/* SF_DEVICE_BAD_SEQLEN and is left as it is.  A row whose old or new page is */
+/* outside the pool is not moved and sets SF_DEVICE_BAD_PAGE.                 */
+/* 1 <= num_layers <= SF_MAX_LAYERS; 1 <= budget; first, recent >= 0, first + */
+/* recent <= budget; 0 <= n_q <= SF_MAX_TREE_ROWS; head_dim a multiple of 8   */
+/* in [8, 256]; H_kv <= 1024.                                                 */
+/* workspace    >= sf_kv_evict_workspace_size(...) bytes, 256-byte aligned,   */
+/*              zero-filled before first use.                                 */
+/* Deterministic.  Lets no kernel start before its stores can be read.        */
+/* ------------------------------------------------------------------------ */
+size_t sf_kv_evict_workspace_size(int num_layers, int B, int H_kv, int budget);
+
+int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_caches,
+                int num_layers, int32_t *block_table, const int32_t *seq_lens, int B, int H_kv,
+                int head_dim, int page_size, int num_pages, int max_pages_per_seq, int mass_width,
+                int budget, int first, int recent, int n_q, float *const *mass_out,
+                int32_t *seq_lens_out, int32_t *const *kept, int32_t *free_pages,
+                int32_t *free_count, int capacity, void *workspace, size_t workspace_bytes,
+                cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -70,19 +70,6 @@ __device__ __forceinline__ float2 pair_turn(const AppendParams &p, unsigned long
   return make_float2(c * p.amplitude, s * p.amplitude);
 }
 
-// Lets the next kernel on the stream start once all stores of the grid can be read by
-// it, also by bulk copies that it issues before it waits for this one.  All threads of
-// the block call it, behind their stores.  (A block stays until its stores have arrived:
-// 35k rows 104 -> 110 us.)
-__device__ __forceinline__ void launch_dependents_after_stores() {
-  asm volatile("fence.proxy.async.global;" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    grid_launch_dependents();
-  }
-}
-
 // The cache row (page * H_kv * 16 + slot; head h adds h * 16) of row t, or -1
 // where the row is not appended.  A whole warp calls it.
 __device__ __forceinline__ long long row_place(const AppendParams &p, int t) {

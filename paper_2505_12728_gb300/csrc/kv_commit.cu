@@ -31,6 +31,7 @@ struct CommitParams {
   const int32_t *num_accepted;
   uint32_t *status;
   int B, n_q, n_q_next, max_pages, capacity;
+  int idle_slots;  // a length of 0 marks a slot that stays as it is
 };
 
 // Block-wide exclusive scan of one int per thread (blockDim.x threads);
@@ -62,7 +63,9 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const CommitP
   int push = 0, take = 0, bad = 0, had = 0, need = 0, next_len = 0;
   if (b < p.B) {
     const int T = p.seq_lens[b], a = p.num_accepted[b];
-    if (T < p.n_q || a < 0) {
+    if (T == 0 && p.idle_slots) {
+      // no pages, no rows
+    } else if (T < p.n_q || a < 0) {
       bad = 1;
     } else {
       const int keep = a + 1 < p.n_q ? a + 1 : p.n_q;
@@ -107,6 +110,29 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const CommitP
   if (b == 0) *p.free_count = base;
 }
 
+int launch_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_pages, int32_t *free_count,
+                     const int32_t *num_accepted, int B, int n_q, int n_q_next, int max_pages, int capacity,
+                     bool idle_slots, uint32_t *status, cudaStream_t stream) {
+  CommitParams prm;
+  prm.seq_lens = seq_lens;
+  prm.block_table = block_table;
+  prm.free_pages = free_pages;
+  prm.free_count = free_count;
+  prm.num_accepted = num_accepted;
+  prm.status = status;
+  prm.B = B;
+  prm.n_q = n_q;
+  prm.n_q_next = n_q_next;
+  prm.max_pages = max_pages;
+  prm.capacity = capacity;
+  prm.idle_slots = idle_slots;
+  const int threads = (B + 31) / 32 * 32;
+  kv_commit_kernel<<<1, threads, 0, stream>>>(prm);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return fail(SF_ERR_CUDA, "kv commit launch: %s", cudaGetErrorString(e));
+  return SF_OK;
+}
+
 }  // namespace sf
 
 extern "C" {
@@ -137,23 +163,8 @@ int sf_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_pages,
   if (workspace_bytes < sf_kv_commit_workspace_size())
     return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes,
                 sf_kv_commit_workspace_size());
-  CommitParams prm;
-  prm.seq_lens = seq_lens;
-  prm.block_table = block_table;
-  prm.free_pages = free_pages;
-  prm.free_count = free_count;
-  prm.num_accepted = num_accepted;
-  prm.status = static_cast<uint32_t *>(workspace);
-  prm.B = B;
-  prm.n_q = n_q;
-  prm.n_q_next = n_q_next;
-  prm.max_pages = max_pages_per_seq;
-  prm.capacity = capacity;
-  const int threads = (B + 31) / 32 * 32;
-  kv_commit_kernel<<<1, threads, 0, stream>>>(prm);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return fail(SF_ERR_CUDA, "kv commit launch: %s", cudaGetErrorString(e));
-  return SF_OK;
+  return launch_kv_commit(seq_lens, block_table, free_pages, free_count, num_accepted, B, n_q, n_q_next,
+                          max_pages_per_seq, capacity, false, static_cast<uint32_t *>(workspace), stream);
 }
 
 }  // extern "C"

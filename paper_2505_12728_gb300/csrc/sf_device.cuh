@@ -496,4 +496,17 @@ __device__ __forceinline__ void set_status(uint32_t *status, uint32_t bits) {
   atomicOr(status, bits);
 }
 
+// Lets the next kernel on the stream start once all stores of the grid can be read by
+// it, also by bulk copies that it issues before it waits for this one.  All threads of
+// the block call it, behind their stores.  (A block stays until its stores have arrived:
+// 35k rows 104 -> 110 us.)
+__device__ __forceinline__ void launch_dependents_after_stores() {
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    grid_launch_dependents();
+  }
+}
+
 }  // namespace sf

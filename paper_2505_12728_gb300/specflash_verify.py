@@ -39,6 +39,9 @@ EXPORTED_SYMBOLS = (
     "sf_verify_lm_head_accept_workspace_size", "sf_verify_lm_head_accept",
     "sf_add_rms_norm", "sf_kv_append_workspace_size", "sf_kv_append",
     "sf_shared_prefix_attention_workspace_size", "sf_shared_prefix_attention",
+    "sf_tree_mask_workspace_size", "sf_tree_mask", "sf_tree_attention_workspace_size", "sf_tree_attention",
+    "sf_tree_commit_workspace_size", "sf_tree_commit", "sf_attention_mass_workspace_size", "sf_attention_mass",
+    "sf_kv_evict_workspace_size", "sf_kv_evict",
 )
 
 _lock = threading.Lock()
@@ -133,6 +136,26 @@ def load_library(path: str | None = None):
         lib.sf_shared_prefix_attention.argtypes = [P, P, P, P, P, P, P, P, I, I, I, I, I, I, I, I,
                                                    I, I, F, P, P, P, S, P]
         lib.sf_shared_prefix_attention.restype = I
+        lib.sf_tree_mask_workspace_size.argtypes = []
+        lib.sf_tree_mask_workspace_size.restype = S
+        lib.sf_tree_mask.argtypes = [P, P, I, I, P, P, P, S, P]
+        lib.sf_tree_mask.restype = I
+        lib.sf_tree_attention_workspace_size.argtypes = [I] * 7
+        lib.sf_tree_attention_workspace_size.restype = S
+        lib.sf_tree_attention.argtypes = [P, P, P, P, P, P, L, I, I, I, I, I, I, I, I, F, P, P, P, S, P]
+        lib.sf_tree_attention.restype = I
+        lib.sf_tree_commit_workspace_size.argtypes = []
+        lib.sf_tree_commit_workspace_size.restype = S
+        lib.sf_tree_commit.argtypes = [P, P, P, P, P, I, P, P, I, I, I, I, I, I, I, P, P, P, P, I, P, P, I, P, S, P]
+        lib.sf_tree_commit.restype = I
+        lib.sf_attention_mass_workspace_size.argtypes = []
+        lib.sf_attention_mass_workspace_size.restype = S
+        lib.sf_attention_mass.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, I, F, P, P, S, P]
+        lib.sf_attention_mass.restype = I
+        lib.sf_kv_evict_workspace_size.argtypes = [I] * 4
+        lib.sf_kv_evict_workspace_size.restype = S
+        lib.sf_kv_evict.argtypes = [P, P, P, I, P, P, I, I, I, I, I, I, I, I, I, I, I, P, P, P, P, P, I, P, S, P]
+        lib.sf_kv_evict.restype = I
         _load_calls(lib)
         _lib = lib
         return lib
@@ -152,7 +175,8 @@ def _load_calls(lib):
     except ImportError:  # a library that it was linked with is gone
         return
     module.set_entries(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        lib.sf_add_rms_norm, lib.sf_kv_append, lib.sf_shared_prefix_attention)))
+        lib.sf_add_rms_norm, lib.sf_kv_append, lib.sf_shared_prefix_attention, lib.sf_tree_mask, lib.sf_tree_attention,
+        lib.sf_tree_commit, lib.sf_attention_mass, lib.sf_kv_evict)))
     _calls = module
 
 
@@ -857,3 +881,324 @@ def shared_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, grou
     if status:
         _check(status)
     return out, lse
+
+
+# --------------------------------------------------------------------------- #
+# trees of drafts, and a cache held at a budget                               #
+# --------------------------------------------------------------------------- #
+_I64, _U8 = torch.int64, torch.uint8
+
+
+def _workspace(workspace, size, device, stream):
+    if workspace is None:
+        workspace = _new(size, _U8, device, stream, zero=True)
+    _need_workspace(workspace)
+    return workspace
+
+
+def _matrix(t, name, dtype):
+    """The shape of a checked contiguous CUDA tensor with two dimensions."""
+    if not isinstance(t, _Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional tensor")
+    _need(t, name, dtype)
+    return t.shape
+
+
+def _layer_pointers(x, name, dtype, dim, shape=None):
+    """(ctypes array of the layers' device pointers, a layer's shape) of one tensor
+    [layers][...] or a sequence of tensors, each layer contiguous."""
+    if isinstance(x, _Tensor):
+        if x.dim() != dim + 1:
+            raise ValueError(f"{name} must have {dim + 1} dimensions (layers first) or be a list of tensors of {dim}")
+        count = x.shape[0]
+        if count and not x[0].is_contiguous():
+            raise ValueError(f"{name} must be contiguous within a layer")
+        each, step, first = x.shape[1:], x.stride(0) * x.element_size(), x.data_ptr()
+        pointers = [first + i * step for i in range(count)]
+        if x.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {x.dtype}")
+        if not x.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+    else:
+        count = len(x)
+        each = x[0].shape if count and isinstance(x[0], _Tensor) else None
+        for t in x:
+            _need(t, name, dtype, each)
+        if count and len(each) != dim:
+            raise ValueError(f"{name} must be tensors of {dim} dimensions")
+        pointers = [t.data_ptr() for t in x]
+    if shape is not None and count and tuple(each) != tuple(shape):
+        raise ValueError(f"{name} has layers of shape {tuple(each)}, expected {tuple(shape)}")
+    return (ctypes.c_void_p * max(count, 1))(*pointers), count, each
+
+
+def _same_count(counts):
+    if len(set(counts.values())) > 1:
+        raise ValueError("different numbers of layers: " + ", ".join(f"{k} {v}" for k, v in counts.items()))
+
+
+def _free_stack(free_pages, free_count):
+    if (free_pages is None) != (free_count is None):
+        raise ValueError("free_pages and free_count belong together")
+    if free_pages is None:
+        return None, None, 0
+    _need(free_pages, "free_pages", _I32)
+    _need(free_count, "free_count", _I32, (1,))
+    return free_pages.data_ptr(), free_count.data_ptr(), free_pages.numel()
+
+
+def tree_mask_workspace_size() -> int:
+    return int(load_library().sf_tree_mask_workspace_size())
+
+
+def tree_mask(parents, start=None, *, mask=None, positions=None, workspace=None, stream=None):
+    """sf_tree_mask: parents int32 [B][n] (each below its row; -1: a root, less: not
+    part of the tree), start int32 [B] or None.  Returns (mask int64 [B][n]: bit j
+    of row i for node i itself and the nodes above it; positions int32 [B][n]:
+    start plus the number of nodes above)."""
+    if _calls is not None and mask is not None and positions is not None and workspace is not None and stream is None:
+        status = _calls.tree_mask(parents, start, mask, positions, workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return mask, positions
+    B, n = shape = _matrix(parents, "parents", _I32)
+    if start is not None:
+        _need(start, "start", _I32, (B,))
+    if mask is None:
+        mask = _new(shape, _I64, parents.device, stream)
+    _need(mask, "mask", _I64, shape)
+    if positions is None:
+        positions = _new(shape, _I32, parents.device, stream)
+    _need(positions, "positions", _I32, shape)
+    workspace = _workspace(workspace, tree_mask_workspace_size(), parents.device, stream)
+    _check(load_library().sf_tree_mask(parents.data_ptr(), _ptr(start), B, n, mask.data_ptr(), positions.data_ptr(),
+                                       workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return mask, positions
+
+
+def tree_attention_workspace_size(B, n_q, H_q, H_kv, head_dim, max_pages_per_seq, page_size=PAGE_SIZE) -> int:
+    n = load_library().sf_tree_attention_workspace_size(B, n_q, H_q, H_kv, head_dim, max_pages_per_seq, page_size)
+    if n == 0:
+        raise SFError(1, "invalid tree-attention shape: " + load_library().sf_last_error().decode())
+    return int(n)
+
+
+def _attention_arguments(q, k_cache, block_table, seq_lens):
+    """Shapes of a checked q, key cache, block table and lengths."""
+    if not isinstance(q, _Tensor) or q.dim() != 4:
+        raise ValueError("q must be a tensor [B][n_q][H_q][d]")
+    B, n_q, H_q, d = q.shape
+    if not isinstance(k_cache, _Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a tensor [pages][H_kv][16][d]")
+    num_pages, H_kv, page, d2 = k_cache.shape
+    if d2 != d:
+        # the library sizes the caches' tensor maps from q's head_dim
+        raise ValueError("head_dim of q and caches differ")
+    _need(q, "q", _BF16)
+    _need(k_cache, "k_cache", _BF16)
+    rows, max_pages = _matrix(block_table, "block_table", _I32)
+    if rows != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected ({B}, max_pages)")
+    _need(seq_lens, "seq_lens", _I32, (B,))
+    return B, n_q, H_q, H_kv, d, page, num_pages, max_pages
+
+
+def tree_attention(q, k_cache, v_cache, block_table, seq_lens, mask, *, out=None, lse=None, workspace=None,
+                   softmax_scale=0.0, stream=None, with_lse=True):
+    """sf_tree_attention: verification attention of n_q <= 64 nodes of a tree.  q,
+    caches, block_table and seq_lens as for verify_attention (seq_lens 0: an idle
+    slot); mask int64 [B][n_q], or [n_q] for one tree in all sequences: bit j of
+    row i where it sees new row j (tree_mask makes it).  Rows that see nothing get
+    0 and an lse of -inf.  Returns (out bf16 [B][n_q][H_q][d], lse fp32
+    [B][n_q][H_q] or None)."""
+    if _calls is not None and out is not None and workspace is not None and stream is None and (
+            lse is not None or not with_lse):
+        status = _calls.tree_attention(q, k_cache, v_cache, block_table, seq_lens, mask, softmax_scale, out, lse,
+                                       workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return out, lse
+    B, n_q, H_q, H_kv, d, page, num_pages, max_pages = _attention_arguments(q, k_cache, block_table, seq_lens)
+    _need(v_cache, "v_cache", _BF16, k_cache.shape)
+    stride = 0
+    if isinstance(mask, _Tensor) and mask.dim() == 1:
+        _need(mask, "mask", _I64, (n_q,))
+    else:
+        stride = _row_stride(mask, "mask", _I64, (B, n_q))
+    if out is None:
+        out = _new(q.shape, _BF16, q.device, stream)
+    _need(out, "out", _BF16, q.shape)
+    if lse is None and with_lse:
+        lse = _new((B, n_q, H_q), _F32, q.device, stream)
+    if lse is not None:
+        _need(lse, "lse", _F32, (B, n_q, H_q))
+    if workspace is None:
+        workspace = _new(tree_attention_workspace_size(B, n_q, H_q, H_kv, d, max_pages, page), _U8, q.device, stream,
+                         zero=True)
+    _need_workspace(workspace)
+    _check(load_library().sf_tree_attention(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        mask.data_ptr(), stride, B, n_q, H_q, H_kv, d, page, num_pages, max_pages, softmax_scale, out.data_ptr(),
+        _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return out, lse
+
+
+def tree_commit_workspace_size() -> int:
+    return int(load_library().sf_tree_commit_workspace_size())
+
+
+def tree_commit(tokens, sampled, parents, k_caches, v_caches, block_table, seq_lens, *, num_accepted=None,
+                out_tokens=None, path=None, row_weights=None, n_q_next=None, free_pages=None, free_count=None,
+                workspace=None, stream=None):
+    """sf_tree_commit: the path that the target's tokens take through a tree, and its
+    keys and values moved to follow the context.  tokens (the nodes'), sampled (the
+    target's after each node) and parents int32 [B][n]; k_caches and v_caches bf16
+    [layers][pages][H_kv][16][d] or lists of the layers' caches; block_table and
+    seq_lens as for tree_attention.  With free_pages and free_count, seq_lens and
+    block_table are then prepared for the next tree of n_q_next nodes (None: n), as
+    by kv_commit.  Returns (num_accepted int32 [B], out_tokens int32 [B][n], path
+    int32 [B][n], row_weights fp32 [B][n])."""
+    if (_calls is not None and workspace is not None and stream is None and num_accepted is not None
+            and out_tokens is not None and path is not None and row_weights is not None):
+        status = _calls.tree_commit(tokens, sampled, parents, k_caches, v_caches, block_table, seq_lens, num_accepted,
+                                    out_tokens, path, row_weights, n_q_next, free_pages, free_count, workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return num_accepted, out_tokens, path, row_weights
+    B, n = shape = _matrix(tokens, "tokens", _I32)
+    _need(sampled, "sampled", _I32, shape)
+    _need(parents, "parents", _I32, shape)
+    k_ptrs, layers, cache = _layer_pointers(k_caches, "k_caches", _BF16, 4)
+    v_ptrs, v_layers, _ = _layer_pointers(v_caches, "v_caches", _BF16, 4, cache)
+    _same_count({"k_caches": layers, "v_caches": v_layers})
+    num_pages, H_kv, page, d = cache if layers else (1, 1, PAGE_SIZE, 64)
+    rows, max_pages = _matrix(block_table, "block_table", _I32)
+    if rows != B:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected ({B}, max_pages)")
+    _need(seq_lens, "seq_lens", _I32, (B,))
+    device = tokens.device
+    if num_accepted is None:
+        num_accepted = _new((B,), _I32, device, stream)
+    if out_tokens is None:
+        out_tokens = _new(shape, _I32, device, stream)
+    if path is None:
+        path = _new(shape, _I32, device, stream)
+    if row_weights is None:
+        row_weights = _new(shape, _F32, device, stream)
+    _need(num_accepted, "num_accepted", _I32, (B,))
+    _need(out_tokens, "out_tokens", _I32, shape)
+    _need(path, "path", _I32, shape)
+    _need(row_weights, "row_weights", _F32, shape)
+    free, count, capacity = _free_stack(free_pages, free_count)
+    workspace = _workspace(workspace, tree_commit_workspace_size(), device, stream)
+    _check(load_library().sf_tree_commit(
+        tokens.data_ptr(), sampled.data_ptr(), parents.data_ptr(), k_ptrs, v_ptrs, layers, block_table.data_ptr(),
+        seq_lens.data_ptr(), B, n, H_kv, d, page, num_pages, max_pages, num_accepted.data_ptr(), out_tokens.data_ptr(),
+        path.data_ptr(), row_weights.data_ptr(), n if n_q_next is None else n_q_next, free, count, capacity,
+        workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return num_accepted, out_tokens, path, row_weights
+
+
+def attention_mass_workspace_size() -> int:
+    return int(load_library().sf_attention_mass_workspace_size())
+
+
+def attention_mass(q, lse, k_cache, block_table, seq_lens, mass=None, *, row_weights=None, out=None,
+                   softmax_scale=0.0, workspace=None, stream=None):
+    """sf_attention_mass: the attention weight that the n_q rows of an attention call
+    gave each key of the context, per KV head.  q, k_cache, block_table and seq_lens
+    are that call's, lse what it returned; mass fp32 [B][H_kv][width] is added to
+    (None: 0), row_weights fp32 [B][n_q] weighs the rows (None: 1).  Returns out fp32
+    [B][H_kv][width], which may be mass; its entries from a sequence's context on
+    (seq_lens - n_q) are not written (a new one has zeros there, or mass's)."""
+    if _calls is not None and out is not None and workspace is not None and stream is None:
+        status = _calls.attention_mass(q, lse, k_cache, block_table, seq_lens, mass, row_weights, softmax_scale, out,
+                                       workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return out
+    B, n_q, H_q, H_kv, d, page, num_pages, max_pages = _attention_arguments(q, k_cache, block_table, seq_lens)
+    _need(lse, "lse", _F32, (B, n_q, H_q))
+    if mass is not None:
+        if not isinstance(mass, _Tensor) or mass.dim() != 3 or mass.shape[:2] != (B, H_kv):
+            raise ValueError(f"mass must be a tensor [{B}][{H_kv}][width]")
+        _need(mass, "mass", _F32)
+    if row_weights is not None:
+        _need(row_weights, "row_weights", _F32, (B, n_q))
+    if out is None:
+        shape = (B, H_kv, max_pages * page) if mass is None else mass.shape
+        out = _new(shape, _F32, q.device, stream, zero=True)
+        if mass is not None:
+            with torch.cuda.stream(stream):
+                out.copy_(mass)
+    if not isinstance(out, _Tensor) or out.dim() != 3 or out.shape[:2] != (B, H_kv):
+        raise ValueError(f"out must be a tensor [{B}][{H_kv}][width]")
+    _need(out, "out", _F32, out.shape if mass is None else mass.shape)
+    workspace = _workspace(workspace, attention_mass_workspace_size(), q.device, stream)
+    _check(load_library().sf_attention_mass(
+        q.data_ptr(), lse.data_ptr(), k_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), _ptr(mass),
+        _ptr(row_weights), B, n_q, H_q, H_kv, d, page, num_pages, max_pages, out.shape[2], softmax_scale,
+        out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return out
+
+
+def kv_evict_workspace_size(num_layers, B, H_kv, budget) -> int:
+    n = load_library().sf_kv_evict_workspace_size(num_layers, B, H_kv, budget)
+    if n == 0:
+        raise SFError(1, "invalid eviction shape: " + load_library().sf_last_error().decode())
+    return int(n)
+
+
+def kv_evict(mass, k_caches, v_caches, block_table, seq_lens, budget, *, first=0, recent=0, n_q=0, mass_out=None,
+             seq_lens_out=None, kept=None, free_pages=None, free_count=None, workspace=None, stream=None):
+    """sf_kv_evict: cuts every sequence of more than `budget` tokens (seq_lens - n_q) to
+    its budget.  Per layer and KV head the `first` tokens, the last `recent` ones and
+    those of largest mass stay, in their order; K, V and mass are compacted.  mass
+    fp32 [layers][B][H_kv][width], k_caches and v_caches bf16
+    [layers][pages][H_kv][16][d], mass_out (None: mass itself) and kept int32
+    [layers][B][H_kv][budget] (the kept positions; None: not wanted): one tensor, or
+    a list of the layers'.  seq_lens_out None: seq_lens itself.  With free_pages and
+    free_count the pages that are no longer needed go back to that stack.  Returns
+    (mass_out, seq_lens_out, kept)."""
+    if mass_out is None:
+        mass_out = mass
+    if seq_lens_out is None:
+        seq_lens_out = seq_lens
+    if _calls is not None and workspace is not None and stream is None:
+        status = _calls.kv_evict(mass, k_caches, v_caches, block_table, seq_lens, budget, first, recent, n_q, mass_out,
+                                 seq_lens_out, kept, free_pages, free_count, workspace)
+        if status is not None:
+            if status:
+                _check(status)
+            return mass_out, seq_lens_out, kept
+    B, max_pages = _matrix(block_table, "block_table", _I32)
+    _need(seq_lens, "seq_lens", _I32, (B,))
+    _need(seq_lens_out, "seq_lens_out", _I32, (B,))
+    k_ptrs, layers, cache = _layer_pointers(k_caches, "k_caches", _BF16, 4)
+    v_ptrs, v_layers, _ = _layer_pointers(v_caches, "v_caches", _BF16, 4, cache)
+    m_ptrs, m_layers, m = _layer_pointers(mass, "mass", _F32, 3)
+    o_ptrs, o_layers, _ = _layer_pointers(mass_out, "mass_out", _F32, 3, m)
+    counts = {"mass": m_layers, "k_caches": layers, "v_caches": v_layers, "mass_out": o_layers}
+    _same_count(counts)
+    if not layers:
+        raise ValueError("no layers")
+    num_pages, H_kv, page, d = cache
+    if tuple(m[:2]) != (B, H_kv):
+        raise ValueError(f"mass has layers of shape {tuple(m)}, expected ({B}, {H_kv}, width)")
+    kept_ptrs = None
+    if kept is not None:
+        kept_ptrs, counts["kept"], _ = _layer_pointers(kept, "kept", _I32, 3, (B, H_kv, budget))
+        _same_count(counts)
+    free, count, capacity = _free_stack(free_pages, free_count)
+    if workspace is None:
+        workspace = _new(kv_evict_workspace_size(layers, B, H_kv, budget), _U8, block_table.device, stream, zero=True)
+    _need_workspace(workspace)
+    _check(load_library().sf_kv_evict(
+        m_ptrs, k_ptrs, v_ptrs, layers, block_table.data_ptr(), seq_lens.data_ptr(), B, H_kv, d, page, num_pages,
+        max_pages, m[2], budget, first, recent, n_q, o_ptrs, seq_lens_out.data_ptr(), kept_ptrs, free, count, capacity,
+        workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    return mass_out, seq_lens_out, kept
