@@ -198,26 +198,6 @@ __device__ __forceinline__ float sp_max3(float a, float b, float c) {
   return d;
 }
 
-// Two fp32 values in one 64-bit register: one instruction for both.
-__device__ __forceinline__ unsigned long long sp_pair(float x, float y) {
-  unsigned long long v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
-  return v;
-}
-__device__ __forceinline__ void sp_unpair(unsigned long long v, float &x, float &y) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
-}
-__device__ __forceinline__ unsigned long long sp_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-  unsigned long long d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ unsigned long long sp_add2(unsigned long long a, unsigned long long b) {
-  unsigned long long d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 template <int D, int STAGES>
 __global__ void __maxnreg__(kSpMaxRegs)
 shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
@@ -846,7 +826,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           }
         }
         mu = ref == -INFINITY ? 0.f : ref;
-        const unsigned long long scale2 = sp_pair(p.scale_log2, p.scale_log2), mu2 = sp_pair(-mu, -mu);
+        const unsigned long long scale2 = f32x2(p.scale_log2, p.scale_log2), mu2 = f32x2(-mu, -mu);
         unsigned long long sum = 0ull;
         // The tile's weights, and with `rest` what their rounding left, as a second term,
         // to columns [64, 128): two loops, as the branch inside of one made the tiles
@@ -859,14 +839,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             for (int i = 0; i < 16; ++i) {
               const int k0 = 32 * ch + 2 * i;
               float x0, x1;
-              sp_unpair(sp_fma2(sp_pair(__uint_as_float(sv[k0]), __uint_as_float(sv[k0 + 1])), scale2, mu2), x0, x1);
+              f32x2_split(f32x2_fma(f32x2(__uint_as_float(sv[k0]), __uint_as_float(sv[k0 + 1])), scale2, mu2), x0, x1);
               const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
               if constexpr (decltype(rest)::value) {
                 sv[k0] = __float_as_uint(p0);
                 sv[k0 + 1] = __float_as_uint(p1);
               }
               w[i] = pack_bf16x2(p0, p1);
-              sum = sp_add2(sum, sp_pair(p0, p1));
+              sum = f32x2_add(sum, f32x2(p0, p1));
             }
             tmem_st_32x32b_x16(ts + 16 * ch, w);
             if constexpr (decltype(rest)::value) {
@@ -891,7 +871,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         else put_weights(std::false_type());
         if (!ok) break;
         float sum0, sum1;
-        sp_unpair(sum, sum0, sum1);
+        f32x2_split(sum, sum0, sum1);
         l_run = l_run * alpha + (sum0 + sum1);
         tmem_wait_st();
         tc_fence_before_sync();
