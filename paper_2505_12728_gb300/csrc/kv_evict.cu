@@ -22,16 +22,21 @@
 //
 // The last cluster to finish writes the lengths and, if asked to, gives the pages
 // that are no longer needed back to the free-page stack.
+#include <mutex>
+
 #include "sf_device.cuh"
 #include "sf_host.h"
 
 namespace sf {
 
-constexpr int kEvictThreads = 512;
+constexpr int kEvictThreads = 256;
+constexpr int kEvictBlocks = 3;        // CTAs per SM
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictBins = 2048;
-constexpr int kEvictBatch = 8;         // 16-byte loads of a thread in flight
+constexpr int kEvictSlot = 4096;       // bytes of a warp's rows of a round
+constexpr int kEvictKeys = 8;          // keys of a thread in flight
 constexpr int kEvictMaxCluster = 8;
+constexpr int kEvictSmem = 2 * kEvictWarps * kEvictSlot > 5 * kEvictBins * 4 ? 2 * kEvictWarps * kEvictSlot : 5 * kEvictBins * 4;
 
 struct EvictLayer {
   const float *mass;
@@ -67,6 +72,16 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Bulk copies of rows back to global memory, in groups of the issuing thread.
+__device__ __forceinline__ void bulk_copy_s2g(void *dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)), "r"(src),
+               "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t ld_dsmem_u32(uint32_t local, uint32_t rank) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(local, rank)) : "memory");
@@ -97,11 +112,16 @@ __device__ __forceinline__ uint32_t evict_scan(uint32_t v, uint32_t *s_warp, uin
 }
 
 template <int C>
-__global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const __grid_constant__ EvictParams p) {
-  __shared__ uint32_t s_hist[3][kEvictBins];
-  __shared__ uint32_t s_warp[kEvictWarps], s_pick[2], s_count[2];
+__global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(const __grid_constant__ EvictParams p) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  // while the keys are chosen; then the slots of the rows on their way, two a warp
+  uint32_t(*s_hist)[kEvictBins] = reinterpret_cast<uint32_t(*)[kEvictBins]>(smem);
+  uint32_t *s_total = s_hist[3];  // a histogram of all CTAs
+  uint32_t *s_few = s_hist[4];    // keys in the first digit's bin
+  __shared__ __align__(8) uint64_t s_bar[kEvictWarps][2];
+  __shared__ uint32_t s_found, s_warp[kEvictWarps], s_pick[2], s_count[2];
   __shared__ uint32_t s_last;
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
   const int rank = C > 1 ? static_cast<int>(blockIdx.x % C) : 0, task = blockIdx.x / C;
   const int h = task % p.H_kv, lb = task / p.H_kv, b = lb % p.B;
   const EvictLayer &layer = p.layers[lb / p.B];
@@ -111,6 +131,11 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const __grid_co
     else __syncthreads();
   };
   for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) s_hist[0][i] = 0u;
+  if (tid == 0) {
+    s_found = 0u;
+    for (int i = 0; i < 2 * kEvictWarps; ++i) mbar_init(smem_addr(&s_bar[0][0]) + 8 * i, 1);
+    fence_mbar_init();
+  }
   grid_dependency_wait();
   bool cut;
   const int L = evict_length(p, b, cut, task / p.H_kv < p.B && h == 0 && rank == 0 && tid == 0);
@@ -128,135 +153,253 @@ __global__ void __launch_bounds__(kEvictThreads) kv_evict_kernel(const __grid_co
   } else {
     const int per = (L + C - 1) / C, from = min(rank * per, L), to = min(from + per, L);
     const int late = L - p.recent;
-    auto key_at = [&](int t) -> uint32_t {
-      return t < p.first || t >= late ? 0xffffffffu : evict_key(mass[t]);
-    };
+    auto key_of = [&](int t, float w) -> uint32_t { return t < p.first || t >= late ? 0xffffffffu : evict_key(w); };
     uint32_t found = 0u, left = static_cast<uint32_t>(p.budget);
+    uint32_t mine = 0u;  // keys of this thread's bins above `found`, of this CTA
+    auto count_keys = [&](uint32_t *hist, bool in, uint32_t bin) {
+      // one add for the lanes that agree with the first: weights cluster, and equal
+      // addresses are served one after the other
+      const unsigned any = __ballot_sync(0xffffffffu, in);
+      if (!any) return;
+      if (!in) bin = kEvictBins;
+      const int lead = __ffs(any) - 1;
+      const uint32_t common = __shfl_sync(0xffffffffu, bin, lead);
+      const unsigned same = __ballot_sync(0xffffffffu, bin == common);
+      if (lane == lead) atomicAdd(&hist[common], static_cast<uint32_t>(__popc(same)));
+      else if (in && bin != common) atomicAdd(&hist[bin], 1u);
+    };
+    // all keys of this CTA's positions, kEvictKeys of a thread at a time
+    auto each_key = [&](auto &&f) {
+      float next[kEvictKeys];
+      auto load = [&](int t0) {
+#pragma unroll
+        for (int u = 0; u < kEvictKeys; ++u) {
+          const int t = t0 + u * kEvictThreads + tid;
+          next[u] = t < to ? mass[t] : 0.f;
+        }
+      };
+      load(from);
+      for (int t0 = from; t0 < to; t0 += kEvictThreads * kEvictKeys) {
+        float now[kEvictKeys];
+#pragma unroll
+        for (int u = 0; u < kEvictKeys; ++u) now[u] = next[u];
+        load(t0 + kEvictThreads * kEvictKeys);
+#pragma unroll
+        for (int u = 0; u < kEvictKeys; ++u) {
+          const int t = t0 + u * kEvictThreads + tid;
+          f(t < to, key_of(t, now[u]));
+        }
+      }
+    };
+    each_key([&](bool in, uint32_t key) { count_keys(s_hist[0], in, key >> 21); });
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
-      const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, width = round == 2 ? 10 : 11;
       uint32_t *hist = s_hist[round];
-      for (int t0 = from; t0 < to; t0 += kEvictThreads) {
-        const int t = t0 + tid;
-        const uint32_t key = t < to ? key_at(t) : 0u;
-        const bool in = t < to && (round == 0 || (key >> (shift + width)) == (found >> (shift + width)));
-        const uint32_t bin = in ? (key >> shift) & ((1u << width) - 1u) : kEvictBins;
-        // one add for the lanes that agree with the first: weights cluster, and equal
-        // addresses are served one after the other
-        const unsigned any = __ballot_sync(0xffffffffu, in);
-        if (!any) continue;
-        const int lead = __ffs(any) - 1;
-        const uint32_t common = __shfl_sync(0xffffffffu, bin, lead);
-        const unsigned same = __ballot_sync(0xffffffffu, bin == common);
-        if (lane == lead) atomicAdd(&hist[common], static_cast<uint32_t>(__popc(same)));
-        else if (in && bin != common) atomicAdd(&hist[bin], 1u);
-      }
       sync_all();
       // the bin that holds the left-th key from the top
       constexpr int kPer = kEvictBins / kEvictThreads;
+      if constexpr (C > 1) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          uint32_t n = 0;
+#pragma unroll
+          for (int r = 0; r < C; ++r) n += ld_dsmem_u32(smem_addr(&hist[i * kEvictThreads + tid]), r);
+          s_total[i * kEvictThreads + tid] = n;
+        }
+        __syncthreads();
+      }
+      const uint32_t *bins = C > 1 ? s_total : hist;
+      const int top = kEvictBins - kPer * (tid + 1);  // the thread's bins top .. top + kPer - 1
       uint32_t n[kPer], sum = 0;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int bin = kEvictBins - 1 - (tid * kPer + i);
-        n[i] = 0;
-        if constexpr (C > 1) {
-#pragma unroll
-          for (int r = 0; r < C; ++r) n[i] += ld_dsmem_u32(smem_addr(&hist[bin]), r);
-        } else {
-          n[i] = hist[bin];
-        }
-        sum += n[i];
+      for (int i = 0; i < kPer; i += 4) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(bins + top + i);
+        n[i] = x.x;
+        n[i + 1] = x.y;
+        n[i + 2] = x.z;
+        n[i + 3] = x.w;
+        sum += x.x + x.y + x.z + x.w;
       }
       uint32_t total, above = evict_scan(sum, s_warp, &total);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
+      for (int i = kPer - 1; i >= 0; --i) {
         if (above < left && left <= above + n[i]) {
-          s_pick[0] = kEvictBins - 1 - (tid * kPer + i);
+          s_pick[0] = top + i;
           s_pick[1] = left - above;
         }
         above += n[i];
       }
       __syncthreads();
-      found |= s_pick[0] << shift;
+      const uint32_t pick = s_pick[0];
+      if constexpr (C > 1) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (static_cast<uint32_t>(top + i) > pick) mine += hist[top + i];
+      }
+      found |= pick << (round == 0 ? 21 : round == 1 ? 10 : 0);
       left = s_pick[1];
+      if (round == 2) break;
+      if (round == 0) {
+        // the keys of that bin, which the other digits are taken from
+        each_key([&](bool in, uint32_t key) {
+          const bool take = in && (key >> 21) == (found >> 21);
+          const unsigned who = __ballot_sync(0xffffffffu, take);
+          if (!who) return;
+          uint32_t at = 0;
+          if (lane == 0) at = atomicAdd(&s_found, static_cast<uint32_t>(__popc(who)));
+          at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+          if (take && at < kEvictBins) s_few[at] = key;
+        });
+      }
       __syncthreads();
+      const int few = s_found;
+      if (few <= kEvictBins) {
+        for (int i = tid; i < (few + 31) / 32 * 32; i += kEvictThreads) {
+          const uint32_t key = i < few ? s_few[i] : 0u;
+          if (round == 0) count_keys(s_hist[1], i < few, (key >> 10) & 2047u);
+          else count_keys(s_hist[2], i < few && (key >> 10) == (found >> 10), key & 1023u);
+        }
+      } else if (round == 0) {
+        each_key([&](bool in, uint32_t key) { count_keys(s_hist[1], in && (key >> 21) == (found >> 21), (key >> 10) & 2047u); });
+      } else {
+        each_key([&](bool in, uint32_t key) { count_keys(s_hist[2], in && (key >> 10) == (found >> 10), key & 1023u); });
+      }
     }
-    // keys above `found` are kept, and the first `left` of those equal to it
+    // Keys above `found` are kept, and the first `left` of those equal to it.  In front
+    // of this CTA's positions:
     uint32_t larger = 0, equal = 0;
     if constexpr (C > 1) {
-      uint32_t mine = 0;
-      for (int t = from + tid; t < to; t += kEvictThreads) {
-        const uint32_t key = key_at(t);
-        mine += key > found ? 1u : 0u;
-        equal += key == found ? 1u : 0u;
-      }
-      uint32_t sum_l, sum_e;
-      (void)evict_scan(mine, s_warp, &sum_l);
-      (void)evict_scan(equal, s_warp, &sum_e);
+      uint32_t sum;
+      (void)evict_scan(mine, s_warp, &sum);
       if (tid == 0) {
-        s_count[0] = sum_l;
-        s_count[1] = sum_e;
+        s_count[0] = sum;
+        s_count[1] = s_hist[2][found & 1023u];
       }
       cluster_sync();
-      larger = equal = 0;
       for (int r = 0; r < rank; ++r) {
         larger += ld_dsmem_u32(smem_addr(&s_count[0]), r);
         equal += ld_dsmem_u32(smem_addr(&s_count[1]), r);
       }
     }
-    for (int t0 = from; t0 < to; t0 += kEvictThreads) {
-      const int t = t0 + tid;
-      const uint32_t key = t < to ? key_at(t) : 0u;
-      const bool gt = t < to && key > found, eq = t < to && key == found;
-      uint32_t total;
-      const uint32_t before = evict_scan((gt ? 1u : 0u) | (eq ? 0x10000u : 0u), s_warp, &total);
-      const uint32_t l = larger + (before & 0xffffu), e = equal + (before >> 16);
-      if (gt || (eq && e < left)) kept[l + min(e, left)] = t;
-      larger += total & 0xffffu;
-      equal += total >> 16;
+    float coming[kEvictKeys];
+    auto load_row = [&](int t0) {  // a warp has 32 * kEvictKeys positions in a row
+#pragma unroll
+      for (int u = 0; u < kEvictKeys; ++u) {
+        const int t = t0 + (warp * kEvictKeys + u) * 32 + lane;
+        coming[u] = t < to ? mass[t] : 0.f;
+      }
+    };
+    load_row(from);
+    for (int t0 = from; t0 < to; t0 += kEvictThreads * kEvictKeys) {
+      const int t1 = t0 + warp * 32 * kEvictKeys + lane;
+      uint32_t key[kEvictKeys], count = 0;
+#pragma unroll
+      for (int u = 0; u < kEvictKeys; ++u) key[u] = key_of(t1 + 32 * u, coming[u]);
+      load_row(t0 + kEvictThreads * kEvictKeys);
+#pragma unroll
+      for (int u = 0; u < kEvictKeys; ++u) {
+        const bool in = t1 + 32 * u < to;
+        count += __popc(__ballot_sync(0xffffffffu, in && key[u] > found)) +
+                 (__popc(__ballot_sync(0xffffffffu, in && key[u] == found)) << 16);
+      }
+      __syncthreads();
+      if (lane == 0) s_warp[warp] = count;
+      __syncthreads();
+      uint32_t l = larger, e = equal;
+#pragma unroll
+      for (int w = 0; w < kEvictWarps; ++w) {
+        const uint32_t x = s_warp[w];
+        if (w < warp) {
+          l += x & 0xffffu;
+          e += x >> 16;
+        }
+        larger += x & 0xffffu;
+        equal += x >> 16;
+      }
+      const unsigned lower = (1u << lane) - 1u;
+#pragma unroll
+      for (int u = 0; u < kEvictKeys; ++u) {
+        const bool in = t1 + 32 * u < to, gt = in && key[u] > found, eq = in && key[u] == found;
+        const unsigned g = __ballot_sync(0xffffffffu, gt), q = __ballot_sync(0xffffffffu, eq);
+        const uint32_t before = e + __popc(q & lower);
+        if (gt || (eq && before < left)) kept[l + __popc(g & lower) + min(before, left)] = t1 + 32 * u;
+        l += __popc(g);
+        e += __popc(q);
+      }
     }
     sync_all();
-    // rows in rounds of ascending places
-    const int wide = p.D / 8, kv_wide = 2 * wide;  // 16-byte pieces of a row of K, and of K and V
-    const int rows = min(kEvictThreads * kEvictBatch / kv_wide, kEvictThreads);  // of a CTA and round
+    // Rows in rounds of ascending places, by asynchronous copies: a warp has some rows of
+    // every round and two slots of shared memory, so that a round's rows are on their way
+    // in while the round before waits for its barrier and goes out.  Where they come from
+    // and go to is looked up a round ahead of that.
+    const int row_bytes = p.D * 2, R = min(16, kEvictSlot / (2 * row_bytes));
     const int32_t *table = p.block_table + static_cast<size_t>(b) * p.max_pages;
-    auto place = [&](int pos) -> long long {
+    auto place = [&](int pos) -> int {
       const int page = table[pos / SF_PAGE_SIZE];
       if (page < 0 || page >= p.num_pages) {
         set_status(p.status, SF_DEVICE_BAD_PAGE);
         return -1;
       }
-      return ((static_cast<long long>(page) * p.H_kv + h) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE) * wide;
+      return (page * p.H_kv + h) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE;
     };
-    for (int j0 = 0; j0 < p.budget; j0 += C * rows) {
-      const int base = j0 + rank * rows;
-      uint4 v[kEvictBatch];
-      uint4 *dst[kEvictBatch];
-      float w = 0.f;
-      if (tid < rows && base + tid < p.budget) w = mass[kept[base + tid]];
-#pragma unroll
-      for (int u = 0; u < kEvictBatch; ++u) {
-        const int x = u * kEvictThreads + tid, r = x / kv_wide, piece = x - r * kv_wide, j = base + r;
-        dst[u] = nullptr;
-        if (r < rows && j < p.budget) {
-          const int pos = kept[j];
-          if (pos != j) {
-            const long long src = place(pos), at = place(j);
-            uint4 *cache = piece < wide ? layer.k : layer.v;
-            const int c = piece < wide ? piece : piece - wide;
-            if (src >= 0 && at >= 0) {
-              v[u] = cache[src + c];
-              dst[u] = cache + at + c;
-            }
-          }
+    const int r = lane % R, side = lane / R;  // the lane's row of the warp's, and K or V
+    const int first_row = (rank * kEvictWarps + warp) * R + r, rows = C * kEvictWarps * R;
+    const int rounds = (p.budget + rows - 1) / rows;
+    char *cache = reinterpret_cast<char *>(side == 0 ? layer.k : layer.v);
+    const uint32_t slot = smem_addr(smem) + warp * 2 * kEvictSlot + (side * R + r) * row_bytes;
+    const uint32_t bar = smem_addr(&s_bar[warp][0]);
+    struct Row {
+      int src, dst;  // cache rows, dst < 0: stays
+      float w;
+    };
+    auto look_up = [&](int round) -> Row {
+      Row x{-1, -1, 0.f};
+      const int j = round * rows + first_row;
+      if (side < 2 && j < p.budget) {
+        const int pos = kept[j];
+        x.w = mass[pos];
+        if (pos != j) {
+          x.src = place(pos);
+          x.dst = place(j);
+          if (x.src < 0) x.dst = -1;
         }
       }
-      sync_all();
-#pragma unroll
-      for (int u = 0; u < kEvictBatch; ++u)
-        if (dst[u]) *dst[u] = v[u];
-      if (tid < rows && base + tid < p.budget) mass_out[base + tid] = w;
+      return x;
+    };
+    bool ok = true;
+    auto copy_in = [&](int round, const Row &x) {
+      const unsigned who = __ballot_sync(0xffffffffu, x.dst >= 0);
+      const uint32_t full = bar + 8 * (round & 1);
+      if (lane == 0) mbar_arrive_expect_tx(full, static_cast<uint32_t>(__popc(who) * row_bytes));
+      __syncwarp();
+      if (x.dst >= 0)
+        bulk_copy_g2s(slot + (round & 1) * kEvictSlot, cache + static_cast<long long>(x.src) * row_bytes, row_bytes, full);
+    };
+    asm volatile("fence.proxy.async;" ::: "memory");  // the slots held the histograms
+    __syncthreads();
+    Row now = look_up(0), next = look_up(1);
+    copy_in(0, now);
+#pragma unroll 1
+    for (int round = 0; round < rounds; ++round) {
+      if (round + 1 < rounds) {
+        bulk_wait_read();  // this lane's rows of the round before have left the slot
+        __syncwarp();
+        copy_in(round + 1, next);
+      }
+      const Row then = look_up(round + 2);
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar + 8 * (round & 1), (round >> 1) & 1)) && ok;
+      sync_all();  // every row of this round and of those before is in
+      if (ok && now.dst >= 0) {
+        bulk_copy_s2g(cache + static_cast<long long>(now.dst) * row_bytes, slot + (round & 1) * kEvictSlot, row_bytes);
+        bulk_commit();
+      }
+      const int j = round * rows + first_row;
+      if (side == 0 && j < p.budget) mass_out[j] = now.w;
+      now = next;
+      next = then;
     }
+    bulk_wait_all();
+    if (!ok && lane == 0) set_status(p.status, SF_DEVICE_TIMEOUT);
     sync_all();
     for (int t = p.budget + rank * kEvictThreads + tid; t < p.width; t += C * kEvictThreads) mass_out[t] = 0.f;
   }
@@ -312,9 +455,27 @@ static int check_evict(int layers, int B, int H_kv, int budget) {
   return SF_OK;
 }
 
+static int evict_setup(int device) {
+  static std::mutex mu;
+  static bool done[64] = {};
+  if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
+  std::lock_guard<std::mutex> lock(mu);
+  if (done[device]) return SF_OK;
+  for (auto fn : {kv_evict_kernel<1>, kv_evict_kernel<2>, kv_evict_kernel<4>, kv_evict_kernel<8>}) {
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictSmem);
+    if (e != cudaSuccess) return fail(SF_ERR_CUDA, "cudaFuncSetAttribute (eviction): %s", cudaGetErrorString(e));
+  }
+  done[device] = true;
+  return SF_OK;
+}
+
+// CTAs per (layer, sequence, KV head): as many as still have an SM each.  A cluster's
+// barriers in every round cost more than they bring once a CTA shares its SM (128 heads
+// of 3008 keys to 1024: 43 us with one CTA a head, 53 with two; 32 heads: 41 with one, 31
+// with four; 4 heads of 32768 keys to 4096: 172 with one, 47 with eight).
 static int evict_cluster(int tasks, int sms) {
   int C = 1;
-  while (C < kEvictMaxCluster && static_cast<long long>(tasks) * C < 2LL * sms) C *= 2;
+  while (C < kEvictMaxCluster && 2LL * tasks * C <= sms) C *= 2;
   return C;
 }
 
@@ -339,6 +500,8 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
     return fail(SF_ERR_UNSUPPORTED, "head_dim=%d (a multiple of 8 in [8, 256])", head_dim);
   if (page_size != SF_PAGE_SIZE) return fail(SF_ERR_UNSUPPORTED, "page_size=%d (built: 16)", page_size);
   if (num_pages < 1) return fail(SF_ERR_INVALID_ARG, "num_pages=%d", num_pages);
+  if ((long long)num_pages * H_kv * SF_PAGE_SIZE >= (1LL << 31))
+    return fail(SF_ERR_UNSUPPORTED, "KV pool of %d pages x %d heads too large", num_pages, H_kv);
   if (max_pages_per_seq < 1 || (long long)max_pages_per_seq * page_size > (1LL << 30))
     return fail(SF_ERR_INVALID_ARG, "max_pages_per_seq=%d", max_pages_per_seq);
   if (mass_width < 1 || mass_width > (1 << 30)) return fail(SF_ERR_INVALID_ARG, "mass_width=%d", mass_width);
@@ -404,9 +567,11 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tasks * C));
   cfg.blockDim = dim3(kEvictThreads);
+  cfg.dynamicSmemBytes = kEvictSmem;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = C > 1 ? 2 : 1;
+  if ((st = evict_setup(dev.ordinal)) != SF_OK) return st;
   auto kernel = C == 1 ? kv_evict_kernel<1> : C == 2 ? kv_evict_kernel<2> : C == 4 ? kv_evict_kernel<4> : kv_evict_kernel<8>;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "eviction launch: %s", cudaGetErrorString(e));
