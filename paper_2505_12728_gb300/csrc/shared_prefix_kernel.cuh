@@ -115,6 +115,9 @@ struct SpParams {
   const unsigned long long *mask;  // a tree's: bit j of a row where it sees new row j
   long long mask_stride;           // elements from one sequence's masks to the next
   int row_tiles;                   // of a sequence's rows (a tree's)
+  int paired;                      // KV heads in pairs (a tree's rows in one row tile)
+  int folds;                       // pairs of row tiles: neighbouring CTAs take one each of the same keys
+  uint32_t fold_rows;              // partial rows of one
   int B, n_q, H_q, H_kv, group, num_pages, num_groups, max_prefix_pages, max_pages;
   int tokens_per_tile;  // floor(128 / group), at least 16
   uint32_t tile_magic;
@@ -161,7 +164,7 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
   x.token0 = first * p.n_q;
   x.tokens = sequences * p.n_q;
   x.tiles = own ? 1 : sp_tiles(p, x.tokens + p.tokens_per_tile - 1);
-  x.pairs = (x.tiles + 1) >> 1;
+  x.pairs = TREE ? 1 : (x.tiles + 1) >> 1;
   x.key_tiles = (keys + kSpTile - 1) / kSpTile;
   x.few = own && !TREE ? 0u : kSpCostFew;
   if (own) {
@@ -171,7 +174,8 @@ __device__ __forceinline__ SpEntity sp_entity(const SpParams &p, bool own, int f
     x.slot_rows = 2u * static_cast<uint32_t>(x.tokens * p.group);
   } else {
     x.units = p.H_kv;
-    x.head_cost = static_cast<uint32_t>(x.tiles >> 1) * x.length(1, x.key_tiles) + (x.tiles & 1) * x.length(0, x.key_tiles);
+    if (TREE) x.head_cost = x.length(x.tiles > 1, x.key_tiles);
+    else x.head_cost = static_cast<uint32_t>(x.tiles >> 1) * x.length(1, x.key_tiles) + (x.tiles & 1) * x.length(0, x.key_tiles);
     x.cost = x.units * x.head_cost;
     x.slot_rows = x.tiles > 1 ? 2u * kSpTile : static_cast<uint32_t>(x.tokens * p.group);
   }
@@ -334,7 +338,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       __syncwarp();
     }
     auto entity = [&](int e) -> SpEntity {
-      if constexpr (TREE) return sp_entity<true>(p, p.row_tiles == 1, e, 1, s_len[e]);
+      if constexpr (TREE) return sp_entity<true>(p, p.paired != 0, e, 1, s_len[e]);
       const bool own = e >= p.num_groups;
       const int first = own ? e - p.num_groups : s_start[e];
       return sp_entity<false>(p, own, first, own ? 1 : s_start[e + 1] - first, s_len[e]);
@@ -352,8 +356,12 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll 1
     for (int e = lane; e < E; e += 32) sum += entity(e).cost;
     const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum), chunk = sp_chunk(p, Tot);
-    const uint32_t c = blockIdx.x;
-    const bool writes = c == gridDim.x - 1;  // this CTA (with the least to do) leaves the plan for the merge kernel
+    // (a tree's: the CTAs of the same keys are neighbours, so that what one reads the others
+    // find in L2: 4 sequences of 32768 tokens, 61 nodes, 28 / 4 heads read 536 MB one pair
+    // of row tiles behind the other)
+    const uint32_t c = TREE ? blockIdx.x / p.folds : blockIdx.x;
+    const int fold = TREE ? blockIdx.x - c * p.folds : 0;
+    const bool writes = blockIdx.x == gridDim.x - 1;  // this CTA (with the least to do) leaves the plan for the merge kernel
     const uint32_t at = min(c * chunk, Tot), end = min(at + chunk, Tot);
     // the entity that position `at` lies in, with the costs and partial rows before it
     int e = E;
@@ -416,6 +424,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       pair = x.pairs > 1 ? static_cast<int>(sp_div(in - h * x.head_cost, x.length(1, x.key_tiles))) : 0;
       base = e_cost + h * x.head_cost + pair * x.length(1, x.key_tiles);
       slot = e_slot + (h * x.pairs + pair) * x.slot_rows + 2u * kSpTile * c;
+      if (TREE) slot += fold * p.fold_rows;
     }
     const uint64_t again = l2_policy_evict_last();
     uint32_t published = 0, jobs[2] = {0, 0};
@@ -430,10 +439,11 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       SpItem it;
       it.n = 0;
       while (it.n == 0 && e < E && base < end) {
-        const bool own = TREE ? p.row_tiles == 1 : e >= p.num_groups;
-        const int dual = 2 * pair + 1 < x.tiles, duo = own && 2 * h + 1 < p.H_kv, key_tiles = x.key_tiles << duo;
-        it.t0 = x.tile_at(at, base, dual, key_tiles);
-        it.n = x.tile_at(end, base, dual, key_tiles) - it.t0;
+        const bool own = TREE ? p.paired != 0 : e >= p.num_groups;
+        const int mine = TREE ? fold : pair;  // the pair of row tiles
+        const int dual = 2 * mine + 1 < x.tiles, along = TREE ? x.tiles > 1 : dual, duo = own && 2 * h + 1 < p.H_kv, key_tiles = x.key_tiles << duo;
+        it.t0 = x.tile_at(at, base, along, key_tiles);
+        it.n = x.tile_at(end, base, along, key_tiles) - it.t0;
         if (it.n > 0) {
           it.keys = x.keys;
           it.own = own;
@@ -441,7 +451,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           it.h = own ? 2 * h : h;
           it.dual = dual;
           it.duo = duo;
-          it.again = x.pairs > 1;
+          it.again = !TREE && x.pairs > 1;
           // Among a sequence's first keys lie those of rows that see few, and those that
           // may carry a row alone (attention sinks): there the roundings of the weights
           // do not average out.
@@ -450,7 +460,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             const int g = group_of(it.row);
             first_keys = s_start[g + 1] == s_start[g] || s_len[g] < kSpTile;
           }
-          const int rows0 = sp_rows(p, x, 2 * pair), tok0 = x.token0 + 2 * pair * p.tokens_per_tile;
+          const int rows0 = sp_rows(p, x, 2 * mine), tok0 = x.token0 + 2 * mine * p.tokens_per_tile;
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             auto &j = it.s[s];
@@ -463,7 +473,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             if (dual) {  // a row tile each
               if (s == 1) {
                 j.token += p.tokens_per_tile;
-                j.rows = sp_rows(p, x, 2 * pair + 1);
+                j.rows = sp_rows(p, x, 2 * mine + 1);
                 j.slot += kSpTile;
               }
             } else if (duo) {  // a head each
@@ -483,7 +493,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           if (!dual && !duo && it.n == 1) turn ^= 1;
         }
         // the next segment
-        base += x.length(dual, key_tiles);
+        base += x.length(along, key_tiles);
         slot += x.slot_rows;
         if (++pair == x.pairs) {
           pair = 0;
@@ -1082,20 +1092,23 @@ struct SpJoin {
 
 // Appends the first partial rows of a row tile's partials of one segment to
 // list[n ..]; returns the new length.  A whole warp calls it.
+template <bool TREE>
 __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32_t cost, uint32_t slot, const SpEntity &x,
                                        bool own, int h, int tile, uint32_t *list, int n) {
   if (x.head_cost == 0) return n;
-  const int lane = threadIdx.x & 31, pair = tile >> 1, dual = 2 * pair + 1 < x.tiles;
+  const int lane = threadIdx.x & 31, dual = tile + 1 - (tile & 1) < x.tiles, pair = TREE ? 0 : tile >> 1;
+  const int along = TREE ? x.tiles > 1 : dual;
   const int duo = own && (h | 1) < p.H_kv, second = h & 1, unit = own ? h >> 1 : h, key_tiles = x.key_tiles << duo;
   const uint32_t base = cost + unit * x.head_cost + pair * x.length(1, x.key_tiles);
+  if (TREE) slot += (tile >> 1) * p.fold_rows;
   slot += (unit * x.pairs + pair) * x.slot_rows + (dual ? (tile & 1) * kSpTile : duo ? second * x.tokens * p.group : 0);
-  const int last = static_cast<int>(sp_div(base + x.length(dual, key_tiles) - 1, chunk));
+  const int last = static_cast<int>(sp_div(base + x.length(along, key_tiles) - 1, chunk));
   for (int c0 = static_cast<int>(sp_div(base, chunk)); c0 <= last; c0 += 32) {
     const int c = c0 + lane;
     // (a range's end may lie past the axis' end: no tile does)
-    const int t0 = x.tile_at(c * chunk, base, dual, key_tiles);
+    const int t0 = x.tile_at(c * chunk, base, along, key_tiles);
     // (of a pair of heads: a tile of this one)
-    const bool piece = c <= last && x.tile_at((c + 1) * chunk, base, dual, key_tiles) > t0 + (duo ? (t0 ^ second) & 1 : 0);
+    const bool piece = c <= last && x.tile_at((c + 1) * chunk, base, along, key_tiles) > t0 + (duo ? (t0 ^ second) & 1 : 0);
     const unsigned in = __ballot_sync(0xffffffffu, piece);
     if (piece) list[n + __popc(in & ((1u << lane) - 1u))] = slot + 2u * kSpTile * c;
     n += __popc(in);
@@ -1121,9 +1134,9 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
   if (rec.keys > 0) {
     if constexpr (TREE) {
       if (warp < p.row_tiles) {
-        const SpEntity x = sp_entity<true>(p, p.row_tiles == 1, b, 1, rec.keys);
+        const SpEntity x = sp_entity<true>(p, p.paired != 0, b, 1, rec.keys);
         s_pre[warp] = 0;
-        s_all[warp] = sp_list(rec.chunk, p, rec.cost, rec.slot, x, p.row_tiles == 1, h, warp, s_list[warp], 0);
+        s_all[warp] = sp_list<true>(rec.chunk, p, rec.cost, rec.slot, x, p.paired != 0, h, warp, s_list[warp], 0);
         s_rows[warp] = sp_rows(p, x, warp);
       }
       __syncthreads();
@@ -1136,11 +1149,11 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
       if (rec.pre_keys > 0) {
         const SpEntity px = sp_entity<false>(p, false, rec.first, rec.sequences, rec.pre_keys);
         if (tile < px.tiles) {
-          n = sp_list(rec.chunk, p, rec.pre_cost, rec.pre_slot, px, false, h, tile, s_list[warp], 0);
+          n = sp_list<false>(rec.chunk, p, rec.pre_cost, rec.pre_slot, px, false, h, tile, s_list[warp], 0);
           rows = sp_rows(p, px, tile);
         }
       }
-      const int all = sp_list(rec.chunk, p, rec.cost, rec.slot, sp_entity<false>(p, true, b, 1, rec.keys), true, h, 0, s_list[warp], n);
+      const int all = sp_list<false>(rec.chunk, p, rec.cost, rec.slot, sp_entity<false>(p, true, b, 1, rec.keys), true, h, 0, s_list[warp], n);
       s_pre[warp] = n;
       s_all[warp] = all;
       s_rows[warp] = rows;
@@ -1296,7 +1309,7 @@ int sp_launch(const CUtensorMap (&m)[4], const SpParams &p, int B, int most, int
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.G);
+  cfg.gridDim = dim3(TREE ? p.G * p.folds : p.G);
   cfg.blockDim = dim3(kSpThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
