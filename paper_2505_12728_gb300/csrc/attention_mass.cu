@@ -21,7 +21,6 @@
 // chunks, the next chunk's MMAs running while one is summed.
 #include <cmath>
 #include <mutex>
-#include <type_traits>
 
 #include "attn_common.cuh"
 #include "sf_host.h"
@@ -218,19 +217,33 @@ attention_mass_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       }
       __syncwarp();
       float *s_c = s_const + buf * p.cols;
-      for (int r = lane; r < p.cols; r += 32) {
-        float k = INFINITY;
-        if (r < p.R) {
-          const int i = r / p.group, j = r - i * p.group;
+      bool none = false;  // rows that do not count
+      constexpr int kBatch = 8;
+      for (int r0 = lane; r0 < p.cols; r0 += 32 * kBatch) {
+        float lse[kBatch], weight[kBatch];  // all loads in front of their use
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int r = r0 + 32 * u, i = r / p.group, j = r - i * p.group;
+          lse[u] = weight[u] = 0.f;
+          if (r >= p.R) continue;
           const size_t row = static_cast<size_t>(w.b) * p.n_q + i;
-          const float lse = p.lse[row * p.H_q + w.h * p.group + j];
-          const float weight = p.weights ? p.weights[row] : 1.f;
-          if (weight > 0.f && lse != -INFINITY) k = lse * kLog2e - (weight == 1.f ? 0.f : log2f(weight));
+          lse[u] = p.lse[row * p.H_q + w.h * p.group + j];
+          weight[u] = p.weights ? p.weights[row] : 1.f;
         }
-        s_c[r] = -k;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int r = r0 + 32 * u;
+          if (r >= p.cols) continue;
+          float k = INFINITY;
+          if (r < p.R) {
+            if (weight[u] > 0.f && lse[u] != -INFINITY) k = lse[u] * kLog2e - (weight[u] == 1.f ? 0.f : log2f(weight[u]));
+            else none = true;
+          }
+          s_c[r] = -k;
+        }
       }
       if (!(ok = __all_sync(0xffffffffu, mbar_wait_or_abort(bar(QCOPY + buf), round & 1u, s_abort)))) break;
-      for (int r = lane; r < p.R; r += 32) {
+      for (int r = lane; none && r < p.R; r += 32) {
         if (s_c[r] != -INFINITY) continue;
         for (int hf = 0; hf < HALVES; ++hf)
           for (int x = 0; x < 8; ++x)
@@ -358,39 +371,45 @@ attention_mass_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const int key = (w.t + it) * kMassTile + r;
         float total = 0.f;
         if (p.mass && key < w.L) total = p.mass[out0 + key];
-        unsigned long long sum = 0ull;
+        unsigned long long sum0 = 0ull, sum1 = 0ull;
         for (int ch = 0; ch < p.chunks; ++ch, ++job) {
           const uint32_t s = group * 2u + (job & 1u);
           if (!(ok = wait(bar(SFULL + s), (job >> 1) & 1u))) break;
           tc_fence_after_sync();
-          const float2 *c2 = reinterpret_cast<const float2 *>(s_c + ch * p.chunk);
-          auto add = [&](const auto &v, int first, auto count) {
+          const float4 *c4 = reinterpret_cast<const float4 *>(s_c + ch * p.chunk);
+          const uint32_t at = ts + (job & 1u) * kMassChunk;
+          auto add = [&](const uint32_t (&v)[16], int first) {
 #pragma unroll
-            for (int i = 0; i < decltype(count)::value; i += 2) {
-              const float2 k = c2[(first + i) / 2];
-              float x0, x1;
+            for (int i = 0; i < 16; i += 4) {
+              const float4 k = c4[(first + i) / 4];
+              float x0, x1, x2, x3;
               f32x2_split(f32x2_fma(f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), scale2, f32x2(k.x, k.y)), x0, x1);
-              sum = f32x2_add(sum, f32x2(fast_exp2(x0), fast_exp2(x1)));
+              f32x2_split(f32x2_fma(f32x2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), scale2, f32x2(k.z, k.w)), x2, x3);
+              sum0 = f32x2_add(sum0, f32x2(fast_exp2(x0), fast_exp2(x1)));
+              sum1 = f32x2_add(sum1, f32x2(fast_exp2(x2), fast_exp2(x3)));
             }
           };
+          // 16 columns on their way while 16 are summed
+          uint32_t va[16], vb[16];
+          tmem_ld_async_x16(at, va);
+          tmem_ld_wait_x16(va);
           int first = 0;
           for (; first + 32 <= p.chunk; first += 32) {
-            uint32_t v[32];
-            tmem_ld_32x32b_x32(ts + (job & 1u) * kMassChunk + first, v);
-            add(v, first, std::integral_constant<int, 32>());
+            tmem_ld_async_x16(at + first + 16, vb);
+            add(va, first);
+            tmem_ld_wait_x16(vb);
+            if (first + 32 < p.chunk) tmem_ld_async_x16(at + first + 32, va);
+            add(vb, first + 16);
+            if (first + 32 < p.chunk) tmem_ld_wait_x16(va);
           }
-          if (first < p.chunk) {
-            uint32_t v[16];
-            tmem_ld_32x32b_x16(ts + (job & 1u) * kMassChunk + first, v);
-            add(v, first, std::integral_constant<int, 16>());
-          }
+          if (first < p.chunk) add(va, first);
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(SEMPTY + s));
         }
         if (!ok) break;
         float a, b;
-        f32x2_split(sum, a, b);
+        f32x2_split(f32x2_add(sum0, sum1), a, b);
         if (key < w.L) p.out[out0 + key] = total + (a + b);
       }
       if (!ok) break;
@@ -426,10 +445,11 @@ static int mass_setup(int device) {
 
 // Chunks of equal width, the q buffers and the ring that shared memory has room for.
 static int mass_plan(MassParams *p, int D, int *smem) {
-  const int unit = p->R <= 16 ? 16 : 32;
   p->chunks = (p->R + kMassChunk - 1) / kMassChunk;
-  p->chunk = ((p->R + p->chunks - 1) / p->chunks + unit - 1) / unit * unit;
+  p->chunk = ((p->R + p->chunks - 1) / p->chunks + 15) / 16 * 16;
   p->cols = p->chunk * p->chunks;
+  // A second q buffer hides the change of segment, which is worth ring slots: 224 rows, 16
+  // segments of 32768 keys 30.6 us with two buffers and three slots, 33.8 with one and five.
   for (p->q_bufs = 2; p->q_bufs >= 1; --p->q_bufs)
     for (p->stages = kMassMaxStages; p->stages >= (p->q_bufs == 2 ? 3 : 2); --p->stages) {
       *smem = mass_layout(D, p->stages, p->q_bufs, p->cols, p->B).total;
