@@ -203,6 +203,43 @@ __device__ __forceinline__ int sp_rows(const SpParams &p, const SpEntity &x, int
   return (left < p.tokens_per_tile ? left : p.tokens_per_tile) * p.group;
 }
 
+// A tree call of at most 32 sequences, by one warp: lane b has sequence b's keys and what
+// lies in front of its segments.
+constexpr int kSpWarpBatch = 32;
+
+struct SpTreeLane {
+  int keys;
+  uint32_t cost, before, slots, Tot, chunk;
+};
+
+__device__ __forceinline__ SpTreeLane sp_tree_lane(const SpParams &p) {
+  const int lane = threadIdx.x & 31;
+  SpTreeLane t;
+  t.keys = lane < p.B ? p.seq_lens[lane] : 0;
+  const int most = p.max_pages * SF_PAGE_SIZE;
+  if ((t.keys < p.n_q || t.keys > most) && t.keys != 0) {
+    set_status(p.status, SF_DEVICE_BAD_SEQLEN);
+    t.keys = t.keys < p.n_q ? p.n_q : most;
+  }
+  const SpEntity x = sp_entity<true>(p, p.paired != 0, lane, 1, t.keys);
+  t.cost = x.cost;
+  uint32_t ci = x.cost, si = x.cost ? x.slot_rows * x.units : 0u;
+  const uint32_t rows = si;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, ci, o), v = __shfl_up_sync(0xffffffffu, si, o);
+    if (lane >= o) {
+      ci += u;
+      si += v;
+    }
+  }
+  t.before = ci - t.cost;
+  t.slots = si - rows;
+  t.Tot = __shfl_sync(0xffffffffu, ci, 31);
+  t.chunk = sp_chunk(p, t.Tot);
+  return t;
+}
+
 // max of three in one instruction (a NaN is ignored, as by fmaxf)
 __device__ __forceinline__ float sp_max3(float a, float b, float c) {
   float d;
@@ -312,8 +349,14 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
     int *s_len = reinterpret_cast<int *>(smem + L::kPlanOffset), *s_start = s_len + E;
     uint32_t *s_cost = reinterpret_cast<uint32_t *>(s_start + p.num_groups + 1), *s_slot = s_cost + p.num_groups;
     bool bad = false;
+    const bool by_warp = TREE && p.B <= kSpWarpBatch;
+    SpTreeLane tl{};
+    if (by_warp) {
+      tl = sp_tree_lane(p);
+      if (lane < p.B) s_len[lane] = tl.keys;
+    }
 #pragma unroll 1
-    for (int e = lane; e <= E; e += 32) {
+    for (int e = lane; e <= E && !by_warp; e += 32) {
       const bool own = TREE || e >= p.num_groups;
       int n = 0, s = 0;
       if (e < E) n = own ? p.seq_lens[e - p.num_groups] : p.prefix_lens[e];
@@ -352,22 +395,34 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
       }
       return lo;
     };
-    uint32_t sum = 0;
+    uint32_t Tot = tl.Tot, chunk = tl.chunk;
+    if (!by_warp) {
+      uint32_t sum = 0;
 #pragma unroll 1
-    for (int e = lane; e < E; e += 32) sum += entity(e).cost;
-    const uint32_t Tot = __reduce_add_sync(0xffffffffu, sum), chunk = sp_chunk(p, Tot);
+      for (int e = lane; e < E; e += 32) sum += entity(e).cost;
+      Tot = __reduce_add_sync(0xffffffffu, sum);
+      chunk = sp_chunk(p, Tot);
+    }
     // (a tree's: the CTAs of the same keys are neighbours, so that what one reads the others
     // find in L2: 4 sequences of 32768 tokens, 61 nodes, 28 / 4 heads read 536 MB one pair
     // of row tiles behind the other)
     const uint32_t c = TREE ? blockIdx.x / p.folds : blockIdx.x;
     const int fold = TREE ? blockIdx.x - c * p.folds : 0;
-    const bool writes = blockIdx.x == gridDim.x - 1;  // this CTA (with the least to do) leaves the plan for the merge kernel
+    const bool writes = blockIdx.x == gridDim.x - 1 && !by_warp;  // this CTA (with the least to do) leaves the plan for the merge kernel
     const uint32_t at = min(c * chunk, Tot), end = min(at + chunk, Tot);
     // the entity that position `at` lies in, with the costs and partial rows before it
     int e = E;
     uint32_t e_cost = 0, e_slot = 0, cost = 0, slot = 0;
+    if (by_warp) {
+      const unsigned in = __ballot_sync(0xffffffffu, tl.before <= at && at < tl.before + tl.cost);
+      if (in) {
+        e = __ffs(in) - 1;
+        e_cost = __shfl_sync(0xffffffffu, tl.before, e);
+        e_slot = __shfl_sync(0xffffffffu, tl.slots, e);
+      }
+    }
 #pragma unroll 1
-    for (int e0 = 0; e0 < E && (e == E || writes); e0 += 32) {
+    for (int e0 = 0; e0 < E && (e == E || writes) && !by_warp; e0 += 32) {
       const int k = e0 + lane;
       SpEntity x{};
       if (k < E) x = entity(k);
@@ -1003,8 +1058,10 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
           uint32_t a[16], b[16];
-          tmem_ld_32x32b_x16(to + half + ch * 16, a);
-          tmem_ld_32x32b_x16(other + half + ch * 16, b);
+          tmem_ld_async_x16(to + half + ch * 16, a);
+          tmem_ld_async_x16(other + half + ch * 16, b);
+          tmem_ld_wait_x16(a);
+          tmem_ld_wait_x16(b);
           if (valid) {
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
@@ -1127,12 +1184,32 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
   const int tid = threadIdx.x, warp = tid >> 5;
   const int b = blockIdx.x / p.H_kv, h = blockIdx.x - b * p.H_kv;
   const int R = p.n_q * p.group, per = R * C4;
+  // A small tree call's plan comes from the lengths, which the split kernel waited for, so
+  // that it is done when that kernel is (0.8 us behind it otherwise).
+  const bool by_warp = TREE && p.B <= kSpWarpBatch;
+  __shared__ int s_keys;
+  if (by_warp && warp < p.row_tiles) {
+    const SpTreeLane tl = sp_tree_lane(p);
+    const int keys = __shfl_sync(0xffffffffu, tl.keys, b);
+    const uint32_t cost = __shfl_sync(0xffffffffu, tl.before, b), slot = __shfl_sync(0xffffffffu, tl.slots, b);
+    const SpEntity x = sp_entity<true>(p, p.paired != 0, b, 1, keys);
+    s_pre[warp] = 0;
+    s_all[warp] = sp_list<true>(tl.chunk, p, cost, slot, x, p.paired != 0, h, warp, s_list[warp], 0);
+    s_rows[warp] = sp_rows(p, x, warp);
+    s_keys = keys;
+  }
   grid_dependency_wait();
   grid_launch_dependents();
-  const SpRecord rec = p.plan[b];
+  SpRecord rec{};
+  if (by_warp) {
+    __syncthreads();
+    rec.keys = s_keys;
+  } else {
+    rec = p.plan[b];
+  }
   int tok0 = 0, tile0 = 0;  // the sequence's first token within its group's, and that token's row tile
   if (rec.keys > 0) {
-    if constexpr (TREE) {
+    if (TREE && !by_warp) {
       if (warp < p.row_tiles) {
         const SpEntity x = sp_entity<true>(p, p.paired != 0, b, 1, rec.keys);
         s_pre[warp] = 0;
@@ -1143,7 +1220,7 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     }
     tok0 = (b - rec.first) * p.n_q;
     tile0 = sp_tiles(p, tok0);
-    if (!TREE && warp < 2) {
+    if constexpr (!TREE) if (warp < 2) {
       const int tile = tile0 + warp;
       int n = 0, rows = 0;
       if (rec.pre_keys > 0) {
