@@ -101,6 +101,17 @@ def test_idle_slots_and_many_sequences():
     check([(7 * b) % 33 for b in range(1024)], 1, 1, 1, 64, seed=8)
 
 
+def test_more_heads_than_ctas_and_more_sequences_than_lanes():
+    # pairs of heads (an odd number of them too) once every SM has a head; plans of more
+    # than 32 sequences; up to four row tiles a head
+    check([(37 * b) % 150 if b % 11 else None for b in range(60)], 6, 3, 3, 64, seed=70)
+    check([(53 * b) % 300 for b in range(100)], 9, 4, 2, 128, seed=71)
+    check([(29 * b) % 200 for b in range(40)], 20, 14, 2, 128, seed=72)
+    check([(29 * b) % 140 for b in range(33)], 64, 8, 1, 64, seed=73)
+    check([500, 3, 200], 40, 7, 1, 128, seed=74)
+    check([(31 * b) % 90 for b in range(32)], 50, 8, 2, 64, seed=75)
+
+
 def test_long_contexts_in_many_pieces():
     check([5000], 20, 4, 2, 128, seed=9)
     check([3000, 70, 1200], 30, 7, 1, 128, seed=10)
@@ -178,9 +189,9 @@ def test_a_late_key_that_outweighs_all_others():
 
 def test_infinities_and_nan_of_new_rows_reach_only_the_rows_that_see_them():
     require_gpu()
-    for H_q, H_kv, d, n in ((8, 8, 64, 20), (28, 4, 128, 30), (3, 3, 128, 7)):
+    for H_q, H_kv, d, n, spare in ((8, 8, 64, 20, 0), (28, 4, 128, 30, 0), (3, 3, 128, 7, 0), (8, 1, 64, 60, 0), (2, 2, 64, 9, 100)):
         for before in (0, 100, 250):
-            args, masks = make([before, before + 9], n, H_q, H_kv, d, seed=21 + before)
+            args, masks = make([before, before + 9] + [4] * spare, n, H_q, H_kv, d, seed=21 + before)
             words = [[w | 1 << i for i, w in enumerate(row)] for row in masks]
             clean = ref.attention(*args[:5], words)
             bad = (n - 2, n // 2)
