@@ -19,6 +19,16 @@
 // warp 10 brings a segment's rows of q and its constants.  A group has two TMEM
 // buffers of up to 128 columns: with more rows than that a tile's columns come in
 // chunks, the next chunk's MMAs running while one is summed.
+//
+// What bounds it.  Up to some 128 rows K's way from memory (4 sequences of 32768 tokens, 4
+// heads: 24.7 us with 112 rows, 5.6 TB/s; 4 sequences of 3008 tokens, 32 heads, 16 rows:
+// 19.0, 5.4).  Then the tile's chain: 224 rows 31.4 us, 4.4 TB/s (25 without the sums and
+// the MMAs, 28 with the sums alone, 30 with the MMAs alone), 448 rows 70; the tensor pipe is
+// active for 41 % of it, the exponentials take 42 % of their pipe.  5 rows, 3008 tokens, 32
+// heads: 5.8 us in a graph for 25 MB; from memory, called from Python, 7.9.  Not kept: page
+// ids loaded four tiles ahead (no change), one q buffer and five ring slots where two and
+// three fit (33 us), all scores in registers in front of the sums (34.6), 32 columns at a
+// time (33.9), one TMEM buffer of 256 columns a group (31.3, and 75 with 448 rows).
 #include <cmath>
 #include <mutex>
 

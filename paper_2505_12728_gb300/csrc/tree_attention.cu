@@ -12,6 +12,18 @@
 // where the tile begins, gives a bit per key.  Masked rows of K drop out as -infinity
 // before the maximum is taken, infinities and NaN in masked rows of V are taken out of
 // the tile and added to the rows that see them.
+//
+// What bounds it.  Many rows (16 sequences of 8192 to 32768 tokens, 61 nodes, 28 / 4 heads:
+// 242 us, 1.08 PFLOP/s, 1.29 with the rows that fill the four tiles up): the MMAs and the
+// softmax between them, tensor pipe active 67 %; neighbouring CTAs take the two pairs of row
+// tiles of the same keys, so that K and V come from memory once (271 of 536 MB at 4 x 32768
+// tokens).  Few rows and keys: the chain.  Of the 17 us of 26 nodes, 3008 tokens, 32 heads
+// (7.4 for the bytes) 2.1 go by from the lengths to the first copy, 2.4 to the first keys,
+// 7.5 to the last, 1.8 to the last CTA's end, 1.3 to the merge kernel, 2 in it.  Not kept:
+// the merge by whichever CTA ends last (21.9 us; with 224 rows 59 for 23.3: 1.3 MB of partials
+// for one SM), clusters that join in shared memory (18.7, 9.8 for 9.3 with 5 nodes and 640
+// tokens, 29.5 for 23.2 with 224 rows), a CTA for every short segment (7.1 for 8.9 with one key
+// tile, but 11.6 for 10.1 with six), the block table fetched to L2 ahead (no change).
 #include "shared_prefix_kernel.cuh"
 
 namespace sf {
