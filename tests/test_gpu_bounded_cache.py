@@ -311,6 +311,29 @@ def test_evict_with_a_full_stack_keeps_the_pages_mapped():
     assert free[2:17].tolist() == bt[0, 4:19].tolist() and torch.equal(table[1:].cpu(), bt[1:])
 
 
+# more sequences than a CTA has threads, of which some give pages back, some are cut
+# inside their last page, some stay; `room`: of the pages that all of them would give
+@pytest.mark.parametrize("room", [1.0, 0.9, 0.45, 0.0])
+def test_evict_gives_back_the_pages_of_many(room):
+    before = [[None, 20, 33, 70, 0, 36, 150][b % 7] for b in range(600)]
+    case = evict_case(before, 1, 1, 8, seed=6)
+    bt, lens = case[3], case[4]
+    had, need = ([-(-(min(x, cut) if x else 0) // 16) for x in lens] for cut in (1000, 32))
+    free = torch.full((7 + int(room * (sum(had) - sum(need))),), -9, dtype=torch.int32)
+    room = len(free) - 7
+    free, count = free.cuda(), i32([7]).cuda()
+    status, table, _ = check_evict(case, 32, in_place=True, stack=(free, count))
+    freed, want, full = [], bt.clone(), False
+    for b, x in enumerate(lens):
+        full |= x > 32 and len(freed) + had[b] - need[b] > room
+        if x > 32 and not full:
+            freed += bt[b, need[b]:had[b]].tolist()
+            want[b, need[b]:had[b]] = -1
+    assert status == (sfv.SF_DEVICE_OUT_OF_PAGES if full else 0)
+    assert int(count) == 7 + len(freed) and free[7:int(count)].tolist() == freed
+    assert free[:7].tolist() == [-9] * 7 and torch.equal(table.cpu(), want)
+
+
 def test_evict_bad_lengths_and_pages_are_flagged():
     require_gpu()
     mass, kc, vc, bt, lens = evict_case([300, 200, 100], 1, 2, 64, seed=5)
