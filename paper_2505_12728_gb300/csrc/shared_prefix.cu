@@ -125,7 +125,7 @@ int sf_shared_prefix_attention(const void *q, const void *k_cache, const void *v
   if ((st = sp_maps(m, k_cache, v_cache, q, rows, B, n_q, H_q, H_kv, head_dim, p.tokens_per_tile)) != SF_OK) return st;
 
   auto partials = [&](int pages, int segments) { return std::min((pages + kSpTilePages - 1) / kSpTilePages, G / segments + 1); };
-  return sp_launch<false>(m, p, B, std::max(partials(max_prefix_pages, num_groups * H_kv), partials(max_pages_per_seq, B * H_kv)),
+  return sp_launch<false, false>(m, p, B, std::max(partials(max_prefix_pages, num_groups * H_kv), partials(max_pages_per_seq, B * H_kv)),
                           head_dim, stream);
 }
 

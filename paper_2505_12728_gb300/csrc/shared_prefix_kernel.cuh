@@ -89,6 +89,10 @@ constexpr int kSpMergeThreads = 256;
 // the costs 195); with 5 for either kind of segment, 59 sequences of some 560 tokens with a prefix
 // of 8 took 174 us (119 with 10): a few CTAs had all the prefix's segments.
 constexpr uint32_t kSpCostSegOne = 5, kSpCostSegTwo = 10, kSpCostFew = 4, kSpCostOne = 3, kSpCostTwo = 4;
+// Of a tree's segment that one piece has all keys of, the split kernel writes the results
+// themselves: in place of its partial the piece has its first token, and this bit.
+constexpr uint32_t kSpWhole = 1u << 31;
+constexpr float kSpLn2 = 0.6931471805599453f;
 constexpr int kSpFirstPages = 4; // pages of a key tile in the first part of P V (the rest follows while that runs)
 
 // What the merge kernel has to know about a sequence: where its own segments and
@@ -247,7 +251,7 @@ __device__ __forceinline__ float sp_max3(float a, float b, float c) {
   return d;
 }
 
-template <int D, int STAGES, bool TREE>
+template <int D, int STAGES, bool TREE, bool WHOLE>
 __global__ void __maxnreg__(kSpMaxRegs)
 shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                            const __grid_constant__ CUtensorMap tmap_q_tile,
@@ -544,6 +548,7 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
               j.n = turn == s;
             }
             j.two = first_keys && (it.t0 + j.first) >> duo == 0;
+            if (WHOLE && (duo ? j.n : it.n) == x.key_tiles) j.slot = kSpWhole | static_cast<uint32_t>(j.token);
           }
           if (!dual && !duo && it.n == 1) turn ^= 1;
         }
@@ -1000,7 +1005,23 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         ref += __log2f(__fdividef(l_run, rounded));  // (near 1: within 2^-21)
         l_run = rounded;
       }
-      float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0) * D) + r;
+      const bool whole = WHOLE && (slot0 & kSpWhole) != 0u;
+      float4 *dst = reinterpret_cast<float4 *>(p.part_o + static_cast<size_t>(slot0 & ~kSpWhole) * D) + r;
+      // the row's place in the results, and what they are divided by (0: the row sees nothing)
+      size_t row = 0;
+      __nv_bfloat16 *result = nullptr;
+      if (whole) {
+        row = static_cast<size_t>((slot0 & ~kSpWhole) + r / p.group) * p.H_q + info[2] * p.group + r % p.group;
+        result = p.out + row * D;
+      }
+      auto put_whole = [&](const float (&v)[16], float inv, int column) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = inv == 0.f ? 0u : pack_bf16x2(v[2 * i] * inv, v[2 * i + 1] * inv);
+        uint4 *at = reinterpret_cast<uint4 *>(result + column);
+        at[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        at[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      };
       // spread_bad: the infinities and NaN that this row sees among the piece's draft
       // rows of V, added to its results of `columns` columns from `first` on.
       auto is_bad = [&](int stream) {
@@ -1022,10 +1043,24 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
                 p.v_cache[((static_cast<size_t>(page) * p.H_kv + info[2]) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE) * D + col]);
             if (!isfinite(v)) f += v;
           }
-          if (f != 0.f) reinterpret_cast<float *>(dst + static_cast<size_t>(col / 4) * rows)[col % 4] += f;
+          if (f != 0.f && whole) result[col] = __float2bfloat16_rn(__bfloat162float(result[col]) + f);
+          else if (f != 0.f) reinterpret_cast<float *>(dst + static_cast<size_t>(col / 4) * rows)[col % 4] += f;
         }
       };
-      if (!joint) {
+      if (!joint && whole) {
+        const float inv = ref == -INFINITY ? 0.f : 1.f / l_run;
+#pragma unroll 1
+        for (int ch = 0; ch < D / 16; ++ch) {
+          uint32_t ov[16];
+          tmem_ld_32x32b_x16(to + ch * 16, ov);
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(ov[i]);
+          if (valid) put_whole(v, inv, ch * 16);
+        }
+        if (valid && p.lse) p.lse[row] = (ref + log2f(l_run)) * kSpLn2;
+        if (is_bad(s)) spread_bad(0, D);
+      } else if (!joint) {
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
           uint32_t ov[32];
@@ -1054,6 +1089,8 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         const float2 ml = s_ml[(1 - s) * kSpTile + r];
         const float top = fmaxf(ref, ml.x);
         const float w = ref == -INFINITY ? 0.f : fast_exp2(ref - top), wo = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
+        const float both = l_run * w + ml.y * wo;
+        const float inv = !whole || top == -INFINITY ? 0.f : 1.f / both;
         const uint32_t half = s * (D / 2), other = to + 128 - 256 * s;  // (O_0, O_1 are 128 columns apart)
 #pragma unroll 1
         for (int ch = 0; ch < D / 32; ++ch) {
@@ -1063,17 +1100,23 @@ shared_prefix_split_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
           tmem_ld_wait_x16(a);
           tmem_ld_wait_x16(b);
           if (valid) {
+            float v[16];
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-              float v[4];
+            for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(a[i]) * w + __uint_as_float(b[i]) * wo;
+            if (whole) {
+              put_whole(v, inv, half + ch * 16);
+            } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                v[i] = __uint_as_float(a[4 * q4 + i]) * w + __uint_as_float(b[4 * q4 + i]) * wo;
-              dst[static_cast<size_t>(half / 4 + ch * 4 + q4) * rows] = make_float4(v[0], v[1], v[2], v[3]);
+              for (int q4 = 0; q4 < 4; ++q4)
+                dst[static_cast<size_t>(half / 4 + ch * 4 + q4) * rows] =
+                    make_float4(v[4 * q4], v[4 * q4 + 1], v[4 * q4 + 2], v[4 * q4 + 3]);
             }
           }
         }
-        if (valid && s == 0) p.part_ml[slot0 + r] = make_float2(top, l_run * w + ml.y * wo);
+        if (valid && s == 0) {
+          if (!whole) p.part_ml[slot0 + r] = make_float2(top, both);
+          else if (p.lse) p.lse[row] = (top + log2f(both)) * kSpLn2;
+        }
         if (is_bad(0) || is_bad(1)) spread_bad(s * (D / 2), D / 2);
         tc_fence_before_sync();
         __syncwarp();
@@ -1174,9 +1217,8 @@ __device__ __forceinline__ int sp_list(uint32_t chunk, const SpParams &p, uint32
 }
 
 // kWays threads an output quad, every kWays-th batch of its partials each.
-template <int D, int kWays, bool TREE>
+template <int D, int kWays, bool TREE, bool WHOLE>
 __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(const __grid_constant__ SpParams p) {
-  constexpr float kLn2 = 0.6931471805599453f;
   constexpr int C4 = D / 4;
   constexpr int kLists = TREE ? kSpTreeTiles : 2;
   __shared__ uint32_t s_list[kLists][TREE ? kSpMaxSms : kSpListMax];
@@ -1218,6 +1260,7 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
       }
       __syncthreads();
     }
+    if (WHOLE && s_all[0] == 1) return;  // (all its row tiles are cut alike) the results are there
     tok0 = (b - rec.first) * p.n_q;
     tile0 = sp_tiles(p, tok0);
     if constexpr (!TREE) if (warp < 2) {
@@ -1281,7 +1324,7 @@ __global__ void __launch_bounds__(kSpMergeThreads) shared_prefix_merge_kernel(co
     packed.x = pack_bf16x2(jn.acc.x * inv, jn.acc.y * inv);
     packed.y = pack_bf16x2(jn.acc.z * inv, jn.acc.w * inv);
     *reinterpret_cast<uint2 *>(p.out + row * D + 4 * c4) = packed;
-    if (p.lse && c4 == 0) p.lse[row] = rec.keys > 0 ? (jn.M + log2f(jn.L)) * kLn2 : -INFINITY;
+    if (p.lse && c4 == 0) p.lse[row] = rec.keys > 0 ? (jn.M + log2f(jn.L)) * kSpLn2 : -INFINITY;
   }
 }
 
@@ -1320,14 +1363,14 @@ inline int sp_grid(int *G) {
 using SpKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const SpParams);
 
 // The kernel with the deepest ring that leaves room for the plan of B sequences.
-template <bool TREE>
+template <bool TREE, bool WHOLE>
 void sp_select(int D, int B, int num_groups, SpKernel *fn, int *smem) {
   const int stages = sp_stages(D, B, num_groups);
   if (D == 128) {
-    *fn = stages == 5 ? shared_prefix_split_kernel<128, 5, TREE> : shared_prefix_split_kernel<128, 4, TREE>;
+    *fn = stages == 5 ? shared_prefix_split_kernel<128, 5, TREE, WHOLE> : shared_prefix_split_kernel<128, 4, TREE, WHOLE>;
     *smem = stages == 5 ? sp_smem_bytes<128, 5>(B, num_groups) : sp_smem_bytes<128, 4>(B, num_groups);
   } else {
-    *fn = stages == 10 ? shared_prefix_split_kernel<64, 10, TREE> : shared_prefix_split_kernel<64, 8, TREE>;
+    *fn = stages == 10 ? shared_prefix_split_kernel<64, 10, TREE, WHOLE> : shared_prefix_split_kernel<64, 8, TREE, WHOLE>;
     *smem = stages == 10 ? sp_smem_bytes<64, 10>(B, num_groups) : sp_smem_bytes<64, 8>(B, num_groups);
   }
 }
@@ -1339,10 +1382,14 @@ int sp_setup(int device) {
   if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
   std::lock_guard<std::mutex> lock(mu);
   if (done[device]) return SF_OK;
-  for (SpKernel fn : {static_cast<SpKernel>(shared_prefix_split_kernel<128, 5, TREE>),
-                      static_cast<SpKernel>(shared_prefix_split_kernel<128, 4, TREE>),
-                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 10, TREE>),
-                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 8, TREE>)}) {
+  for (SpKernel fn : {static_cast<SpKernel>(shared_prefix_split_kernel<128, 5, TREE, false>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<128, 5, TREE, TREE>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<128, 4, TREE, false>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<128, 4, TREE, TREE>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 10, TREE, false>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 10, TREE, TREE>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 8, TREE, false>),
+                      static_cast<SpKernel>(shared_prefix_split_kernel<64, 8, TREE, TREE>)}) {
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kSpSmemMax);
     if (e != cudaSuccess) return fail(SF_ERR_CUDA, "cudaFuncSetAttribute (shared prefix): %s", cudaGetErrorString(e));
   }
@@ -1377,11 +1424,11 @@ inline int sp_maps(CUtensorMap (&m)[4], const void *k, const void *v, const void
 }
 
 // The two kernels of one call.  `most` bounds a row's partials.
-template <bool TREE>
+template <bool TREE, bool WHOLE>
 int sp_launch(const CUtensorMap (&m)[4], const SpParams &p, int B, int most, int head_dim, cudaStream_t stream) {
   SpKernel fn;
   int smem;
-  sp_select<TREE>(head_dim, B, p.num_groups, &fn, &smem);
+  sp_select<TREE, WHOLE>(head_dim, B, p.num_groups, &fn, &smem);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1410,10 +1457,10 @@ int sp_launch(const CUtensorMap (&m)[4], const SpParams &p, int B, int most, int
   cfg.gridDim = dim3(static_cast<unsigned>(B * p.H_kv), static_cast<unsigned>(parts));
   cfg.blockDim = dim3(kSpMergeThreads);
   cfg.dynamicSmemBytes = 0;
-  e = head_dim == 128 ? (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 4, TREE>, p)
-                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 1, TREE>, p))
-                      : (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 4, TREE>, p)
-                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 1, TREE>, p));
+  e = head_dim == 128 ? (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 4, TREE, WHOLE>, p)
+                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<128, 1, TREE, WHOLE>, p))
+                      : (wide ? cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 4, TREE, WHOLE>, p)
+                              : cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64, 1, TREE, WHOLE>, p));
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "shared-prefix merge launch: %s", cudaGetErrorString(e));
   return SF_OK;
 }

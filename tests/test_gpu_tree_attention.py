@@ -216,6 +216,41 @@ def test_infinities_and_nan_of_new_rows_reach_only_the_rows_that_see_them():
                         close(out[b:b + 1, i:i + 1], lse[b:b + 1, i:i + 1], part)
 
 
+# more segments than CTAs: most lie in one piece; pairs of heads (the last alone), one row
+# tile, two, three and four
+@pytest.mark.parametrize("H_q, H_kv, d, n, B", [(3, 3, 64, 9, 90), (4, 2, 64, 5, 100), (2, 1, 128, 12, 170), (8, 1, 128, 20, 90),
+                                                (8, 1, 64, 40, 90), (8, 1, 64, 60, 90)])
+def test_segments_of_one_piece(H_q, H_kv, d, n, B):
+    require_gpu()
+    before = [None if b % 13 == 5 else 0 if b % 5 == 1 else (37 * b) % 170 for b in range(B)]
+    g = torch.Generator().manual_seed(76)
+    masks = [ref.masks(random_tree(n, g)) for _ in before]
+    for b in range(0, B, 4):
+        masks[b][n // 3] = 0
+    args, _ = make(before, n, H_q, H_kv, d, seed=77, masks=masks)
+    clean = ref.attention(*args[:5], masks)
+    out, lse, status = run(args)
+    assert status == 0
+    close(out, lse, clean)
+    for c, row in ((1, n - 2), (2, n // 2)):
+        for b in range(0, B, 3):
+            if before[b] is not None:
+                page, slot = ref.place(args[3][b], before[b] + row)
+                args[c][page, :, slot, 5] = math.nan if c == 1 else -math.inf
+    out, lse, status = run(args)
+    assert status == 0
+    out, lse = out.cpu(), lse.cpu()
+    for b in range(0, B, 3):
+        for i in range(n) if before[b] is not None else ():
+            if masks[b][i] >> n - 2 & 1:
+                assert out[b, i].isnan().all() and lse[b, i].isnan().all()
+                out[b, i], lse[b, i] = clean[0][b, i].to(out.dtype), clean[1][b, i].to(lse.dtype)
+            elif masks[b][i] >> n // 2 & 1:
+                assert not out[b, i, :, 5].isfinite().any()
+                out[b, i, :, 5] = clean[0][b, i, :, 5].to(out.dtype)
+    close(out, lse, clean)
+
+
 def test_infinities_and_nan_of_the_context_reach_all_rows():
     require_gpu()
     args, masks = make([300], 10, 6, 2, 64, seed=22)
