@@ -47,6 +47,7 @@ constexpr int kEvictBins = 2048;
 constexpr int kEvictSlot = 4096;       // bytes of a warp's rows of a round
 constexpr int kEvictKeys = 8;          // keys of a thread in flight
 constexpr int kEvictMaxCluster = 8;
+constexpr int kShortBatch = 4;         // 16-byte loads of a thread in flight
 constexpr int kEvictSmem = 2 * kEvictWarps * kEvictSlot > 5 * kEvictBins * 4 ? 2 * kEvictWarps * kEvictSlot : 5 * kEvictBins * 4;
 
 struct EvictLayer {
@@ -100,7 +101,7 @@ __device__ __forceinline__ uint32_t ld_dsmem_u32(uint32_t local, uint32_t rank) 
 }
 
 // Exclusive sum over the block's threads; *total is all of them.
-template <typename T>
+template <int WARPS, typename T>
 __device__ __forceinline__ T evict_scan(T v, T *s_warp, T *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   T incl = v;
@@ -113,7 +114,7 @@ __device__ __forceinline__ T evict_scan(T v, T *s_warp, T *total) {
   __syncthreads();
   T off = 0, sum = 0;
 #pragma unroll
-  for (int w = 0; w < kEvictWarps; ++w) {
+  for (int w = 0; w < WARPS; ++w) {
     const T x = s_warp[w];
     if (w < warp) off += x;
     sum += x;
@@ -121,6 +122,76 @@ __device__ __forceinline__ T evict_scan(T v, T *s_warp, T *total) {
   __syncthreads();
   *total = sum;
   return off + incl - v;
+}
+
+// The last CTA to come here writes the lengths and gives the pages back.
+template <int THREADS>
+__device__ __forceinline__ void evict_finish(const EvictParams &p, uint32_t *s_plan /* [2][THREADS] */) {
+  __shared__ uint32_t s_last;
+  __shared__ long long s_wide[THREADS / 32];
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid == 0) s_last = atom_add_acq_rel_gpu(p.ticket, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (s_last) {
+    if (tid == 0) *p.ticket = 0u;
+    // A thread a sequence; then the pages of all of them, found by their places on the stack.
+    const int fc0 = p.free_count ? *p.free_count : 0;
+    long long freed = fc0;
+    bool full = fc0 < 0;
+    uint32_t *s_off = s_plan, *s_need = s_plan + THREADS;
+    for (int b0 = 0; b0 < p.B; b0 += THREADS) {
+      const int b1 = b0 + tid;
+      bool c1 = false;
+      int need = 0;
+      long long gone = 0, total;
+      if (b1 < p.B) {
+        const int T = p.seq_lens[b1];
+        (void)evict_length(p, b1, c1, false);
+        const int now = c1 ? p.budget + p.n_q : T;
+        p.seq_lens_out[b1] = now;  // (may be seq_lens)
+        need = (now + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE;
+        if (c1) gone = (T + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE - need;
+      }
+      if (!p.free_count) continue;
+      const long long off = evict_scan<THREADS / 32>(gone, s_wide, &total);
+      // sequences that the stack has no room for: their pages stay mapped
+      const bool stays = c1 && (full || freed + off + gone > p.capacity);
+      s_off[tid] = static_cast<uint32_t>(off > p.capacity ? p.capacity : off);
+      s_need[tid] = need;
+      if (__syncthreads_or(stays)) {
+        full = true;
+        (void)evict_scan<THREADS / 32>(stays ? 0ll : gone, s_wide, &total);
+      }
+      for (long long f0 = 0; f0 < total; f0 += kEvictKeys * THREADS) {
+        int32_t *from[kEvictKeys], page[kEvictKeys];
+#pragma unroll
+        for (int u = 0; u < kEvictKeys; ++u) {
+          const long long f = f0 + u * THREADS + tid;
+          if (f >= total) continue;
+          int at = 0;  // the last sequence whose pages start at or before f
+#pragma unroll
+          for (int step = THREADS / 2; step > 0; step >>= 1)
+            if (s_off[at + step] <= f) at += step;
+          from[u] = p.block_table + static_cast<size_t>(b0 + at) * p.max_pages + s_need[at] + (f - s_off[at]);
+          page[u] = *from[u];
+        }
+#pragma unroll
+        for (int u = 0; u < kEvictKeys; ++u) {
+          const long long f = f0 + u * THREADS + tid;
+          if (f >= total) continue;
+          p.free_pages[freed + f] = page[u];
+          *from[u] = -1;
+        }
+      }
+      freed += total;
+      __syncthreads();
+    }
+    if (tid == 0 && p.free_count) {
+      if (!(fc0 < 0)) *p.free_count = static_cast<int32_t>(freed);
+      if (full) set_status(p.status, SF_DEVICE_OUT_OF_PAGES);
+    }
+  }
 }
 
 template <int C>
@@ -132,8 +203,6 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
   uint32_t *s_few = s_hist[4];    // keys in the first digit's bin
   __shared__ __align__(8) uint64_t s_bar[kEvictWarps][2];
   __shared__ uint32_t s_found, s_warp[kEvictWarps], s_pick[2], s_count[2];
-  __shared__ uint32_t s_last;
-  __shared__ long long s_wide[kEvictWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
   const int rank = C > 1 ? static_cast<int>(blockIdx.x % C) : 0, task = blockIdx.x / C;
   const int h = task % p.H_kv, lb = task / p.H_kv, b = lb % p.B;
@@ -233,7 +302,7 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
         n[i + 3] = x.w;
         sum += x.x + x.y + x.z + x.w;
       }
-      uint32_t total, above = evict_scan(sum, s_warp, &total);
+      uint32_t total, above = evict_scan<kEvictWarps>(sum, s_warp, &total);
 #pragma unroll
       for (int i = kPer - 1; i >= 0; --i) {
         if (above < left && left <= above + n[i]) {
@@ -283,7 +352,7 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
     uint32_t larger = 0, equal = 0;
     if constexpr (C > 1) {
       uint32_t sum;
-      (void)evict_scan(mine, s_warp, &sum);
+      (void)evict_scan<kEvictWarps>(mine, s_warp, &sum);
       if (tid == 0) {
         s_count[0] = sum;
         s_count[1] = s_hist[2][found & 1023u];
@@ -417,69 +486,127 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
     for (int t = p.budget + rank * kEvictThreads + tid; t < p.width; t += C * kEvictThreads) mass_out[t] = 0.f;
   }
 
-  // the last CTA: lengths and pages
-  __syncthreads();
-  if (tid == 0) s_last = atom_add_acq_rel_gpu(p.ticket, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (s_last) {
-    if (tid == 0) *p.ticket = 0u;
-    // A thread a sequence; then the pages of all of them, found by their places on the stack.
-    const int fc0 = p.free_count ? *p.free_count : 0;
-    long long freed = fc0;
-    bool full = fc0 < 0;
-    uint32_t *s_off = reinterpret_cast<uint32_t *>(smem), *s_need = s_off + kEvictThreads;
-    for (int b0 = 0; b0 < p.B; b0 += kEvictThreads) {
-      const int b1 = b0 + tid;
-      bool c1 = false;
-      int need = 0;
-      long long gone = 0, total;
-      if (b1 < p.B) {
-        const int T = p.seq_lens[b1];
-        (void)evict_length(p, b1, c1, false);
-        const int now = c1 ? p.budget + p.n_q : T;
-        p.seq_lens_out[b1] = now;  // (may be seq_lens)
-        need = (now + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE;
-        if (c1) gone = (T + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE - need;
-      }
-      if (!p.free_count) continue;
-      const long long off = evict_scan(gone, s_wide, &total);
-      // sequences that the stack has no room for: their pages stay mapped
-      const bool stays = c1 && (full || freed + off + gone > p.capacity);
-      s_off[tid] = static_cast<uint32_t>(off > p.capacity ? p.capacity : off);
-      s_need[tid] = need;
-      if (__syncthreads_or(stays)) {
-        full = true;
-        (void)evict_scan(stays ? 0ll : gone, s_wide, &total);
-      }
-      for (long long f0 = 0; f0 < total; f0 += kEvictKeys * kEvictThreads) {
-        int32_t *from[kEvictKeys], page[kEvictKeys];
+  evict_finish<kEvictThreads>(p, reinterpret_cast<uint32_t *>(smem));
+  launch_dependents_after_stores();
+}
+
+// Contexts of at most 32 * KEYS keys: one CTA a (layer, sequence, KV head).  Its first
+// warp has all weights in registers and finds the value of the last kept key bit by bit,
+// by counting.  Then each warp moves some columns of K or of V, in the order of the rows, a
+// batch's loads in front of its stores, as tree_commit does: it needs no barrier.
+template <int KEYS, int WARPS, int BLOCKS>
+__global__ void __launch_bounds__(32 * WARPS, BLOCKS) kv_evict_short_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int THREADS = 32 * WARPS, PARTS = WARPS / 2, MOST = 32 * KEYS;
+  __shared__ uint32_t s_plan[2 * THREADS];
+  __shared__ int32_t s_page[MOST / SF_PAGE_SIZE];
+  __shared__ uint16_t s_pos[MOST];
+  __shared__ int s_first;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
+  const int task = blockIdx.x, h = task % p.H_kv, lb = task / p.H_kv, b = lb % p.B;
+  const EvictLayer &layer = p.layers[lb / p.B];
+  const size_t bh = static_cast<size_t>(b) * p.H_kv + h;
+  grid_dependency_wait();
+  bool cut;
+  const int L = evict_length(p, b, cut, lb < p.B && h == 0 && tid == 0);
+  const float *mass = layer.mass + bh * p.width;
+  float *mass_out = layer.mass_out + bh * p.width;
+  int32_t *kept = layer.kept + bh * p.budget;
+  if (!cut) {
+    for (int t = tid; t < p.width; t += THREADS)
+      if (t >= L) mass_out[t] = 0.f;
+      else if (mass != mass_out) mass_out[t] = mass[t];
+    for (int j = tid; j < p.budget; j += THREADS) kept[j] = j < L ? j : -1;
+  } else {
+    if (warp == 1 && lane < MOST / SF_PAGE_SIZE)
+      s_page[lane] = lane * SF_PAGE_SIZE < L ? p.block_table[static_cast<size_t>(b) * p.max_pages + lane] : -1;
+    if (warp == 0) {
+      float w[KEYS];
+      uint32_t key[KEYS];
 #pragma unroll
-        for (int u = 0; u < kEvictKeys; ++u) {
-          const long long f = f0 + u * kEvictThreads + tid;
-          if (f >= total) continue;
-          int at = 0;  // the last sequence whose pages start at or before f
+      for (int u = 0; u < KEYS; ++u) w[u] = 32 * u + lane < L ? mass[32 * u + lane] : 0.f;
 #pragma unroll
-          for (int step = kEvictThreads / 2; step > 0; step >>= 1)
-            if (s_off[at + step] <= f) at += step;
-          from[u] = p.block_table + static_cast<size_t>(b0 + at) * p.max_pages + s_need[at] + (f - s_off[at]);
-          page[u] = *from[u];
+      for (int u = 0; u < KEYS; ++u) {
+        const int t = 32 * u + lane;
+        key[u] = t >= L ? 0u : t < p.first || t >= L - p.recent ? 0xffffffffu : evict_key(w[u]);  // (no weight's is 0)
+      }
+      // the largest value that `budget` keys reach; once as many do, it need not be exact
+      const int budget = p.budget;
+      uint32_t found = 0u;
+      int reach = L;
+      for (uint32_t bit = 1u << 31; bit && reach != budget; bit >>= 1) {
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < KEYS; ++u) n += key[u] >= (found | bit);
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (n >= budget) {
+          found |= bit;
+          reach = n;
         }
-#pragma unroll
-        for (int u = 0; u < kEvictKeys; ++u) {
-          const long long f = f0 + u * kEvictThreads + tid;
-          if (f >= total) continue;
-          p.free_pages[freed + f] = page[u];
-          *from[u] = -1;
-        }
       }
-      freed += total;
-      __syncthreads();
+      // all above, and the first of those equal to it
+      int above = 0;
+#pragma unroll
+      for (int u = 0; u < KEYS; ++u) above += key[u] > found;
+      int left = reach == budget ? MOST : budget - __reduce_add_sync(0xffffffffu, above);
+      int at = 0, in_place = MOST;
+#pragma unroll
+      for (int u = 0; u < KEYS; ++u) {
+        const unsigned lower = (1u << lane) - 1u;
+        const bool eq = key[u] == found && 32 * u + lane < L;
+        const unsigned equal = __ballot_sync(0xffffffffu, eq);
+        const bool stays = key[u] > found || (eq && __popc(equal & lower) < left);
+        left -= __popc(equal);
+        const unsigned who = __ballot_sync(0xffffffffu, stays);
+        if (in_place == MOST && ~who) in_place = 32 * u + __ffs(~who) - 1;
+        if (stays) {
+          const int j = at + __popc(who & lower);
+          kept[j] = 32 * u + lane;
+          s_pos[j] = static_cast<uint16_t>(32 * u + lane);
+          mass_out[j] = w[u];
+        }
+        at += __popc(who);
+      }
+      for (int t = budget + lane; t < p.width; t += 32) mass_out[t] = 0.f;
+      if (lane == 0) s_first = in_place;
     }
-    if (tid == 0 && p.free_count) {
-      if (!(fc0 < 0)) *p.free_count = static_cast<int32_t>(freed);
-      if (full) set_status(p.status, SF_DEVICE_OUT_OF_PAGES);
+    __syncthreads();
+    uint4 *cache = warp & 1 ? layer.v : layer.k;
+    const int wide = p.D / 8, from = (warp >> 1) * wide / PARTS, columns = ((warp >> 1) + 1) * wide / PARTS - from;
+    const int first = s_first, total = (p.budget - first) * columns;
+    auto place = [&](int pos) -> long long {  // in 16-byte pieces; -1: a page outside the pool
+      const int page = s_page[pos / SF_PAGE_SIZE];
+      if (page < 0 || page >= p.num_pages) {
+        set_status(p.status, SF_DEVICE_BAD_PAGE);
+        return -1;
+      }
+      return ((static_cast<long long>(page) * p.H_kv + h) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE) * wide + from;
+    };
+    for (int base = 0; base < total; base += 32 * kShortBatch) {
+      uint4 v[kShortBatch];
+      long long to[kShortBatch];
+#pragma unroll
+      for (int u = 0; u < kShortBatch; ++u) {
+        const int x = base + 32 * u + lane;
+        to[u] = -1;
+        if (x < total) {
+          const int r = x / columns, piece = x - r * columns;
+          const long long source = place(s_pos[first + r]);
+          to[u] = place(first + r);
+          if (source < 0) to[u] = -1;
+          if (to[u] >= 0) {
+            to[u] += piece;
+            v[u] = cache[source + piece];
+          }
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < kShortBatch; ++u)
+        if (to[u] >= 0) cache[to[u]] = v[u];
+      __syncwarp();
     }
   }
+  evict_finish<THREADS>(p, s_plan);
   launch_dependents_after_stores();
 }
 
@@ -519,6 +646,27 @@ static int evict_cluster(int tasks, int sms) {
   int C = 1;
   while (C < kEvictMaxCluster && 2LL * tasks * C <= sms) C *= 2;
   return C;
+}
+
+struct EvictLaunch {
+  void (*kernel)(const EvictParams);
+  int cluster, threads, smem;
+};
+
+// Weights of at most 256 tokens a head: 16 warps where no SM has more than two heads (8
+// heads of 250 tokens to 200: 11.9 us, by a cluster of kv_evict_kernel 18; 128 heads 12.7, 13.1),
+// else four, which leave room for eight heads an SM (2400 heads of 85 tokens to 12: 13.5 us, with
+// 16 warps 43, with kv_evict_kernel, three heads an SM and a chain of barriers, 56; of 250 to
+// 200: 90, 131, 120).  Of at most 512, many heads: 2400 of 500 tokens to 64 47 us, with
+// kv_evict_kernel 75, to 400 173 and 193 (but 128 heads to 400 21, 17.5).
+static EvictLaunch evict_launch(int tasks, int width, int sms) {
+  const bool many = tasks > 2 * sms;
+  if (width <= 256)
+    return many ? EvictLaunch{kv_evict_short_kernel<8, 4, 8>, 1, 128, 0} : EvictLaunch{kv_evict_short_kernel<8, 16, 2>, 1, 512, 0};
+  if (width <= 512 && many) return {kv_evict_short_kernel<16, 4, 8>, 1, 128, 0};
+  const int C = evict_cluster(tasks, sms);
+  return {C == 1 ? kv_evict_kernel<1> : C == 2 ? kv_evict_kernel<2> : C == 4 ? kv_evict_kernel<4> : kv_evict_kernel<8>, C,
+          kEvictThreads, kEvictSmem};
 }
 
 }  // namespace sf
@@ -599,7 +747,9 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
   p.recent = recent;
   p.n_q = n_q;
   p.capacity = capacity;
-  const int tasks = num_layers * B * H_kv, C = evict_cluster(tasks, dev.sm_count);
+  const int tasks = num_layers * B * H_kv;
+  const EvictLaunch launch = evict_launch(tasks, mass_width, dev.sm_count);
+  const int C = launch.cluster;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -608,14 +758,13 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tasks * C));
-  cfg.blockDim = dim3(kEvictThreads);
-  cfg.dynamicSmemBytes = kEvictSmem;
+  cfg.blockDim = dim3(launch.threads);
+  cfg.dynamicSmemBytes = launch.smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = C > 1 ? 2 : 1;
   if ((st = evict_setup(dev.ordinal)) != SF_OK) return st;
-  auto kernel = C == 1 ? kv_evict_kernel<1> : C == 2 ? kv_evict_kernel<2> : C == 4 ? kv_evict_kernel<4> : kv_evict_kernel<8>;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, launch.kernel, p);
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "eviction launch: %s", cudaGetErrorString(e));
   return SF_OK;
 }

@@ -262,6 +262,19 @@ def test_evict_lengths_around_a_round(L):
         assert check_evict(evict_case([L], 1, 2, 128, seed=L), budget, 1, 5, in_place=True)[0] == 0
 
 
+# both sides of the widths up to which one warp has all weights, few heads and many
+@pytest.mark.parametrize("width, layers", [(256, 2), (256, 12), (257, 2), (257, 12), (512, 2), (512, 12), (513, 12)])
+@pytest.mark.parametrize("budget, first, recent, d, ties", [(1, 0, 1, 128, False), (31, 3, 8, 64, True), (32, 0, 0, 8, False),
+                                                            (100, 40, 60, 24, False), (129, 1, 2, 256, True), (255, 0, 9, 128, True)])
+def test_evict_short_contexts(width, layers, budget, first, recent, d, ties):
+    long = min(width, 512)
+    before = [256, 255, None, 1, 0, 31, 33, 128, 130, 200, 101, long, long - 1, long - 130]
+    for in_place in (False, True):
+        case = evict_case(before, layers, 3, d, seed=budget + d, n=0 if in_place else 4, ties=ties, width=width)
+        case[0][0, 0, 0, 5:9], case[0][1, 1, 2, 200:] = math.nan, -math.inf
+        assert check_evict(case, budget, first, recent, n=0 if in_place else 4, in_place=in_place)[0] == 0
+
+
 def test_evict_ties_zeros_infinities_and_nan():
     case = evict_case([900, 333], 2, 2, 64, seed=1, ties=True)
     case[0][0, 0, 0] = 0
