@@ -33,6 +33,7 @@
 // longer needed back to the free-page stack: a thread a sequence, then a thread a page (one
 // sequence after the other took 37.6 us for 256 sequences of which none is cut, 10.2 so;
 // 256 sequences of 4 pages back 123 -> 38).
+#include <algorithm>
 #include <mutex>
 
 #include "sf_device.cuh"
@@ -638,14 +639,22 @@ static int evict_setup(int device) {
   return SF_OK;
 }
 
-// CTAs per (layer, sequence, KV head): as many as still have an SM each.  A cluster's
-// barriers in every round cost more than they bring once a CTA shares its SM (128 heads
-// of 3008 keys to 1024: 43 us with one CTA a head, 53 with two; 32 heads: 41 with one, 31
-// with four; 4 heads of 32768 keys to 4096: 172 with one, 47 with eight).
-static int evict_cluster(int tasks, int sms) {
-  int C = 1;
-  while (C < kEvictMaxCluster && 2LL * tasks * C <= sms) C *= 2;
-  return C;
+// CTAs per (layer, sequence, KV head).  One CTA takes 9 us, 22 ns a row and 3.3 a key, so
+// `rows` says how long; a cluster's chain of barriers takes 6 us more with two or four CTAs
+// and 9 with eight, more yet where CTAs share an SM, and its rows 19, 10 and 5 ns.  In us,
+// one / two / four / eight CTAs (152 SMs):
+//     heads    500 to 400      1000 to 900     3000 to 1024    10000 to 6000
+//         8  17 / 21 / 19 / 19  28 / 30 / 23 / 21  35 / 33 / 24 / 22  163 / 125 / 72 / 45
+//        18  17 / 21 / 18 / 25  28 / 30 / 23 / 28  36 / 33 / 24 / 28  165 / 126 / 73 / 58
+//        40  17 / 21 / 22 / 31  28 / 30 / 27 / 34  36 / 33 / 29 / 35  193 / 143 / 108 / 86
+//       100  18 / 25 / 27 / 65  28 / 36 / 34 / 71  37 / 41 / 37 / 75  212 / 205 / 150 / 183
+//       200  22 / 29 / 51 / 126  41 / 48 / 71 / 147  54 / 59 / 81 / 154  286 / 268 / 291 / 354
+static int evict_cluster(int tasks, int budget, int width, int sms) {
+  const long long rows = budget + 3LL * width / 20, slots = static_cast<long long>(kEvictBlocks) * sms;
+  if (rows < 640) return 1;
+  if (8LL * tasks <= slots && (9LL * tasks <= sms || rows >= 3400)) return 8;
+  if (4LL * tasks <= slots && (2LL * tasks <= sms || rows >= 1800)) return 4;
+  return 2LL * tasks <= slots && rows >= 4500 ? 2 : 1;
 }
 
 struct EvictLaunch {
@@ -654,17 +663,17 @@ struct EvictLaunch {
 };
 
 // Weights of at most 256 tokens a head: 16 warps where no SM has more than two heads (8
-// heads of 250 tokens to 200: 11.9 us, by a cluster of kv_evict_kernel 18; 128 heads 12.7, 13.1),
+// heads of 250 tokens to 200: 11.9 us, with kv_evict_kernel 13.1),
 // else four, which leave room for eight heads an SM (2400 heads of 85 tokens to 12: 13.5 us, with
 // 16 warps 43, with kv_evict_kernel, three heads an SM and a chain of barriers, 56; of 250 to
 // 200: 90, 131, 120).  Of at most 512, many heads: 2400 of 500 tokens to 64 47 us, with
 // kv_evict_kernel 75, to 400 173 and 193 (but 128 heads to 400 21, 17.5).
-static EvictLaunch evict_launch(int tasks, int width, int sms) {
+static EvictLaunch evict_launch(int tasks, int budget, int width, int sms) {
   const bool many = tasks > 2 * sms;
   if (width <= 256)
     return many ? EvictLaunch{kv_evict_short_kernel<8, 4, 8>, 1, 128, 0} : EvictLaunch{kv_evict_short_kernel<8, 16, 2>, 1, 512, 0};
   if (width <= 512 && many) return {kv_evict_short_kernel<16, 4, 8>, 1, 128, 0};
-  const int C = evict_cluster(tasks, sms);
+  const int C = evict_cluster(tasks, budget, width, sms);
   return {C == 1 ? kv_evict_kernel<1> : C == 2 ? kv_evict_kernel<2> : C == 4 ? kv_evict_kernel<4> : kv_evict_kernel<8>, C,
           kEvictThreads, kEvictSmem};
 }
@@ -748,7 +757,7 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
   p.n_q = n_q;
   p.capacity = capacity;
   const int tasks = num_layers * B * H_kv;
-  const EvictLaunch launch = evict_launch(tasks, mass_width, dev.sm_count);
+  const EvictLaunch launch = evict_launch(tasks, budget, std::min(mass_width, max_pages_per_seq * SF_PAGE_SIZE), dev.sm_count);
   const int C = launch.cluster;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
