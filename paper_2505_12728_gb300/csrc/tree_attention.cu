@@ -142,11 +142,13 @@ int sf_tree_attention(const void *q, const void *k_cache, const void *v_cache, c
   if ((st = sp_maps(m, k_cache, v_cache, q, rows, B, n_q, H_q, H_kv, head_dim, p.tokens_per_tile)) != SF_OK) return st;
   const int most = std::min((max_pages_per_seq + kSpTilePages - 1) / kSpTilePages, G / (B * H_kv) + 1);
   // With a segment and more for each CTA most segments are one piece (256 sequences of 508
-  // tokens, 4 heads, 56 rows: 91.5 -> 80.2 us; of 216 tokens, 32 heads, 16 rows 367 -> 317).
-  // With fewer hardly any are, and the code for them costs (2 sequences of 645 tokens, 8
-  // heads, 5 rows: 8.8 us, with it 9.1; 16 of 8 to 32 K tokens, 4 heads, 427 rows: 233, 237).
-  return B * H_kv >= p.G ? sp_launch<true, true>(m, p, B, most, head_dim, stream)
-                         : sp_launch<true, false>(m, p, B, most, head_dim, stream);
+  // tokens, 4 heads, 56 rows: 91.5 -> 80.2 us; of 216 tokens, 32 heads, 16 rows 367 -> 317), and
+  // all are where a table has one key tile (6 sequences of 5 to 67 tokens, 3 heads, 4 to 252
+  // rows: 9.1 -> 8.6 to 15.6 -> 13.2).  Otherwise hardly any are, and the code for them costs
+  // (2 sequences of 645 tokens, 8 heads, 5 rows: 8.8 us, with it 9.1; 16 of 8 to 32 K tokens,
+  // 4 heads, 427 rows: 233, 237).
+  return B * H_kv >= p.G || max_pages_per_seq <= kSpTilePages ? sp_launch<true, true>(m, p, B, most, head_dim, stream)
+                                                              : sp_launch<true, false>(m, p, B, most, head_dim, stream);
 }
 
 }  // extern "C"
