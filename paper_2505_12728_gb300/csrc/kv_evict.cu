@@ -3,8 +3,10 @@
 // weight (the first and the last ones in any case), in their order, and its rows of
 // K, V and weights are compacted in place.
 //
-// One cluster of CTAs per (layer, sequence, KV head); nothing is shared between
-// them but the pages, of which each has rows of its own.
+// One CTA, or a cluster, per (layer, sequence, KV head); nothing is shared between
+// them but the pages, of which each has rows of its own.  Contexts of up to 256 or 512
+// tokens have a kernel of their own, kv_evict_short_kernel; the rest of this is about
+// kv_evict_kernel.
 //
 // Which keys.  The weights' bits, ordered as unsigned integers (positive values above
 // negative ones, NaN as -infinity, the keys that stay in any case above all), in
@@ -16,9 +18,9 @@
 // that a kept key moves to.
 //
 // In place.  Row j of the result comes from position kept[j] >= j, and the positions
-// ascend.  So rows are moved in rounds of ascending j, each round's loads (into
-// registers) in front of a barrier and its stores behind it: a store overwrites rows
-// at or below its own j only, which later rounds do not read.
+// ascend.  So rows are moved in rounds of ascending j, each round's copies into shared
+// memory in front of a barrier and those out of it behind it: they overwrite rows at
+// or below their own j only, which later rounds do not read.
 //
 // What bounds it: the rows' way out and in, 256 bytes at a time from all over the cache.  32
 // layers of 32 heads, 3008 -> 1024 keys: 202 us, 5.4 TB/s, 79 % of the copy rate (with 16-byte
