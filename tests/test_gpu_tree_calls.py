@@ -50,8 +50,8 @@ def mass_args():
         workspace=sfv.new_workspace(256))
 
 
-def evict_args():
-    mass, kc, vc, bt, lens = evict_case([300, 40, None], 2, 2, 64, seed=4)
+def evict_args(longest=300):
+    mass, kc, vc, bt, lens = evict_case([longest, 40, None], 2, 2, 64, seed=4)
     return dict(mass=mass.cuda(), k_caches=kc.cuda(), v_caches=vc.cuda(), block_table=bt.cuda(), seq_lens=cuda(lens),
                 budget=64, first=1, recent=8, n_q=0, mass_out=torch.empty_like(mass, device="cuda"),
                 seq_lens_out=torch.empty(3, dtype=I32, device="cuda"),
@@ -262,3 +262,31 @@ def test_attention_over_what_eviction_left(calls):
                     tol = (w @ values[at].abs()) * (2.0 ** -8 + 2.0 ** -11) + (w @ values[at]).abs() * 2.0 ** -8 * (1 + 2.0 ** -6)
                     assert ((out[b, i, 2 * h + j].cpu().double() - w @ values[at]).abs() <= tol).all()
                     assert abs(float(lse[b, i, 2 * h + j]) - float(torch.logsumexp(s, 0))) <= 2.0 ** -11
+
+
+@pytest.mark.parametrize("name, args", OPS[1:] + [("kv_evict", lambda: evict_args(200))])
+def test_pages_more_than_32_bits_away(name, args):
+    # the same pages at the end of a pool of 2^31 elements and more
+    require_gpu()
+    one, two = args(), args()
+    pools = [k for k in two if k.endswith(("k_cache", "v_cache", "k_caches", "v_caches"))]
+    small = one[pools[0]].shape[-4]
+    many = 2 ** 31 // one[pools[0]].shape[-3:].numel() + 2 * small
+    if name == "tree_attention":  # infinities are looked up in the cache
+        for a in (one, two):
+            t = int(a["seq_lens"][0]) - 2
+            a["v_cache"][int(a["block_table"][0, t // 16]), :, t % 16, 3] = float("inf")
+    for k in pools:
+        shape = list(two[k].shape)
+        shape[-4] = many
+        big = torch.empty(shape, dtype=two[k].dtype, device="cuda")
+        big[..., -small:, :, :, :] = two[k]
+        two[k] = big
+    two["block_table"] = torch.where(two["block_table"] >= 0, two["block_table"] + many - small, -1).to(I32)
+    for a in (one, two):
+        getattr(sfv, name)(**a)
+        assert sfv.read_device_status(a["workspace"]) == 0
+    for key, a in one.items():
+        if isinstance(a, torch.Tensor) and key not in ("block_table", "workspace"):
+            b = two[key][..., -small:, :, :, :] if key in pools else two[key]
+            assert torch.equal(a.nan_to_num(-3), b.nan_to_num(-3)), key
