@@ -8,9 +8,9 @@
 // tokens have a kernel of their own, kv_evict_short_kernel; the rest of this is about
 // kv_evict_kernel.
 //
-// Which keys.  The weights' bits, ordered as unsigned integers (positive values above
-// negative ones, NaN as -infinity, the keys that stay in any case above all), in
-// three rounds of 11, 11 and 10 bits from the top: a histogram of the keys that agree
+// Which keys.  The first and the last ones stay in any case; of those between, the
+// weights' bits, ordered as unsigned integers (positive values above negative ones, NaN
+// as -infinity), in three rounds of 11, 11 and 10 bits from the top: a histogram of the keys that agree
 // with the digits found so far, the bin in which the budget's last key lies, the
 // same again inside that bin.  That gives the last kept key's value exactly, and how
 // many of its equals are kept (the lowest positions).  A second pass in order of the
@@ -23,13 +23,15 @@
 // or below their own j only, which later rounds do not read.
 //
 // What bounds it: the rows' way out and in, 256 bytes at a time from all over the cache.  32
-// layers of 32 heads, 3008 -> 1024 keys: 202 us, 5.4 TB/s, 79 % of the copy rate (with 16-byte
+// layers of 32 heads, 3008 -> 1024 keys: 196 us, 5.6 TB/s, 82 % of the copy rate (with 16-byte
 // loads and a barrier a round 350); 28 layers of 4 sequences and 4 heads, 8192 to 32768 ->
-// 4096 keys: 355 us, 80 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, so
-// that one's choice of keys runs beside another's rows (four with 24 KB: 197 and 368; five with
-// 16 KB: 219 and 436).  The choice itself reads the weights three times, the second and third
+// 4096 keys: 347 us, 82 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, or
+// four with 24 KB (evict_launch), so that one's choice of keys runs beside another's rows (five
+// with 16 KB: 219 and 436).  The choice reads the weights three times, the second and third
 // time from L2: the first digit's histogram, the few keys of its bin to shared memory, where
-// the other digits are found, and the places.
+// the other digits are found, and the places.  It is bound by its instructions, some 50 a
+// key and warp: with 65 (tests of every key for its place, both compares for ties in all
+// rounds) 448 heads of 30000 keys to 1000 took 148 us, so 132.
 //
 // The last CTA to finish writes the lengths and, if asked to, gives the pages that are no
 // longer needed back to the free-page stack: a thread a sequence, then a thread a page (one
@@ -44,14 +46,16 @@
 namespace sf {
 
 constexpr int kEvictThreads = 256;
-constexpr int kEvictBlocks = 3;        // CTAs per SM
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictBins = 2048;
-constexpr int kEvictSlot = 4096;       // bytes of a warp's rows of a round
 constexpr int kEvictKeys = 8;          // keys of a thread in flight
 constexpr int kEvictMaxCluster = 8;
 constexpr int kShortBatch = 4;         // 16-byte loads of a thread in flight
-constexpr int kEvictSmem = 2 * kEvictWarps * kEvictSlot > 5 * kEvictBins * 4 ? 2 * kEvictWarps * kEvictSlot : 5 * kEvictBins * 4;
+// With `blocks` CTAs per SM: bytes of a warp's rows of a round, and of shared memory.
+constexpr int evict_slot(int blocks) { return blocks == 4 ? 3072 : 4096; }
+constexpr int evict_smem(int blocks) {
+  return 2 * kEvictWarps * evict_slot(blocks) > 5 * kEvictBins * 4 ? 2 * kEvictWarps * evict_slot(blocks) : 5 * kEvictBins * 4;
+}
 
 struct EvictLayer {
   const float *mass;
@@ -83,8 +87,8 @@ __device__ __forceinline__ int evict_length(const EvictParams &p, int b, bool &c
 
 // Larger weights have larger keys; -0 counts as 0, NaN as -infinity.
 __device__ __forceinline__ uint32_t evict_key(float w) {
-  const uint32_t u = __float_as_uint(w == w ? w + 0.f : -INFINITY);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const int u = __float_as_int(fmaxf(w, -INFINITY) + 0.f);
+  return static_cast<uint32_t>(u ^ (u >> 31 | static_cast<int>(0x80000000u)));
 }
 
 // Bulk copies of rows back to global memory, in groups of the issuing thread.
@@ -197,15 +201,17 @@ __device__ __forceinline__ void evict_finish(const EvictParams &p, uint32_t *s_p
   }
 }
 
-template <int C>
-__global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(const __grid_constant__ EvictParams p) {
+template <int C, int BLOCKS>
+__global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kSlot = evict_slot(BLOCKS);
   extern __shared__ __align__(128) uint8_t smem[];
   // while the keys are chosen; then the slots of the rows on their way, two a warp
   uint32_t(*s_hist)[kEvictBins] = reinterpret_cast<uint32_t(*)[kEvictBins]>(smem);
   uint32_t *s_total = s_hist[3];  // a histogram of all CTAs
   uint32_t *s_few = s_hist[4];    // keys in the first digit's bin
   __shared__ __align__(8) uint64_t s_bar[kEvictWarps][2];
-  __shared__ uint32_t s_found, s_warp[kEvictWarps], s_pick[2], s_count[2];
+  __shared__ uint32_t s_rows[2][kEvictWarps];
+  __shared__ uint32_t s_found, s_warp[kEvictWarps], s_pick[3], s_count[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp_id();
   const int rank = C > 1 ? static_cast<int>(blockIdx.x % C) : 0, task = blockIdx.x / C;
   const int h = task % p.H_kv, lb = task / p.H_kv, b = lb % p.B;
@@ -236,12 +242,16 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       else if (mass != mass_out) mass_out[t] = mass[t];
     for (int j = me; j < p.budget; j += all) kept[j] = j < L ? j : -1;
   } else {
-    const int per = (L + C - 1) / C, from = min(rank * per, L), to = min(from + per, L);
-    const int late = L - p.recent;
-    auto key_of = [&](int t, float w) -> uint32_t { return t < p.first || t >= late ? 0xffffffffu : evict_key(w); };
-    uint32_t found = 0u, left = static_cast<uint32_t>(p.budget);
+    // the first and the last ones stay; of the `inner` others, `left` do
+    const int late = L - p.recent, inner = late - p.first;
+    const int per = (inner + C - 1) / C, from = p.first + min(rank * per, inner), to = min(from + per, late);
+    for (int i = rank * kEvictThreads + tid; i < p.first + p.recent; i += C * kEvictThreads) {
+      if (i < p.first) kept[i] = i;
+      else kept[p.budget - p.recent + i - p.first] = late + i - p.first;
+    }
+    uint32_t found = 0u, left = static_cast<uint32_t>(p.budget - p.first - p.recent);
     uint32_t mine = 0u;  // keys of this thread's bins above `found`, of this CTA
-    auto count_keys = [&](uint32_t *hist, bool in, uint32_t bin) {
+    auto count_keys = [&](uint32_t *hist, bool in, uint32_t bin) {  // (`in` is a constant for whole chunks)
       // one add for the lanes that agree with the first: weights cluster, and equal
       // addresses are served one after the other
       const unsigned any = __ballot_sync(0xffffffffu, in);
@@ -254,31 +264,38 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       else if (in && bin != common) atomicAdd(&hist[bin], 1u);
     };
     // all keys of this CTA's positions, kEvictKeys of a thread at a time
+    constexpr int kStep = kEvictThreads * kEvictKeys;
     auto each_key = [&](auto &&f) {
       float next[kEvictKeys];
       auto load = [&](int t0) {
+        const float *at = mass + t0 + tid;
+        if (t0 + kStep <= to) {
 #pragma unroll
-        for (int u = 0; u < kEvictKeys; ++u) {
-          const int t = t0 + u * kEvictThreads + tid;
-          next[u] = t < to ? mass[t] : 0.f;
+          for (int u = 0; u < kEvictKeys; ++u) next[u] = at[u * kEvictThreads];
+        } else {
+#pragma unroll
+          for (int u = 0; u < kEvictKeys; ++u) next[u] = t0 + u * kEvictThreads + tid < to ? at[u * kEvictThreads] : 0.f;
         }
       };
       load(from);
-      for (int t0 = from; t0 < to; t0 += kEvictThreads * kEvictKeys) {
+#pragma unroll 1
+      for (int t0 = from; t0 < to; t0 += kStep) {
         float now[kEvictKeys];
 #pragma unroll
         for (int u = 0; u < kEvictKeys; ++u) now[u] = next[u];
-        load(t0 + kEvictThreads * kEvictKeys);
+        load(t0 + kStep);
+        if (t0 + kStep <= to) {
 #pragma unroll
-        for (int u = 0; u < kEvictKeys; ++u) {
-          const int t = t0 + u * kEvictThreads + tid;
-          f(t < to, key_of(t, now[u]));
+          for (int u = 0; u < kEvictKeys; ++u) f(true, evict_key(now[u]));
+        } else {
+#pragma unroll
+          for (int u = 0; u < kEvictKeys; ++u) f(t0 + u * kEvictThreads + tid < to, evict_key(now[u]));
         }
       }
     };
-    each_key([&](bool in, uint32_t key) { count_keys(s_hist[0], in, key >> 21); });
+    if (left) each_key([&](bool in, uint32_t key) { count_keys(s_hist[0], in, key >> 21); });
 #pragma unroll 1
-    for (int round = 0; round < 3; ++round) {
+    for (int round = 0; round < 3 && left; ++round) {
       uint32_t *hist = s_hist[round];
       sync_all();
       // the bin that holds the left-th key from the top
@@ -311,6 +328,7 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
         if (above < left && left <= above + n[i]) {
           s_pick[0] = top + i;
           s_pick[1] = left - above;
+          s_pick[2] = n[i];
         }
         above += n[i];
       }
@@ -327,7 +345,7 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       if (round == 0) {
         // the keys of that bin, which the other digits are taken from
         each_key([&](bool in, uint32_t key) {
-          const bool take = in && (key >> 21) == (found >> 21);
+          const bool take = in && (key ^ found) < 1u << 21;
           const unsigned who = __ballot_sync(0xffffffffu, take);
           if (!who) return;
           uint32_t at = 0;
@@ -350,10 +368,11 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
         each_key([&](bool in, uint32_t key) { count_keys(s_hist[2], in && (key >> 10) == (found >> 10), key & 1023u); });
       }
     }
-    // Keys above `found` are kept, and the first `left` of those equal to it.  In front
-    // of this CTA's positions:
+    // Keys above `found` are kept, and the first `left` of those equal to it (mostly that
+    // is one, or all).  In front of this CTA's positions:
+    const bool all = left && left == s_pick[2];
     uint32_t larger = 0, equal = 0;
-    if constexpr (C > 1) {
+    if (C > 1 && left) {
       uint32_t sum;
       (void)evict_scan<kEvictWarps>(mine, s_warp, &sum);
       if (tid == 0) {
@@ -366,34 +385,41 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
         equal += ld_dsmem_u32(smem_addr(&s_count[1]), r);
       }
     }
+    if (all) larger += equal;
     float coming[kEvictKeys];
     auto load_row = [&](int t0) {  // a warp has 32 * kEvictKeys positions in a row
-#pragma unroll
-      for (int u = 0; u < kEvictKeys; ++u) {
-        const int t = t0 + (warp * kEvictKeys + u) * 32 + lane;
-        coming[u] = t < to ? mass[t] : 0.f;
-      }
-    };
-    load_row(from);
-    for (int t0 = from; t0 < to; t0 += kEvictThreads * kEvictKeys) {
       const int t1 = t0 + warp * 32 * kEvictKeys + lane;
-      uint32_t key[kEvictKeys], count = 0;
 #pragma unroll
-      for (int u = 0; u < kEvictKeys; ++u) key[u] = key_of(t1 + 32 * u, coming[u]);
-      load_row(t0 + kEvictThreads * kEvictKeys);
+      for (int u = 0; u < kEvictKeys; ++u) coming[u] = t1 + 32 * u < to ? mass[t1 + 32 * u] : 0.f;
+    };
+    const unsigned lower = (1u << lane) - 1u;
+    int32_t *const others = kept + p.first;
+    int turn = 0;
+    load_row(from);
+#pragma unroll 1
+    for (int t0 = from; t0 < to && left; t0 += kStep, turn ^= 1) {
+      const int t1 = t0 + warp * 32 * kEvictKeys + lane;
+      unsigned who[kEvictKeys], same[kEvictKeys];
+      uint32_t count = 0;
 #pragma unroll
       for (int u = 0; u < kEvictKeys; ++u) {
+        const uint32_t key = evict_key(coming[u]);
         const bool in = t1 + 32 * u < to;
-        count += __popc(__ballot_sync(0xffffffffu, in && key[u] > found)) +
-                 (__popc(__ballot_sync(0xffffffffu, in && key[u] == found)) << 16);
+        who[u] = __ballot_sync(0xffffffffu, in && (all ? key >= found : key > found));
+        count += __popc(who[u]);
+        same[u] = 0u;
+        if (!all) {
+          same[u] = __ballot_sync(0xffffffffu, in && key == found);
+          count += __popc(same[u]) << 16;
+        }
       }
-      __syncthreads();
-      if (lane == 0) s_warp[warp] = count;
+      load_row(t0 + kStep);
+      if (lane == 0) s_rows[turn][warp] = count;
       __syncthreads();
       uint32_t l = larger, e = equal;
 #pragma unroll
       for (int w = 0; w < kEvictWarps; ++w) {
-        const uint32_t x = s_warp[w];
+        const uint32_t x = s_rows[turn][w];
         if (w < warp) {
           l += x & 0xffffu;
           e += x >> 16;
@@ -401,23 +427,25 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
         larger += x & 0xffffu;
         equal += x >> 16;
       }
-      const unsigned lower = (1u << lane) - 1u;
 #pragma unroll
       for (int u = 0; u < kEvictKeys; ++u) {
-        const bool in = t1 + 32 * u < to, gt = in && key[u] > found, eq = in && key[u] == found;
-        const unsigned g = __ballot_sync(0xffffffffu, gt), q = __ballot_sync(0xffffffffu, eq);
-        const uint32_t before = e + __popc(q & lower);
-        if (gt || (eq && before < left)) kept[l + __popc(g & lower) + min(before, left)] = t1 + 32 * u;
-        l += __popc(g);
-        e += __popc(q);
+        const uint32_t before = all ? 0u : e + __popc(same[u] & lower);
+        if ((who[u] >> lane & 1u) || ((same[u] >> lane & 1u) && before < left))
+          others[l + __popc(who[u] & lower) + (all ? 0u : min(before, left))] = t1 + 32 * u;
+        l += __popc(who[u]);
+        e += __popc(same[u]);
       }
     }
     sync_all();
     // Rows in rounds of ascending places, by asynchronous copies: a warp has some rows of
     // every round and two slots of shared memory, so that a round's rows are on their way
     // in while the round before waits for its barrier and goes out.  Where they come from
-    // and go to is looked up a round ahead of that.
-    const int row_bytes = p.D * 2, R = min(16, kEvictSlot / (2 * row_bytes));
+    // and go to is looked up a round ahead of that.  One of two CTAs has K and the other V, so
+    // that neither waits for the other (11 ns a row, with rows of both 19); of more each has
+    // rows of both (a CTA's copies are bound by their number: 128-byte parts of rows
+    // took as long as whole ones).
+    constexpr int kSheets = C == 2 ? 1 : 2, kGroups = C == 2 ? 1 : C;
+    const int row_bytes = p.D * 2, R = min(32 / kSheets, kSlot / (kSheets * row_bytes));
     const int32_t *table = p.block_table + static_cast<size_t>(b) * p.max_pages;
     auto place = [&](int pos) -> int {
       const int page = table[pos / SF_PAGE_SIZE];
@@ -427,11 +455,13 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       }
       return (page * p.H_kv + h) * SF_PAGE_SIZE + pos % SF_PAGE_SIZE;
     };
-    const int r = lane % R, side = lane / R;  // the lane's row of the warp's, and K or V
-    const int first_row = (rank * kEvictWarps + warp) * R + r, rows = C * kEvictWarps * R;
+    const int r = lane % R, sheet = lane / R;  // the lane's row of the warp's
+    const int side = C == 2 ? rank : sheet;    // K or V
+    const bool works = sheet < kSheets;
+    const int group = C == 2 ? 0 : rank, first_row = (group * kEvictWarps + warp) * R + r, rows = kGroups * kEvictWarps * R;
     const int rounds = (p.budget + rows - 1) / rows;
     char *cache = reinterpret_cast<char *>(side == 0 ? layer.k : layer.v);
-    const uint32_t slot = smem_addr(smem) + warp * 2 * kEvictSlot + (side * R + r) * row_bytes;
+    const uint32_t slot = smem_addr(smem) + warp * 2 * kSlot + lane * row_bytes;
     const uint32_t bar = smem_addr(&s_bar[warp][0]);
     struct Row {
       int src, dst;  // cache rows, dst < 0: stays
@@ -440,9 +470,9 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
     auto look_up = [&](int round) -> Row {
       Row x{-1, -1, 0.f};
       const int j = round * rows + first_row;
-      if (side < 2 && j < p.budget) {
+      if (works && j < p.budget) {
         const int pos = kept[j];
-        x.w = mass[pos];
+        if (side == 0) x.w = mass[pos];
         if (pos != j) {
           x.src = place(pos);
           x.dst = place(j);
@@ -458,7 +488,7 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       if (lane == 0) mbar_arrive_expect_tx(full, static_cast<uint32_t>(__popc(who) * row_bytes));
       __syncwarp();
       if (x.dst >= 0)
-        bulk_copy_g2s(slot + (round & 1) * kEvictSlot, cache + static_cast<long long>(x.src) * row_bytes, row_bytes, full);
+        bulk_copy_g2s(slot + (round & 1) * kSlot, cache + static_cast<long long>(x.src) * row_bytes, row_bytes, full);
     };
     asm volatile("fence.proxy.async;" ::: "memory");  // the slots held the histograms
     __syncthreads();
@@ -473,13 +503,14 @@ __global__ void __launch_bounds__(kEvictThreads, kEvictBlocks) kv_evict_kernel(c
       }
       const Row then = look_up(round + 2);
       ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar + 8 * (round & 1), (round >> 1) & 1)) && ok;
-      sync_all();  // every row of this round and of those before is in
+      if constexpr (kGroups > 1) cluster_sync();  // every row of this round and of those before is in
+      else __syncthreads();
       if (ok && now.dst >= 0) {
-        bulk_copy_s2g(cache + static_cast<long long>(now.dst) * row_bytes, slot + (round & 1) * kEvictSlot, row_bytes);
+        bulk_copy_s2g(cache + static_cast<long long>(now.dst) * row_bytes, slot + (round & 1) * kSlot, row_bytes);
         bulk_commit();
       }
       const int j = round * rows + first_row;
-      if (side == 0 && j < p.budget) mass_out[j] = now.w;
+      if (works && side == 0 && j < p.budget) mass_out[j] = now.w;
       now = next;
       next = then;
     }
@@ -633,30 +664,31 @@ static int evict_setup(int device) {
   if (device < 0 || device >= 64) return fail(SF_ERR_UNSUPPORTED, "device ordinal %d", device);
   std::lock_guard<std::mutex> lock(mu);
   if (done[device]) return SF_OK;
-  for (auto fn : {kv_evict_kernel<1>, kv_evict_kernel<2>, kv_evict_kernel<4>, kv_evict_kernel<8>}) {
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictSmem);
+  for (auto fn : {kv_evict_kernel<1, 3>, kv_evict_kernel<1, 4>, kv_evict_kernel<2, 3>, kv_evict_kernel<4, 3>, kv_evict_kernel<8, 3>}) {
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, evict_smem(3));
     if (e != cudaSuccess) return fail(SF_ERR_CUDA, "cudaFuncSetAttribute (eviction): %s", cudaGetErrorString(e));
   }
   done[device] = true;
   return SF_OK;
 }
 
-// CTAs per (layer, sequence, KV head).  One CTA takes 9 us, 22 ns a row and 3.3 a key, so
-// `rows` says how long; a cluster's chain of barriers takes 6 us more with two or four CTAs
-// and 9 with eight, more yet where CTAs share an SM, and its rows 19, 10 and 5 ns.  In us,
-// one / two / four / eight CTAs (152 SMs):
+// CTAs per (layer, sequence, KV head).  One CTA takes 10 us, 24 ns a row and 2.5 a key, so
+// `rows` says how long; a cluster starts 6 to 9 us later, more yet where CTAs share an SM, and
+// takes 11 ns a row with two CTAs, 10 with four and 5 with eight.  In us, one / two / four /
+// eight CTAs (152 SMs):
 //     heads    500 to 400      1000 to 900     3000 to 1024    10000 to 6000
-//         8  17 / 21 / 19 / 19  28 / 30 / 23 / 21  35 / 33 / 24 / 22  163 / 125 / 72 / 45
-//        18  17 / 21 / 18 / 25  28 / 30 / 23 / 28  36 / 33 / 24 / 28  165 / 126 / 73 / 58
-//        40  17 / 21 / 22 / 31  28 / 30 / 27 / 34  36 / 33 / 29 / 35  193 / 143 / 108 / 86
-//       100  18 / 25 / 27 / 65  28 / 36 / 34 / 71  37 / 41 / 37 / 75  212 / 205 / 150 / 183
-//       200  22 / 29 / 51 / 126  41 / 48 / 71 / 147  54 / 59 / 81 / 154  286 / 268 / 291 / 354
+//         8  17 / 20 / 19 / 19  29 / 26 / 23 / 21  36 / 28 / 24 / 22  173 / 96 / 72 / 45
+//        18  18 / 20 / 18 / 25  29 / 26 / 23 / 28  36 / 28 / 25 / 28  177 / 97 / 72 / 58
+//        40  18 / 20 / 22 / 31  29 / 26 / 27 / 35  36 / 29 / 29 / 36  209 / 110 / 98 / 78
+//       100  18 / 23 / 26 / 65  29 / 31 / 33 / 71  38 / 35 / 36 / 74  228 / 150 / 133 / 168
+//       200  22 / 26 / 50 / 126  41 / 41 / 70 / 147  57 / 52 / 82 / 154  283 / 226 / 295 / 354
 static int evict_cluster(int tasks, int budget, int width, int sms) {
-  const long long rows = budget + 3LL * width / 20, slots = static_cast<long long>(kEvictBlocks) * sms;
+  const long long rows = budget + 3LL * width / 20, slots = 3LL * sms;
   if (rows < 640) return 1;
   if (8LL * tasks <= slots && (9LL * tasks <= sms || rows >= 3400)) return 8;
-  if (4LL * tasks <= slots && (2LL * tasks <= sms || rows >= 1800)) return 4;
-  return 2LL * tasks <= slots && rows >= 4500 ? 2 : 1;
+  if (4LL * tasks <= slots && (4LL * tasks <= sms || rows >= 2400)) return 4;
+  if (2LL * tasks <= slots && (2LL * tasks <= sms || rows >= 1400)) return 2;
+  return 1;
 }
 
 struct EvictLaunch {
@@ -676,8 +708,13 @@ static EvictLaunch evict_launch(int tasks, int budget, int width, int sms) {
     return many ? EvictLaunch{kv_evict_short_kernel<8, 4, 8>, 1, 128, 0} : EvictLaunch{kv_evict_short_kernel<8, 16, 2>, 1, 512, 0};
   if (width <= 512 && many) return {kv_evict_short_kernel<16, 4, 8>, 1, 128, 0};
   const int C = evict_cluster(tasks, budget, width, sms);
-  return {C == 1 ? kv_evict_kernel<1> : C == 2 ? kv_evict_kernel<2> : C == 4 ? kv_evict_kernel<4> : kv_evict_kernel<8>, C,
-          kEvictThreads, kEvictSmem};
+  // Four CTAs an SM with smaller slots where three leave more of the last wave empty (1024
+  // heads of 3008 tokens to 1024: 195 us, with three 210; 600 of 3000 to 1000 122, 134; 3584
+  // of 1000 to 200 164, 178; but 680 of 3000 to 2500 345, 305).
+  const int three = (tasks + 3 * sms - 1) / (3 * sms) * 3, four = (tasks + 4 * sms - 1) / (4 * sms) * 4;
+  if (C == 1 && four <= three) return {kv_evict_kernel<1, 4>, 1, kEvictThreads, evict_smem(4)};
+  return {C == 1 ? kv_evict_kernel<1, 3> : C == 2 ? kv_evict_kernel<2, 3> : C == 4 ? kv_evict_kernel<4, 3> : kv_evict_kernel<8, 3>, C,
+          kEvictThreads, evict_smem(3)};
 }
 
 }  // namespace sf

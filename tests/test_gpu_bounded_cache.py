@@ -251,8 +251,9 @@ def test_evict_budgets(budget, first, recent, in_place):
     ([5000], 1, 1, 128, 700), ([5000], 1, 2, 64, 4999), ([3000, 2000], 3, 8, 128, 1024), ([700] * 8, 16, 4, 64, 333),
     ([200, 90], 2, 3, 24, 61), ([200], 1, 2, 256, 100), ([150], 2, 1, 8, 40), ([20000], 1, 1, 64, 64),
     ([40] * 300, 1, 2, 64, 17), ([600], 128, 1, 64, 200),
-    # clusters of eight, four and two where CTAs share an SM
-    ([4500, 3600], 1, 20, 8, 3501), ([3000], 3, 30, 8, 1600), ([5200], 4, 40, 8, 4400), ([700, 4000], 2, 15, 16, 640)])
+    # clusters of eight, four and two, and of each where CTAs share an SM
+    ([2000], 1, 3, 256, 800), ([2000, 1900], 1, 10, 256, 800), ([2500], 1, 60, 128, 900), ([2500], 1, 60, 24, 900),
+    ([4500, 3600], 1, 20, 8, 3501), ([3000], 3, 30, 8, 2400), ([5200], 4, 40, 8, 4400), ([700, 4000], 2, 15, 16, 640)])
 def test_evict_shapes(before, layers, H_kv, d, budget):
     case = evict_case(before, layers, H_kv, d, seed=budget + d)
     assert check_evict(case, budget, 2, min(16, budget - 2), in_place=True, as_list=layers == 3)[0] == 0
