@@ -23,15 +23,15 @@
 // or below their own j only, which later rounds do not read.
 //
 // What bounds it: the rows' way out and in, 256 bytes at a time from all over the cache.  32
-// layers of 32 heads, 3008 -> 1024 keys: 196 us, 5.6 TB/s, 82 % of the copy rate (with 16-byte
+// layers of 32 heads, 3008 -> 1024 keys: 195 us, 5.6 TB/s, 82 % of the copy rate (with 16-byte
 // loads and a barrier a round 350); 28 layers of 4 sequences and 4 heads, 8192 to 32768 ->
-// 4096 keys: 347 us, 82 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, or
+// 4096 keys: 342 us, 83 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, or
 // four with 24 KB (evict_launch), so that one's choice of keys runs beside another's rows (five
 // with 16 KB: 219 and 436).  The choice reads the weights three times, the second and third
 // time from L2: the first digit's histogram, the few keys of its bin to shared memory, where
-// the other digits are found, and the places.  It is bound by its instructions, some 50 a
-// key and warp: with 65 (tests of every key for its place, both compares for ties in all
-// rounds) 448 heads of 30000 keys to 1000 took 148 us, so 132.
+// the other digits are found, and the places.  It is bound by its instructions: 448 heads of
+// 30000 keys to 1000 took 148 us with a test of every key for its place and two compares
+// for ties in all cases, 132 without, 129 with plain adds to the histogram.
 //
 // The last CTA to finish writes the lengths and, if asked to, gives the pages that are no
 // longer needed back to the free-page stack: a thread a sequence, then a thread a page (one
@@ -251,17 +251,10 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
     }
     uint32_t found = 0u, left = static_cast<uint32_t>(p.budget - p.first - p.recent);
     uint32_t mine = 0u;  // keys of this thread's bins above `found`, of this CTA
-    auto count_keys = [&](uint32_t *hist, bool in, uint32_t bin) {  // (`in` is a constant for whole chunks)
-      // one add for the lanes that agree with the first: weights cluster, and equal
-      // addresses are served one after the other
-      const unsigned any = __ballot_sync(0xffffffffu, in);
-      if (!any) return;
-      if (!in) bin = kEvictBins;
-      const int lead = __ffs(any) - 1;
-      const uint32_t common = __shfl_sync(0xffffffffu, bin, lead);
-      const unsigned same = __ballot_sync(0xffffffffu, bin == common);
-      if (lane == lead) atomicAdd(&hist[common], static_cast<uint32_t>(__popc(same)));
-      else if (in && bin != common) atomicAdd(&hist[bin], 1u);
+    // (an add a lane; one for all lanes of the first one's bin was slower whatever the weights:
+    // 448 heads of 30000 keys 135 us against 131, uniform ones 183, 159, all equal 133, 105)
+    auto count_keys = [&](uint32_t *hist, bool in, uint32_t bin) {
+      if (in) atomicAdd(&hist[bin], 1u);
     };
     // all keys of this CTA's positions, kEvictKeys of a thread at a time
     constexpr int kStep = kEvictThreads * kEvictKeys;
