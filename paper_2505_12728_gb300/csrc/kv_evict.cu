@@ -52,7 +52,7 @@ constexpr int kEvictKeys = 8;          // keys of a thread in flight
 constexpr int kEvictMaxCluster = 8;
 constexpr int kShortBatch = 4;         // 16-byte loads of a thread in flight
 // With `blocks` CTAs per SM: bytes of a warp's rows of a round, and of shared memory.
-constexpr int evict_slot(int blocks) { return blocks == 4 ? 3072 : 4096; }
+constexpr int evict_slot(int blocks) { return 12 * 1024 / blocks; }
 constexpr int evict_smem(int blocks) {
   return 2 * kEvictWarps * evict_slot(blocks) > 5 * kEvictBins * 4 ? 2 * kEvictWarps * evict_slot(blocks) : 5 * kEvictBins * 4;
 }
