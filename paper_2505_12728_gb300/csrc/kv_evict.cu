@@ -72,17 +72,23 @@ struct EvictParams {
   EvictLayer layers[SF_MAX_LAYERS];
 };
 
-// What is left of sequence b: the tokens of its context, and whether it is cut.
-__device__ __forceinline__ int evict_length(const EvictParams &p, int b, bool &cut, bool flag) {
-  const int T = p.seq_lens[b], n = T - p.n_q;
-  cut = false;
-  if (T == 0) return 0;
-  if (n < 0 || T > p.max_pages * SF_PAGE_SIZE || n > p.width) {
-    if (flag) set_status(p.status, SF_DEVICE_BAD_SEQLEN);
-    return n < 0 ? 0 : n > p.width ? p.width : n;
-  }
-  cut = n > p.budget;
-  return n;
+// What is left of sequence b: the tokens of its context, whether it is cut, and whether its
+// length cannot be (then nothing of it changes).
+__device__ __forceinline__ int evict_length(const EvictParams &p, int b, bool &cut, bool &bad) {
+  const int T = p.seq_lens[b], n = T < p.n_q ? 0 : T - p.n_q;
+  bad = T != 0 && (T < p.n_q || T > p.max_pages * SF_PAGE_SIZE || n > p.width);
+  cut = !bad && n > p.budget;
+  return min(n, p.width);
+}
+
+// A head of which nothing moves, by `all` threads: what lies behind the context has no weight
+// (that of a bad length says nothing about where that is).
+__device__ __forceinline__ void evict_nothing(const EvictParams &p, const float *mass, float *mass_out, int32_t *kept, int L,
+                                              bool bad, int me, int all) {
+  for (int t = me; t < p.width; t += all)
+    if (t >= L && !bad) mass_out[t] = 0.f;
+    else if (mass != mass_out) mass_out[t] = mass[t];
+  for (int j = me; j < p.budget; j += all) kept[j] = j < L ? j : -1;
 }
 
 // Larger weights have larger keys; -0 counts as 0, NaN as -infinity.
@@ -149,12 +155,12 @@ __device__ __forceinline__ void evict_finish(const EvictParams &p, uint32_t *s_p
     uint32_t *s_off = s_plan, *s_need = s_plan + THREADS;
     for (int b0 = 0; b0 < p.B; b0 += THREADS) {
       const int b1 = b0 + tid;
-      bool c1 = false;
+      bool c1 = false, bad;
       int need = 0;
       long long gone = 0, total;
       if (b1 < p.B) {
         const int T = p.seq_lens[b1];
-        (void)evict_length(p, b1, c1, false);
+        (void)evict_length(p, b1, c1, bad);
         const int now = c1 ? p.budget + p.n_q : T;
         p.seq_lens_out[b1] = now;  // (may be seq_lens)
         need = (now + SF_PAGE_SIZE - 1) / SF_PAGE_SIZE;
@@ -228,19 +234,15 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
     fence_mbar_init();
   }
   grid_dependency_wait();
-  bool cut;
-  const int L = evict_length(p, b, cut, task / p.H_kv < p.B && h == 0 && rank == 0 && tid == 0);
+  bool cut, bad;
+  const int L = evict_length(p, b, cut, bad);
+  if (bad && lb < p.B && h == 0 && rank == 0 && tid == 0) set_status(p.status, SF_DEVICE_BAD_SEQLEN);
   const float *mass = layer.mass + bh * p.width;
   float *mass_out = layer.mass_out + bh * p.width;
   int32_t *kept = layer.kept + bh * p.budget;
   __syncthreads();
   if (!cut) {
-    // nothing moves
-    const int all = C * kEvictThreads, me = rank * kEvictThreads + tid;
-    for (int t = me; t < p.width; t += all)
-      if (t >= L) mass_out[t] = 0.f;
-      else if (mass != mass_out) mass_out[t] = mass[t];
-    for (int j = me; j < p.budget; j += all) kept[j] = j < L ? j : -1;
+    evict_nothing(p, mass, mass_out, kept, L, bad, rank * kEvictThreads + tid, C * kEvictThreads);
   } else {
     // the first and the last ones stay; of the `inner` others, `left` do
     const int late = L - p.recent, inner = late - p.first;
@@ -533,16 +535,14 @@ __global__ void __launch_bounds__(32 * WARPS, BLOCKS) kv_evict_short_kernel(cons
   const EvictLayer &layer = p.layers[lb / p.B];
   const size_t bh = static_cast<size_t>(b) * p.H_kv + h;
   grid_dependency_wait();
-  bool cut;
-  const int L = evict_length(p, b, cut, lb < p.B && h == 0 && tid == 0);
+  bool cut, bad;
+  const int L = evict_length(p, b, cut, bad);
+  if (bad && lb < p.B && h == 0 && tid == 0) set_status(p.status, SF_DEVICE_BAD_SEQLEN);
   const float *mass = layer.mass + bh * p.width;
   float *mass_out = layer.mass_out + bh * p.width;
   int32_t *kept = layer.kept + bh * p.budget;
   if (!cut) {
-    for (int t = tid; t < p.width; t += THREADS)
-      if (t >= L) mass_out[t] = 0.f;
-      else if (mass != mass_out) mass_out[t] = mass[t];
-    for (int j = tid; j < p.budget; j += THREADS) kept[j] = j < L ? j : -1;
+    evict_nothing(p, mass, mass_out, kept, L, bad, tid, THREADS);
   } else {
     if (warp == 1 && lane < MOST / SF_PAGE_SIZE)
       s_page[lane] = lane * SF_PAGE_SIZE < L ? p.block_table[static_cast<size_t>(b) * p.max_pages + lane] : -1;
