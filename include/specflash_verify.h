@@ -701,8 +701,9 @@ int sf_tree_commit(const int32_t *tokens, const int32_t *sampled, const int32_t 
 /*                                                                           */
 /* lse          fp32 [B][n_q][H_q] (natural log); a row of -inf counts 0.     */
 /* mass         fp32 [B][H_kv][mass_width], or NULL for 0; may be mass_out.   */
-/* row_weights  fp32 [B][n_q], finite and >= 0, or NULL for 1.  What a row of */
-/*              weight 0 holds has no effect (NaN neither).                   */
+/* row_weights  fp32 [B][n_q], finite and >= 0, or NULL for 1.  A row of      */
+/*              weight 0 has no effect, whatever it and the keys hold (NaN    */
+/*              and infinities neither).                                      */
 /* Limits and device flags: those of sf_tree_attention (n_q likewise); L_b    */
 /* above mass_width is clamped and flagged with SF_DEVICE_BAD_SEQLEN.         */
 /* workspace    >= sf_attention_mass_workspace_size() bytes, 256-byte         */
