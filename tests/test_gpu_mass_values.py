@@ -1,5 +1,6 @@
 """sf_attention_mass where it is easy to go wrong (GPU): infinite keys beside rows that do
-not count."""
+not count, and contexts of many key tiles a CTA, in which the ring of keys, the buffers of
+queries and those of scores come round several times."""
 import math
 
 import pytest
@@ -59,3 +60,46 @@ def test_infinite_keys_and_rows_that_saw_nothing():
     assert float(got[0, 1, 50]) == 0.0
     got[0, 1, 50] = want[0, 1, 50]
     assert torch.equal(got, want)
+
+
+def reference(args, weights):
+    """As tree_reference.mass, on the GPU, one sequence and KV head at a time."""
+    q, lse, kc, bt, lens = (a.cuda() for a in args)
+    B, n, H, d = q.shape
+    kv, scale = kc.shape[1], 1 / math.sqrt(d)
+    g = H // kv
+    for b in range(B):
+        before = int(lens[b]) - n
+        if before <= 0:
+            continue
+        pages = bt[b, :-(-before // 16)].long()
+        for h in range(kv):
+            k = kc[pages, h].reshape(-1, d)[:before].double()
+            x = q[b, :, h * g:(h + 1) * g].reshape(n * g, d).double()
+            m = lse[b, :, h * g:(h + 1) * g].reshape(n * g, 1).double()
+            w = weights[b].cuda().double().repeat_interleave(g)[:, None]
+            s = scale * (x @ k.T) - m
+            p = w * s.exp()
+            off = d * 2.0 ** -23 * scale * (x.abs() @ k.abs().T) + (s.abs() + m.abs()) * 2.0 ** -22 + 2.0 ** -20
+            yield b, h, before, p.sum(0), (p * (off + n * g * 2.0 ** -24)).sum(0)
+
+
+# 224 rows: two q buffers, three ring slots, two chunks; 512: one q buffer, two slots, four
+# chunks, several segments a CTA; few rows: the deepest rings, with 64-wide heads as well
+@pytest.mark.parametrize("lens, n, H_q, H_kv, d", [
+    ([16000] * 16, 32, 28, 4, 128), ([200 + (37 * b) % 401 for b in range(200)], 64, 8, 1, 128),
+    ([40000, 39999, 17, 30001], 5, 8, 8, 64), ([20000] * 4, 5, 8, 8, 128), ([9000, None, 12000], 64, 16, 2, 64),
+    ([6000] * 12, 33, 6, 6, 128)])
+def test_many_key_tiles_a_cta(lens, n, H_q, H_kv, d):
+    require_gpu()
+    args = make(lens, n, H_q, H_kv, d, seed=len(lens) + n)
+    g = torch.Generator().manual_seed(9)
+    weights = (torch.rand(len(lens), n, generator=g) < 0.8).float() * torch.rand(len(lens), n, generator=g)
+    got, status = run_mass(args, row_weights=weights.cuda())
+    assert status == 0
+    again, _ = run_mass(args, row_weights=weights.cuda())
+    assert torch.equal(got, again)
+    for b, h, before, want, bound in reference(args, weights):
+        err = (got[b, h, :before].double() - want).abs()
+        assert (err <= bound).all(), (b, h, (err - bound).max())
+        assert not got[b, h, before:].any()
