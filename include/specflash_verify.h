@@ -653,11 +653,14 @@ int sf_tree_attention(const void *q, const void *k_cache, const void *v_cache,
 /* With free_pages, the lengths and pages are then prepared for the next tree */
 /* of n_q_next nodes, exactly as by sf_kv_commit (whose arguments these are); */
 /* without, seq_lens and block_table stay as they are.                        */
-/* Slots with seq_lens[b] = 0 are idle: num_accepted 0, path and out_tokens   */
-/* -1, row_weights 0.  A seq_lens[b] outside [n_q, 16 * max_pages_per_seq]    */
-/* sets SF_DEVICE_BAD_SEQLEN and counts as idle (and sf_kv_commit's part      */
-/* changes nothing); a row whose page is outside the pool is not moved and    */
-/* sets SF_DEVICE_BAD_PAGE.                                                   */
+/* A sequence whose node 0 is no root (parents[b][0] not -1; from 0 on it     */
+/* also sets SF_DEVICE_BAD_INDEX) has no path: num_accepted 0, path and       */
+/* out_tokens -1, row_weights 0, no row moves, and its context stays as long  */
+/* as it was (with free_pages the next tree's rows follow it). Slots with     */
+/* seq_lens[b] = 0 are idle: the same results, and no pages. A seq_lens[b]    */
+/* outside [n_q, 16 * max_pages_per_seq] sets SF_DEVICE_BAD_SEQLEN and counts */
+/* as idle (and sf_kv_commit's part changes nothing); a row whose page is     */
+/* outside the pool is not moved and sets SF_DEVICE_BAD_PAGE.                 */
 /*                                                                           */
 /* tokens       int32 [B][n_q], the nodes' tokens; sampled int32 [B][n_q];    */
 /* parents      int32 [B][n_q], as for sf_tree_mask.                          */

@@ -31,7 +31,9 @@ struct CommitParams {
   const int32_t *num_accepted;
   uint32_t *status;
   int B, n_q, n_q_next, max_pages, capacity;
-  int idle_slots;  // a length of 0 marks a slot that stays as it is
+  // A tree's [B][n_q], or null.  With it a length of 0 marks a slot that stays as it is, and
+  // no row stays where node 0 is not a root (-1).
+  const int32_t *parents;
 };
 
 // Block-wide exclusive scan of one int per thread (blockDim.x threads);
@@ -63,12 +65,13 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const CommitP
   int push = 0, take = 0, bad = 0, had = 0, need = 0, next_len = 0;
   if (b < p.B) {
     const int T = p.seq_lens[b], a = p.num_accepted[b];
-    if (T == 0 && p.idle_slots) {
+    if (T == 0 && p.parents) {
       // no pages, no rows
     } else if (T < p.n_q || a < 0) {
       bad = 1;
     } else {
-      const int keep = a + 1 < p.n_q ? a + 1 : p.n_q;
+      const bool none = p.parents && p.parents[static_cast<size_t>(b) * p.n_q] != -1;
+      const int keep = none ? 0 : a + 1 < p.n_q ? a + 1 : p.n_q;
       const long long nl = (long long)(T - p.n_q) + keep + p.n_q_next;
       had = (T + kPageTokensCommit - 1) / kPageTokensCommit;
       const long long nd = (nl + kPageTokensCommit - 1) / kPageTokensCommit;
@@ -112,7 +115,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const CommitP
 
 int launch_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_pages, int32_t *free_count,
                      const int32_t *num_accepted, int B, int n_q, int n_q_next, int max_pages, int capacity,
-                     bool idle_slots, uint32_t *status, cudaStream_t stream) {
+                     const int32_t *parents, uint32_t *status, cudaStream_t stream) {
   CommitParams prm;
   prm.seq_lens = seq_lens;
   prm.block_table = block_table;
@@ -125,7 +128,7 @@ int launch_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_page
   prm.n_q_next = n_q_next;
   prm.max_pages = max_pages;
   prm.capacity = capacity;
-  prm.idle_slots = idle_slots;
+  prm.parents = parents;
   const int threads = (B + 31) / 32 * 32;
   kv_commit_kernel<<<1, threads, 0, stream>>>(prm);
   cudaError_t e = cudaGetLastError();
@@ -164,7 +167,7 @@ int sf_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_pages,
     return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes,
                 sf_kv_commit_workspace_size());
   return launch_kv_commit(seq_lens, block_table, free_pages, free_count, num_accepted, B, n_q, n_q_next,
-                          max_pages_per_seq, capacity, false, static_cast<uint32_t *>(workspace), stream);
+                          max_pages_per_seq, capacity, nullptr, static_cast<uint32_t *>(workspace), stream);
 }
 
 }  // extern "C"

@@ -16,7 +16,8 @@
 // so a tree of depth t takes log2(t) rounds, at most six.
 //
 // tree_commit: from the root, as long as a child carries the token that the
-// target gives at its parent, the lowest such child is next.  The rows of the
+// target gives at its parent, the lowest such child is next (a sequence whose node
+// 0 is no root has no path: its masks are 0).  The rows of the
 // path then follow the context: row path[r] of keys and values moves to row r.
 // path[r] >= r and ascends, so rows that are written never hold what a later row
 // still has to be read from, and a warp that moves one KV head's rows of one layer
@@ -29,10 +30,11 @@
 namespace sf {
 
 // kv_commit.cu: the pages and lengths after n_q verified rows (sf_kv_commit), where
-// a length of 0 marks an idle slot.
+// a length of 0 marks an idle slot and none of the rows stay where parents [B][n_q]
+// has no root at node 0.
 int launch_kv_commit(int32_t *seq_lens, int32_t *block_table, int32_t *free_pages, int32_t *free_count,
                      const int32_t *num_accepted, int B, int n_q, int n_q_next, int max_pages, int capacity,
-                     bool idle_slots, uint32_t *status, cudaStream_t stream);
+                     const int32_t *parents, uint32_t *status, cudaStream_t stream);
 
 constexpr int kTreeWarps = 4;
 constexpr int kTreeBatch = 8;  // 16-byte loads of a thread in flight
@@ -121,6 +123,7 @@ __device__ __forceinline__ void commit_rows(const TreeCommitParams &p, int b, in
     if (at_head == 0 && lane == 0) set_status(p.status, SF_DEVICE_BAD_SEQLEN);
     live = false;
   }
+  if (__shfl_sync(0xffffffffu, parent[0], 0) != -1) live = false;  // node 0 is no root
   // path[r] of r = lane and r = lane + 32, its node's target token
   int path[2] = {-1, -1}, out[2] = {-1, -1};
   unsigned long long on = 0ull;
@@ -321,7 +324,7 @@ int sf_tree_commit(const int32_t *tokens, const int32_t *sampled, const int32_t 
   if (e != cudaSuccess) return fail(SF_ERR_CUDA, "tree commit launch: %s", cudaGetErrorString(e));
   if (!free_pages) return SF_OK;
   return launch_kv_commit(seq_lens, block_table, free_pages, free_count, num_accepted, B, n_q, n_q_next,
-                          max_pages_per_seq, capacity, true, p.status, stream);
+                          max_pages_per_seq, capacity, parents, p.status, stream);
 }
 
 }  // extern "C"

@@ -1056,7 +1056,8 @@ def tree_commit(tokens, sampled, parents, k_caches, v_caches, block_table, seq_l
     keys and values moved to follow the context.  tokens (the nodes'), sampled (the
     target's after each node) and parents int32 [B][n]; k_caches and v_caches bf16
     [layers][pages][H_kv][16][d] or lists of the layers' caches; block_table and
-    seq_lens as for tree_attention.  With free_pages and free_count, seq_lens and
+    seq_lens as for tree_attention.  Where node 0 is no root (parents not -1) there is
+    no path: path and out_tokens -1, the rest 0.  With free_pages and free_count, seq_lens and
     block_table are then prepared for the next tree of n_q_next nodes (None: n), as
     by kv_commit.  Returns (num_accepted int32 [B], out_tokens int32 [B][n], path
     int32 [B][n], row_weights fp32 [B][n])."""
