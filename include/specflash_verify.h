@@ -753,7 +753,9 @@ int sf_attention_mass(const void *q, const float *lse, const void *k_cache,
 /* A sequence with L_b < 0, or longer than its pages or mass_width, sets      */
 /* SF_DEVICE_BAD_SEQLEN and is left as it is, its weights over the whole      */
 /* width too (mass_out = mass).  A row whose old or new page is outside the   */
-/* pool is not moved and sets SF_DEVICE_BAD_PAGE.                             */
+/* pool is not moved and sets SF_DEVICE_BAD_PAGE.  After SF_DEVICE_TIMEOUT    */
+/* lengths, block_table and the stack are what they were, and what the caches */
+/* and weights hold is undefined.                                             */
 /* 1 <= num_layers <= SF_MAX_LAYERS; 1 <= budget; first, recent >= 0, first + */
 /* recent <= budget; 0 <= n_q <= SF_MAX_TREE_ROWS; head_dim a multiple of 8   */
 /* in [8, 256]; H_kv <= 1024.                                                 */

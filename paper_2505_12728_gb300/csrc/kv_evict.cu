@@ -67,7 +67,7 @@ struct EvictLayer {
 struct EvictParams {
   const int32_t *seq_lens;
   int32_t *block_table, *seq_lens_out, *free_pages, *free_count;
-  uint32_t *status, *ticket;
+  uint32_t *status, *ticket, *gave_up;
   int B, H_kv, D, num_pages, max_pages, width, budget, first, recent, n_q, capacity;
   EvictLayer layers[SF_MAX_LAYERS];
 };
@@ -137,17 +137,29 @@ __device__ __forceinline__ T evict_scan(T v, T *s_warp, T *total) {
   return off + incl - v;
 }
 
-// The last CTA to come here writes the lengths and gives the pages back.
+// The last CTA to come here writes the lengths and gives the pages back.  If one gave up
+// on a row they stay as they were: what is in the cache is nobody's context.
 template <int THREADS>
-__device__ __forceinline__ void evict_finish(const EvictParams &p, uint32_t *s_plan /* [2][THREADS] */) {
-  __shared__ uint32_t s_last;
+__device__ __forceinline__ void evict_finish(const EvictParams &p) {
+  __shared__ uint32_t s_last, s_stop;
   __shared__ long long s_wide[THREADS / 32];
+  __shared__ uint32_t s_plan[2 * THREADS];
   const int tid = threadIdx.x;
   __syncthreads();
-  if (tid == 0) s_last = atom_add_acq_rel_gpu(p.ticket, 1u) == gridDim.x - 1;
+  if (tid == 0) {
+    s_last = atom_add_acq_rel_gpu(p.ticket, 1u) == gridDim.x - 1;
+    s_stop = s_last ? *p.gave_up : 0u;
+  }
   __syncthreads();
   if (s_last) {
-    if (tid == 0) *p.ticket = 0u;
+    if (tid == 0) {
+      *p.ticket = 0u;
+      if (s_stop) *p.gave_up = 0u;
+    }
+    if (s_stop) {
+      for (int b = tid; b < p.B; b += THREADS) p.seq_lens_out[b] = p.seq_lens[b];
+      return;
+    }
     // A thread a sequence; then the pages of all of them, found by their places on the stack.
     const int fc0 = p.free_count ? *p.free_count : 0;
     long long freed = fc0;
@@ -477,7 +489,9 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
       return x;
     };
     bool ok = true;
+    int asked = 0;  // rounds whose rows were asked for
     auto copy_in = [&](int round, const Row &x) {
+      asked = round + 1;
       const unsigned who = __ballot_sync(0xffffffffu, x.dst >= 0);
       const uint32_t full = bar + 8 * (round & 1);
       if (lane == 0) mbar_arrive_expect_tx(full, static_cast<uint32_t>(__popc(who) * row_bytes));
@@ -491,13 +505,13 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
     copy_in(0, now);
 #pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
-      if (round + 1 < rounds) {
+      if (ok && round + 1 < rounds) {
         bulk_wait_read();  // this lane's rows of the round before have left the slot
         __syncwarp();
         copy_in(round + 1, next);
       }
       const Row then = look_up(round + 2);
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar + 8 * (round & 1), (round >> 1) & 1)) && ok;
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar + 8 * (round & 1), (round >> 1) & 1));
       if constexpr (kGroups > 1) cluster_sync();  // every row of this round and of those before is in
       else __syncthreads();
       if (ok && now.dst >= 0) {
@@ -510,12 +524,20 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
       next = then;
     }
     bulk_wait_all();
-    if (!ok && lane == 0) set_status(p.status, SF_DEVICE_TIMEOUT);
+    if (!ok) {  // the copies still in flight land (bounded) before shared memory is left
+      for (int round = max(asked - 2, 0); round < asked; ++round)
+        (void)mbar_wait_bounded(bar + 8 * (round & 1), (round >> 1) & 1);
+      if (lane == 0) {
+        set_status(p.status, SF_DEVICE_TIMEOUT);
+        atomicOr(p.gave_up, 1u);
+      }
+      __syncwarp();
+    }
     sync_all();
     for (int t = p.budget + rank * kEvictThreads + tid; t < p.width; t += C * kEvictThreads) mass_out[t] = 0.f;
   }
 
-  evict_finish<kEvictThreads>(p, reinterpret_cast<uint32_t *>(smem));
+  evict_finish<kEvictThreads>(p);
   launch_dependents_after_stores();
 }
 
@@ -526,7 +548,6 @@ __global__ void __launch_bounds__(kEvictThreads, BLOCKS) kv_evict_kernel(const _
 template <int KEYS, int WARPS, int BLOCKS>
 __global__ void __launch_bounds__(32 * WARPS, BLOCKS) kv_evict_short_kernel(const __grid_constant__ EvictParams p) {
   constexpr int THREADS = 32 * WARPS, PARTS = WARPS / 2, MOST = 32 * KEYS;
-  __shared__ uint32_t s_plan[2 * THREADS];
   __shared__ int32_t s_page[MOST / SF_PAGE_SIZE];
   __shared__ uint16_t s_pos[MOST];
   __shared__ int s_first;
@@ -633,7 +654,7 @@ __global__ void __launch_bounds__(32 * WARPS, BLOCKS) kv_evict_short_kernel(cons
       __syncwarp();
     }
   }
-  evict_finish<THREADS>(p, s_plan);
+  evict_finish<THREADS>(p);
   launch_dependents_after_stores();
 }
 
@@ -777,6 +798,7 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
   p.free_count = free_count;
   p.status = reinterpret_cast<uint32_t *>(ws);
   p.ticket = reinterpret_cast<uint32_t *>(ws + 128);
+  p.gave_up = reinterpret_cast<uint32_t *>(ws + 192);
   p.B = B;
   p.H_kv = H_kv;
   p.D = head_dim;

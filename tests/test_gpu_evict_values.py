@@ -1,5 +1,5 @@
-"""sf_kv_evict where it is easy to go wrong (GPU): lengths that it refuses on the device.
-Everything has to be equal."""
+"""sf_kv_evict where it is easy to go wrong (GPU): lengths that it refuses on the device,
+and calls in which a CTA gave up.  Everything has to be equal."""
 import pytest
 import torch
 
@@ -11,6 +11,9 @@ from tests.test_gpu_bounded_cache import evict_case
 pytestmark = pytest.mark.gpu
 
 i32 = lambda v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+
+# The word of the workspace in which CTAs that gave up on a copy say so.
+GAVE_UP = slice(192, 196)
 
 
 # Kernels: one warp a head (tables of up to 256 tokens), one CTA a head, clusters of eight.
@@ -58,3 +61,26 @@ def test_a_length_of_more_than_the_weights_leaves_them():
         sfv.kv_evict(m, kc.cuda(), vc.cuda(), bt.cuda(), sl, 50, workspace=ws)
         assert sfv.read_device_status(ws) == sfv.SF_DEVICE_BAD_SEQLEN and sl.tolist() == [1000, 50]
         assert torch.equal(m[0, 0].cpu(), mass[0, 0])
+
+
+@pytest.mark.parametrize("longest, H_kv", [(200, 2), (700, 2), (4000, 2)])
+def test_lengths_and_pages_stay_where_a_cta_gave_up(longest, H_kv):
+    # Rows that did not arrive make the cache useless; a length or a page that says otherwise
+    # would hand it on.  The failure is made here, by the word in which such a CTA says so.
+    require_gpu()
+    mass, kc, vc, bt, lens = evict_case([longest, 100], 1, H_kv, 64, seed=longest + 1, n=4)
+    m, k, v, table, sl = mass.cuda(), kc.cuda(), vc.cuda(), bt.cuda(), i32(lens).cuda()
+    free, count = torch.full((600,), -9, dtype=torch.int32, device="cuda"), i32([3]).cuda()
+    sl_out = torch.full_like(sl, -1)
+    ws = sfv.new_workspace(sfv.kv_evict_workspace_size(1, 2, H_kv, 40))
+    ws[GAVE_UP] = 1
+    call = lambda: sfv.kv_evict(m, k, v, table, sl, 40, n_q=4, mass_out=torch.empty_like(m), seq_lens_out=sl_out,  # noqa: E731
+                                free_pages=free, free_count=count, workspace=ws)
+    call()
+    assert sl_out.tolist() == lens and torch.equal(table.cpu(), bt)
+    assert int(count) == 3 and (free == -9).all()
+    assert not ws[GAVE_UP].any()  # the next call starts anew
+    k.copy_(kc)
+    v.copy_(vc)
+    call()
+    assert sl_out.tolist() == [44, 44] and int(count) == 3 + sum(-(-x // 16) - 3 for x in lens)
