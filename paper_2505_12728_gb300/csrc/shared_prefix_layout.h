@@ -67,4 +67,15 @@ constexpr int sp_stages(int D, int B, int num_groups) {
                   : (sp_smem_bytes<64, 10>(B, num_groups) <= kSpSmemMax ? 10 : 8);
 }
 
+// Partial rows that the pieces of a tree call may take: a KV head's n_q * group rows of each
+// sequence (of one more head where pairs of an odd number of heads lie on the axis), two
+// tiles for each pair of row tiles where one tile does not hold them, and two tiles for each
+// CTA, so that the pieces of a segment in several CTAs lie apart.
+constexpr long long sp_tree_rows(int B, int n_q, int group, int H_kv, int G) {
+  const int per_tile = kSpTile / group, tiles = (n_q + per_tile - 1) / per_tile;
+  const long long segments = tiles == 1 ? static_cast<long long>(B) * (H_kv + 1) * n_q * group
+                                        : static_cast<long long>(B) * H_kv * 2 * kSpTile;
+  return (tiles + 1) / 2 * (segments + 2LL * kSpTile * G);
+}
+
 }  // namespace sf

@@ -43,14 +43,12 @@ static int check_tree_attention(int B, int n_q, int H_q, int H_kv, int D, int ma
   return SF_OK;
 }
 
-
 // Upper bounds over all lengths of B sequences.
 static SpBounds tree_bounds(int B, int n_q, int H_q, int H_kv, int max_pages, int G) {
-  const long long group = H_q / H_kv, per_tile = kSpTile / group, tiles = (n_q + per_tile - 1) / per_tile;
-  const long long pairs = (tiles + 1) / 2, key_tiles = ((long long)max_pages + kSpTilePages - 1) / kSpTilePages;
+  const long long key_tiles = ((long long)max_pages + kSpTilePages - 1) / kSpTilePages;
   SpBounds b;
   b.cost = (long long)B * H_kv * (kSpCostSegTwo + kSpCostFew + std::max(kSpCostTwo, 2 * kSpCostOne) * key_tiles);
-  b.rows = pairs * ((long long)B * (H_kv + 1) * 2 * kSpTile + 2LL * kSpTile * G);
+  b.rows = sp_tree_rows(B, n_q, H_q / H_kv, H_kv, G);
   return b;
 }
 
