@@ -759,8 +759,8 @@ int sf_attention_mass(const void *q, const float *lse, const void *k_cache,
 /* 1 <= num_layers <= SF_MAX_LAYERS; 1 <= budget; first, recent >= 0, first + */
 /* recent <= budget; 0 <= n_q <= SF_MAX_TREE_ROWS; head_dim a multiple of 8   */
 /* in [8, 256]; H_kv <= 1024.                                                 */
-/* workspace    >= sf_kv_evict_workspace_size(...) bytes, 256-byte aligned,   */
-/*              zero-filled before first use.                                 */
+/* workspace    >= sf_kv_evict_workspace_size(...) bytes (256 where kept is   */
+/*              given), 256-byte aligned, zero-filled before first use.       */
 /* Deterministic.  Lets no kernel start before its stores can be read.        */
 /* ------------------------------------------------------------------------ */
 size_t sf_kv_evict_workspace_size(int num_layers, int B, int H_kv, int budget);

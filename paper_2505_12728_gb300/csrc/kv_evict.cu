@@ -50,6 +50,7 @@ constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictBins = 2048;
 constexpr int kEvictKeys = 8;          // keys of a thread in flight
 constexpr int kEvictMaxCluster = 8;
+constexpr size_t kEvictHeader = 256;   // status, ticket, word of the CTAs that gave up
 constexpr int kShortBatch = 4;         // 16-byte loads of a thread in flight
 // With `blocks` CTAs per SM: bytes of a warp's rows of a round, and of shared memory.
 constexpr int evict_slot(int blocks) { return 12 * 1024 / blocks; }
@@ -660,7 +661,7 @@ __global__ void __launch_bounds__(32 * WARPS, BLOCKS) kv_evict_short_kernel(cons
 
 // `kept` of all layers for a call that does not ask for it lies behind the header.
 static size_t evict_bytes(int layers, int B, int H_kv, int budget) {
-  return 256 + round_up(static_cast<size_t>(layers) * B * H_kv * budget * sizeof(int32_t), 256);
+  return kEvictHeader + round_up(static_cast<size_t>(layers) * B * H_kv * budget * sizeof(int32_t), 256);
 }
 
 static int check_evict(int layers, int B, int H_kv, int budget) {
@@ -772,9 +773,8 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
     return fail(SF_ERR_UNSUPPORTED, "%d layers of %d sequences with %d heads", num_layers, B, H_kv);
   if (!workspace || !aligned(workspace, 256))
     return fail(SF_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
-  if (workspace_bytes < evict_bytes(num_layers, B, H_kv, budget))
-    return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes,
-                evict_bytes(num_layers, B, H_kv, budget));
+  const size_t need = kept ? kEvictHeader : evict_bytes(num_layers, B, H_kv, budget);
+  if (workspace_bytes < need) return fail(SF_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
   EvictParams p;
   uint8_t *ws = static_cast<uint8_t *>(workspace);
   for (int l = 0; l < num_layers; ++l) {
@@ -783,7 +783,7 @@ int sf_kv_evict(const float *const *mass, void *const *k_caches, void *const *v_
     x.mass_out = mass_out[l];
     x.k = static_cast<uint4 *>(k_caches[l]);
     x.v = static_cast<uint4 *>(v_caches[l]);
-    x.kept = kept ? kept[l] : reinterpret_cast<int32_t *>(ws + 256) + static_cast<size_t>(l) * B * H_kv * budget;
+    x.kept = kept ? kept[l] : reinterpret_cast<int32_t *>(ws + kEvictHeader) + static_cast<size_t>(l) * B * H_kv * budget;
     if (!x.mass || !x.mass_out || !x.k || !x.v || !x.kept)
       return fail(SF_ERR_INVALID_ARG, "a required pointer of layer %d is NULL", l);
     if (!aligned(x.mass, 4) || !aligned(x.mass_out, 4) || !aligned(x.k, 16) || !aligned(x.v, 16) || !aligned(x.kept, 4))

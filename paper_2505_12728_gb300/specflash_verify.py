@@ -1196,7 +1196,8 @@ def kv_evict(mass, k_caches, v_caches, block_table, seq_lens, budget, *, first=0
         _same_count(counts)
     free, count, capacity = _free_stack(free_pages, free_count)
     if workspace is None:
-        workspace = _new(kv_evict_workspace_size(layers, B, H_kv, budget), _U8, block_table.device, stream, zero=True)
+        size = kv_evict_workspace_size(layers, B, H_kv, budget) if kept is None else 256
+        workspace = _new(size, _U8, block_table.device, stream, zero=True)
     _need_workspace(workspace)
     _check(load_library().sf_kv_evict(
         m_ptrs, k_ptrs, v_ptrs, layers, block_table.data_ptr(), seq_lens.data_ptr(), B, H_kv, d, page, num_pages,

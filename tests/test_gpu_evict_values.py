@@ -84,3 +84,23 @@ def test_lengths_and_pages_stay_where_a_cta_gave_up(longest, H_kv):
     v.copy_(vc)
     call()
     assert sl_out.tolist() == [44, 44] and int(count) == 3 + sum(-(-x // 16) - 3 for x in lens)
+
+
+@pytest.mark.parametrize("longest", [200, 700])
+def test_places_of_the_kept_ones_need_no_room_in_the_workspace(longest):
+    require_gpu()
+    mass, kc, vc, bt, lens = evict_case([longest, 90], 2, 3, 64, seed=longest)
+    got = []
+    for size in (256, sfv.kv_evict_workspace_size(2, 2, 3, 64), None):
+        m, k, v, sl = mass.cuda(), kc.cuda(), vc.cuda(), i32(lens).cuda()
+        kept = torch.full((2, 2, 3, 64), -7, dtype=torch.int32, device="cuda")
+        room = None if size is None else sfv.new_workspace(size + 256)  # nothing behind is written
+        ws = None if size is None else room[:size]
+        sfv.kv_evict(m, k, v, bt.cuda(), sl, 64, kept=kept, workspace=ws)
+        assert room is None or not room[256:].any()
+        got.append([m, k, v, sl, kept])
+    for other in got[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(got[0], other))
+    with pytest.raises(sfv.SFError) as e:
+        sfv.kv_evict(mass.cuda(), kc.cuda(), vc.cuda(), bt.cuda(), i32(lens).cuda(), 64, workspace=sfv.new_workspace(256))
+    assert e.value.status == 4
