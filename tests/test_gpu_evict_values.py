@@ -1,5 +1,8 @@
 """sf_kv_evict where it is easy to go wrong (GPU): lengths that it refuses on the device,
-and calls in which a CTA gave up.  Everything has to be equal."""
+calls in which a CTA gave up, and long contexts of whose weights more fall into one bin of
+the choice's first digit than shared memory has room for.  Everything has to be equal."""
+import math
+
 import pytest
 import torch
 
@@ -104,3 +107,51 @@ def test_places_of_the_kept_ones_need_no_room_in_the_workspace(longest):
     with pytest.raises(sfv.SFError) as e:
         sfv.kv_evict(mass.cuda(), kc.cuda(), vc.cuda(), bt.cuda(), i32(lens).cuda(), 64, workspace=sfv.new_workspace(256))
     assert e.value.status == 4
+
+
+def weights(kind, shape, g):
+    x = torch.rand(shape, generator=g, device="cuda")
+    if kind == "uniform":
+        return x
+    if kind == "equal":
+        return torch.full_like(x, 0.75)
+    if kind == "half zeros":
+        return torch.where(torch.rand(shape, generator=g, device="cuda") < 0.5, 0.0, x)
+    if kind == "neighbours":  # a few hundred steps of fp32 above 1: ties, too
+        return 1 + (x * 700).floor() * 2.0 ** -23
+    if kind == "two digits":  # one value of the first digit, many of the second, ties in the third
+        return 1 + (x * 2 ** 20).floor() * 2.0 ** -22
+    assert kind == "special"
+    x = torch.where(x < 0.3, -math.inf, torch.where(x < 0.6, math.nan, torch.where(x < 0.8, -0.0, 0.0)))
+    x[..., ::501] = math.inf
+    return x
+
+
+# heads of one CTA each (three and four an SM), and in clusters of two, four and eight
+@pytest.mark.parametrize("heads, L", [(500, 12000), (320, 9000), (120, 10000), (30, 20000), (9, 30000), (1, 30001)])
+@pytest.mark.parametrize("kind", ["uniform", "equal", "half zeros", "neighbours", "two digits", "special"])
+def test_more_keys_in_a_bin_than_shared_memory_has_room_for(heads, L, kind):
+    require_gpu()
+    g = torch.Generator("cuda").manual_seed(heads + L)
+    d, pages = 8, -(-L // 16)
+    mass = weights(kind, (1, 1, heads, pages * 16), g)
+    first_k, first_v = torch.randn(2, 1, pages, heads, 16, d, generator=g, device="cuda").bfloat16()
+    table = torch.randperm(pages, generator=g, device="cuda").int()[None]
+    value = mass[0, 0, :, :L].nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
+    for budget, first, recent in ((L // 3, 0, 0), (L * 7 // 10, 3, 60), (700, 4, 32)):
+        best = torch.sort(value[:, first:L - recent], dim=1, descending=True, stable=True)[1][:, :budget - first - recent] + first
+        ends = torch.cat([torch.arange(first, device="cuda"), torch.arange(L - recent, L, device="cuda")])
+        stay = torch.sort(torch.cat([best, ends.expand(heads, -1)], 1), 1)[0]
+        m, k, v, sl = mass.clone(), first_k.clone(), first_v.clone(), i32([L]).cuda()
+        kept = torch.empty(1, 1, heads, budget, dtype=torch.int32, device="cuda")
+        ws = sfv.new_workspace(256 + 4 * heads * budget + 256)
+        sfv.kv_evict(m, k, v, table, sl, budget, first=first, recent=recent, kept=kept, workspace=ws)
+        assert sfv.read_device_status(ws) == 0 and sl.tolist() == [budget]
+        assert torch.equal(kept[0, 0].long(), stay)
+        want = torch.zeros_like(mass[0, 0])
+        want[:, :budget] = mass[0, 0].gather(1, stay)
+        assert torch.equal(m[0, 0].nan_to_num(-3), want.nan_to_num(-3))
+        for new, old in ((k, first_k), (v, first_v)):
+            rows, before = (c[0, table[0].long()].transpose(0, 1).reshape(heads, pages * 16, d) for c in (new, old))
+            assert torch.equal(rows[:, :budget], before.gather(1, stay[..., None].expand(-1, -1, d)))
+            assert torch.equal(rows[:, budget:], before[:, budget:])
