@@ -40,11 +40,13 @@
  *     seq_lens[b] - n_q), and the LM-head projections read the weights;
  *     these, and the workspace, must already be in place when the previous
  *     kernel on the stream starts (so neither it nor a kernel it may overlap
- *     writes them; sf_kv_append says which of its calls may come in front of
- *     sf_verify_attention all the same).  Everything else (q, hidden states,
- *     the draft rows' K/V, logits, probabilities, tokens, uniforms,
- *     temperatures) may come from the previous kernel: every kernel waits for
- *     it before reading them.
+ *     writes them).  Three calls that write the cache hold the next kernel back
+ *     until their stores can be read, so that sf_verify_attention may follow all
+ *     the same: sf_kv_append (which says for which of its calls), sf_tree_commit
+ *     (without free_pages) and sf_kv_evict (its lengths and block table, too).
+ *     Everything else (q, hidden states, the draft rows' K/V, logits,
+ *     probabilities, tokens, uniforms, temperatures) may come from the
+ *     previous kernel: every kernel waits for it before reading them.
  */
 #ifndef SPECFLASH_VERIFY_H
 #define SPECFLASH_VERIFY_H

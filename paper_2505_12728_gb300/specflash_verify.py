@@ -308,7 +308,8 @@ def verify_attention(q, k_cache, v_cache, block_table, seq_lens, *, out=None, ls
     The keys and values in front of the n_q draft rows, the block table and the
     lengths are read before the kernel waits for the previous one on the stream: a
     kernel that lets its successor start early must not write them (kv_append says
-    which of its calls may precede this one)."""
+    which of its calls may precede this one; tree_commit without free_pages and
+    kv_evict may)."""
     B, n_q, H_q, d = q.shape
     num_pages, H_kv, page, d2 = k_cache.shape
     if block_table.dim() != 2 or block_table.shape[0] != B:
