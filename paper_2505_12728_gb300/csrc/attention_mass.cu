@@ -35,6 +35,7 @@
 #include <mutex>
 
 #include "attn_common.cuh"
+#include "layer_device.cuh"
 #include "sf_host.h"
 
 namespace sf {

@@ -23,7 +23,7 @@
 // of 28 + 8 heads of 128, 2 bytes off: 174 us, 52 on the boundary).
 #include <cmath>
 
-#include "sf_device.cuh"
+#include "layer_device.cuh"
 #include "sf_host.h"
 
 namespace sf {

@@ -40,7 +40,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "sf_device.cuh"
+#include "layer_device.cuh"
 #include "sf_host.h"
 
 namespace sf {

@@ -66,6 +66,7 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "layer_device.cuh"
 #include "sf_host.h"
 #include "shared_prefix_layout.h"
 

@@ -24,7 +24,7 @@
 // in order (a batch's loads in front of its stores) needs nothing but its own order.
 // Every warp takes the walk for itself: that is a few hundred cycles beside
 // loads that every one of them needs anyway, and a second launch costs more.
-#include "sf_device.cuh"
+#include "layer_device.cuh"
 #include "sf_host.h"
 
 namespace sf {
