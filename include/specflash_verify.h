@@ -669,7 +669,7 @@ int sf_tree_attention(const void *q, const void *k_cache, const void *v_cache,
 /* k_caches, v_caches  HOST arrays of num_layers device pointers, bf16        */
 /*              [num_pages][H_kv][16][head_dim] each, all with the same       */
 /*              block_table; 0 <= num_layers <= SF_MAX_LAYERS.  A page is in  */
-/*              one sequence's table only.                                    */
+/*              one sequence's table only, and a cache in the arrays once.    */
 /* num_accepted int32 [B]; out_tokens, path int32 [B][n_q] and row_weights    */
 /*              fp32 [B][n_q] may be NULL.                                    */
 /* head_dim a multiple of 8 in [8, 256]; H_kv <= 1024.                        */

@@ -4,9 +4,9 @@
 // K, V and weights are compacted in place.
 //
 // One CTA, or a cluster, per (layer, sequence, KV head); nothing is shared between
-// them but the pages, of which each has rows of its own.  Contexts of up to 256 or 512
-// tokens have a kernel of their own, kv_evict_short_kernel; the rest of this is about
-// kv_evict_kernel.
+// them but the pages, of which each has rows of its own.  Where the weights' width or the
+// table, whichever is less, has room for at most 256 or 512 tokens, contexts have a kernel of
+// their own, kv_evict_short_kernel; the rest of this is about kv_evict_kernel.
 //
 // Which keys.  The first and the last ones stay in any case; of those between, the
 // weights' bits, ordered as unsigned integers (positive values above negative ones, NaN
@@ -25,7 +25,7 @@
 // What bounds it: the rows' way out and in, 256 bytes at a time from all over the cache.  32
 // layers of 32 heads, 3008 -> 1024 keys: 195 us, 5.6 TB/s, 82 % of the copy rate (with 16-byte
 // loads and a barrier a round 350); 28 layers of 4 sequences and 4 heads, 8192 to 32768 ->
-// 4096 keys: 342 us, 83 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, or
+// 4096 keys: 340 us, 83 % (770).  Three CTAs a SM with two rounds of 32 KB each in flight, or
 // four with 24 KB (evict_launch), so that one's choice of keys runs beside another's rows (five
 // with 16 KB: 219 and 436).  The choice reads the weights three times, the second and third
 // time from L2: the first digit's histogram, the few keys of its bin to shared memory, where
@@ -711,11 +711,12 @@ struct EvictLaunch {
   int cluster, threads, smem;
 };
 
-// Weights of at most 256 tokens a head: 16 warps where no SM has more than two heads (8
+// The lengths are on the device, so `width` bounds them: the weights' or the table's, whichever
+// is less.  Of at most 256 tokens a head: 16 warps where no SM has more than two heads (8
 // heads of 250 tokens to 200: 11.9 us, with kv_evict_kernel 13.1),
-// else four, which leave room for eight heads an SM (2400 heads of 85 tokens to 12: 13.5 us, with
-// 16 warps 43, with kv_evict_kernel, three heads an SM and a chain of barriers, 56; of 250 to
-// 200: 90, 131, 120).  Of at most 512, many heads: 2400 of 500 tokens to 64 47 us, with
+// else four, which leave room for eight heads an SM (2400 heads of 85 tokens to 12: 12.2 us, with
+// 16 warps 43; in a table of 4096 tokens, which takes kv_evict_kernel, 27; of 250 to
+// 200: 90, with 16 warps 131, 120).  Of at most 512, many heads: 2400 of 500 tokens to 64 47 us, with
 // kv_evict_kernel 75, to 400 173 and 193 (but 128 heads to 400 21, 17.5).
 static EvictLaunch evict_launch(int tasks, int budget, int width, int sms) {
   const bool many = tasks > 2 * sms;
